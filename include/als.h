@@ -179,6 +179,76 @@ als_status als_loss(als_ctx *ctx, const als_csr *Y, const als_table *W, const al
 als_status als_topk(als_ctx *ctx, const als_table *Q, const als_table *H, const als_csr *exclude, int32_t k,
                     int32_t *ids, float *scores, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Answering from trained tables: a table in 4 bits an entry, scores against it, rules on scores, the best of them.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/* Embedding table in 4 bits an entry with one scale per group of `group` consecutive entries of a row (16, 32, 64 or
+ * 128, at most d): entry (r, c) stands for code(r, c) * scale(r, c / group), exactly (an fp32 number).
+ * codes: device [rows][d/2] bytes, rows one after the other; entry 2j in the low half of byte j, entry 2j+1 in the
+ * high half, in two's complement.  scales: device [rows][d/group] bf16, rows one after the other.  Both start at a
+ * multiple of their row's size (of 16 bytes where that is more), so any range of rows is such a table too. */
+typedef struct {
+    void *codes;
+    void *scales;
+    int64_t rows;
+    int32_t d;     /* 16, 32, 64 or 128 */
+    int32_t group;
+} als_qtable;
+
+/* Matrix of scores, row-major: element (q, i) at data[q*ld + i], 0 <= i < cols <= 2^31 - 1; ld >= cols, in elements.
+ * Rows need no alignment beyond the element's. */
+typedef struct {
+    void *data; /* device */
+    int64_t rows, cols, ld;
+    als_dtype dtype;
+} als_matrix;
+
+/* X in 4 bits an entry, into T's buffers (T->rows, T->d as X's): per group the scale is max|x| / 7 rounded to bf16 and
+ * a code is x / scale rounded to the nearest whole number (halves to even), kept within -7 .. 7.  A group whose scale
+ * rounds to zero has codes 0.  A group with an entry that is infinite or NaN has such a scale too and codes 0: all
+ * its entries read as NaN.  Asynchronous on `stream`, as everything below. */
+als_status als_quantize(als_ctx *ctx, const als_table *X, const als_qtable *T, void *stream);
+
+/* The values of T as an ordinary table (rounded to nearest even where X is bf16); X is written. */
+als_status als_dequantize(als_ctx *ctx, const als_qtable *T, const als_table *X, void *stream);
+
+/* S[q][i] = <Q[q], T[i]> for every row of Q and of T: Q in fp32 or bf16, S in either.  Queries keep their 24 bits,
+ * products and sums are fp32, S is rounded once.  S must not overlap Q or T. */
+als_status als_scores(als_ctx *ctx, const als_table *Q, const als_qtable *T, const als_matrix *S, void *stream);
+
+/* Rules that change a score x of row q and item i, in this order, in fp32:
+ *   history    c = how often row q of `history` stores item i (in any order; values are not read).  Where c > 0:
+ *              x = x > 0 ? x / repetition : x * repetition;  x = (x - frequency * c) - presence
+ *   bias       x = x + bias[i]
+ *   entries    x = x + the value that row q of `entries` stores for item i (the last one where there are several;
+ *              1 without values)
+ *   allowed    x = -inf where bit i % 32 of word i / 32 of row q is clear, whatever x is (NaN too)
+ * Every pointer may be NULL: no such rule.  Item ids outside 0 .. cols-1 in `history` and `entries` are passed over. */
+typedef struct {
+    const als_csr *history; /* rows and cols as the scores' */
+    const als_csr *entries; /* the same */
+    const float *bias;      /* device [cols] */
+    const uint32_t *allowed; /* device [rows][allowed_ld] words, or one row of them for all rows where allowed_ld = 0 */
+    int64_t allowed_ld;      /* 0, or at least (cols + 31) / 32 */
+    const float *penalties;  /* device [rows][3]: repetition, presence, frequency of each row; NULL: those below */
+    float repetition;        /* > 0 and finite, 1: none */
+    float presence, frequency; /* finite, 0: none */
+} als_rules;
+
+/* Y = X changed by the rules, rounded once to Y's type.  Y may be X itself (same data, ld and type); otherwise they
+ * must not overlap. */
+als_status als_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rules, const als_matrix *Y, void *stream);
+
+/* The best k items of every row of X changed by the rules (NULL: as they are), best first, equal scores by ascending
+ * id; scores of -inf and NaN are not returned: where fewer than k are left the tail holds id -1 and score -inf.
+ * ids: device int32 [rows*k], scores: device fp32 [rows*k] (unrounded), row q at q*k; 1 <= k <= ALS_TOPK_MAX_K.
+ * lse: device fp32 [rows] or NULL: log(sum_i exp(x_i / temperature)) over all items of the row, with which
+ * scores / temperature - lse are the log-probabilities of the returned ones; -inf for a row without a score above
+ * -inf, NaN for a row with a NaN that is not masked.  temperature > 0 and finite.  The order of all sums is fixed. */
+als_status als_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int32_t k,
+                      int32_t *ids, float *scores, float *lse, void *stream);
+
 /* Synchronise `stream` and report (then clear) the device-side error flag. */
 als_status als_status_sync(als_ctx *ctx, void *stream);
 

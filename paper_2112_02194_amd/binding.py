@@ -24,7 +24,8 @@ SOLVER_DIRECT, SOLVER_CG, SOLVER_CG_FREE = 0, 1, 2
 
 EXPORTS = ["als_create", "als_destroy", "als_gramian", "als_solve_rows", "als_epoch", "als_loss",
            "als_status_sync", "als_check_csr", "als_copy_probe", "als_set_timing", "als_get_timing",
-           "als_strerror", "als_last_error", "als_gramian_static", "als_static_last_error", "als_topk"]
+           "als_strerror", "als_last_error", "als_gramian_static", "als_static_last_error", "als_topk",
+           "als_quantize", "als_dequantize", "als_scores", "als_adjust", "als_select"]
 
 
 class c_als_csr(ctypes.Structure):
@@ -41,6 +42,22 @@ class c_als_params(ctypes.Structure):
     _fields_ = [("alpha", ctypes.c_float), ("lambda_", ctypes.c_float), ("path", ctypes.c_int32),
                 ("dual_max_k", ctypes.c_int32), ("split_nnz", ctypes.c_int32), ("solver", ctypes.c_int32),
                 ("cg_max_iters", ctypes.c_int32), ("cg_tol", ctypes.c_float)]
+
+
+class c_als_qtable(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("d", ctypes.c_int32),
+                ("group", ctypes.c_int32)]
+
+
+class c_als_matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("dtype", ctypes.c_int)]
+
+
+class c_als_rules(ctypes.Structure):
+    _fields_ = [("history", ctypes.POINTER(c_als_csr)), ("entries", ctypes.POINTER(c_als_csr)), ("bias", ctypes.c_void_p),
+                ("allowed", ctypes.c_void_p), ("allowed_ld", ctypes.c_int64), ("penalties", ctypes.c_void_p),
+                ("repetition", ctypes.c_float), ("presence", ctypes.c_float), ("frequency", ctypes.c_float)]
 
 
 class AlsError(RuntimeError):
@@ -83,6 +100,13 @@ def load_library(path: str = LIB_PATH):
     lib.als_gramian_static.restype = i32
     lib.als_topk.argtypes = [vp, P(c_als_table), P(c_als_table), P(c_als_csr), i32, vp, vp, vp]
     lib.als_topk.restype = i32
+    lib.als_quantize.argtypes = [vp, P(c_als_table), P(c_als_qtable), vp]
+    lib.als_dequantize.argtypes = [vp, P(c_als_qtable), P(c_als_table), vp]
+    lib.als_scores.argtypes = [vp, P(c_als_table), P(c_als_qtable), P(c_als_matrix), vp]
+    lib.als_adjust.argtypes = [vp, P(c_als_matrix), P(c_als_rules), P(c_als_matrix), vp]
+    lib.als_select.argtypes = [vp, P(c_als_matrix), P(c_als_rules), ctypes.c_float, i32, vp, vp, vp, vp]
+    for name in ("als_quantize", "als_dequantize", "als_scores", "als_adjust", "als_select"):
+        getattr(lib, name).restype = i32
     lib.als_static_last_error.argtypes = []
     lib.als_static_last_error.restype = ctypes.c_char_p
     _lib = lib
@@ -218,6 +242,142 @@ def als_topk(ctx: Context, Q: torch.Tensor, H: torch.Tensor, k: int, exclude: Op
     ctx._check(ctx.lib.als_topk(ctx.handle, ctypes.byref(tq), ctypes.byref(th), ctypes.byref(ex) if ex is not None else None,
                                 k, ids.data_ptr(), scores.data_ptr(), _stream()))
     return ids, scores
+
+
+@dataclass
+class QTable:
+    """Table in 4 bits an entry: uint8 codes [rows, d/2] and bf16 scales [rows, d/group], both contiguous.  A range of
+    rows of both is such a table too."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    @property
+    def shape(self):
+        return self.codes.shape[0], 2 * self.codes.shape[1]
+
+    @property
+    def group(self) -> int:
+        return 2 * self.codes.shape[1] // max(1, self.scales.shape[1])
+
+    def c(self) -> c_als_qtable:
+        codes, scales = self.codes, self.scales
+        if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16:
+            raise TypeError("codes must be uint8 and scales bfloat16")
+        if codes.dim() != 2 or scales.dim() != 2 or not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("codes and scales must be 2-D and contiguous")
+        rows, half = codes.shape
+        if scales.shape[0] != rows:
+            raise ValueError("codes and scales differ in rows")
+        return c_als_qtable(codes.data_ptr() or None, scales.data_ptr() or None, rows, 2 * half, self.group)
+
+
+@dataclass
+class Rules:
+    """What is done to scores [rows, cols], in this order; everything is optional.
+
+    ``history``: Csr of the items a row has had, an item as often as it was had; such scores are divided by
+    ``repetition`` (multiplied where negative), then lowered by ``frequency`` for every time and by ``presence`` once;
+    ``penalties`` (fp32 [rows, 3]: repetition, presence, frequency) takes the place of the three numbers.
+    ``bias`` (fp32 [cols]) and ``entries`` (Csr with values) are added.  ``allowed``: int32 words [rows or 1, >= cols/32],
+    bit i % 32 of word i // 32 clear: the score of item i is -inf."""
+    history: Optional[Csr] = None
+    repetition: float = 1.0
+    presence: float = 0.0
+    frequency: float = 0.0
+    penalties: Optional[torch.Tensor] = None
+    bias: Optional[torch.Tensor] = None
+    entries: Optional[Csr] = None
+    allowed: Optional[torch.Tensor] = None
+
+    def c(self, rows: int, cols: int) -> c_als_rules:
+        out = c_als_rules(repetition=self.repetition, presence=self.presence, frequency=self.frequency)
+        if self.history is not None:
+            out.history = ctypes.pointer(self.history.c())
+        if self.entries is not None:
+            out.entries = ctypes.pointer(self.entries.c())
+        if self.bias is not None:
+            if self.bias.dtype != torch.float32 or not self.bias.is_contiguous() or self.bias.shape != (cols,):
+                raise ValueError("bias must be contiguous float32 [cols]")
+            out.bias = self.bias.data_ptr()
+        if self.penalties is not None:
+            if self.penalties.dtype != torch.float32 or not self.penalties.is_contiguous() or self.penalties.shape != (rows, 3):
+                raise ValueError("penalties must be contiguous float32 [rows, 3]")
+            out.penalties = self.penalties.data_ptr()
+        if self.allowed is not None:
+            a = self.allowed
+            if a.dtype != torch.int32 or a.dim() != 2 or a.shape[0] not in (1, rows) or a.shape[1] < (cols + 31) // 32:
+                raise ValueError("allowed must be int32 [rows or 1, at least (cols + 31) // 32]")
+            if a.shape[1] > 1 and a.stride(1) != 1:
+                raise ValueError("allowed must have unit column stride")
+            out.allowed = a.data_ptr() or None
+            # one set for all rows: no step from row to row (an expanded tensor has none by itself)
+            out.allowed_ld = 0 if a.shape[0] == 1 else a.stride(0)
+        return out
+
+
+def _matrix(t: torch.Tensor) -> c_als_matrix:
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("scores must be 2-D with unit column stride")
+    if t.dtype == torch.float32:
+        dt = ALS_F32
+    elif t.dtype == torch.bfloat16:
+        dt = ALS_BF16
+    else:
+        raise TypeError("scores must be float32 or bfloat16")
+    rows, cols = t.shape
+    return c_als_matrix(t.data_ptr() or None, rows, cols, t.stride(0) if rows > 1 else max(t.stride(0), cols), dt)
+
+
+def als_quantize(ctx: Context, X: torch.Tensor, group: int = 32, out: Optional[QTable] = None) -> QTable:
+    """X in 4 bits an entry, one bf16 scale per ``group`` entries of a row (at most d, so 16 for d = 16)."""
+    tx = _table(X)
+    if out is None:
+        if group not in (16, 32, 64, 128) or group > X.shape[1]:
+            raise ValueError("group must be 16, 32, 64 or 128 and at most d")
+        out = QTable(torch.empty((X.shape[0], X.shape[1] // 2), dtype=torch.uint8, device=X.device),
+                     torch.empty((X.shape[0], X.shape[1] // group), dtype=torch.bfloat16, device=X.device))
+    ct = out.c()
+    ctx._check(ctx.lib.als_quantize(ctx.handle, ctypes.byref(tx), ctypes.byref(ct), _stream()))
+    return out
+
+
+def als_dequantize(ctx: Context, T: QTable, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """The values of T as an ordinary table."""
+    X = out if out is not None else torch.empty(T.shape, dtype=dtype, device=T.codes.device)
+    ct, tx = T.c(), _table(X)
+    ctx._check(ctx.lib.als_dequantize(ctx.handle, ctypes.byref(ct), ctypes.byref(tx), _stream()))
+    return X
+
+
+def als_scores(ctx: Context, Q: torch.Tensor, T: QTable, out: Optional[torch.Tensor] = None,
+               dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """Inner products of every row of Q with every row of T -> [Q rows, T rows], fp32 or bf16."""
+    S = out if out is not None else torch.empty((Q.shape[0], T.codes.shape[0]), dtype=dtype, device=Q.device)
+    tq, ct, cs = _table(Q), T.c(), _matrix(S)
+    ctx._check(ctx.lib.als_scores(ctx.handle, ctypes.byref(tq), ctypes.byref(ct), ctypes.byref(cs), _stream()))
+    return S
+
+
+def als_adjust(ctx: Context, S: torch.Tensor, rules: Rules, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """S changed by the rules, in place unless ``out`` (of S's shape, fp32 or bf16) is given."""
+    Y = out if out is not None else S
+    cs, cy, cr = _matrix(S), _matrix(Y), rules.c(*S.shape)
+    ctx._check(ctx.lib.als_adjust(ctx.handle, ctypes.byref(cs), ctypes.byref(cr), ctypes.byref(cy), _stream()))
+    return Y
+
+
+def als_select(ctx: Context, S: torch.Tensor, k: int, rules: Optional[Rules] = None, temperature: float = 1.0):
+    """Best k of every row of S changed by the rules -> (ids int32 [rows, k], scores fp32 [rows, k], lse fp32 [rows]).
+
+    ``scores / temperature - lse[:, None]`` are the log-probabilities of the returned items among all of the row."""
+    cs = _matrix(S)
+    cr = ctypes.byref(rules.c(*S.shape)) if rules is not None else None
+    ids = torch.empty((S.shape[0], max(k, 0)), dtype=torch.int32, device=S.device)
+    scores = torch.empty((S.shape[0], max(k, 0)), dtype=torch.float32, device=S.device)
+    lse = torch.empty((S.shape[0],), dtype=torch.float32, device=S.device)
+    ctx._check(ctx.lib.als_select(ctx.handle, ctypes.byref(cs), cr, temperature, k, ids.data_ptr(), scores.data_ptr(),
+                                  lse.data_ptr(), _stream()))
+    return ids, scores, lse
 
 
 def als_status_sync(ctx: Context) -> None:

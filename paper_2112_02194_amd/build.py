@@ -29,6 +29,10 @@ UNITS = [
     ("solve_rows.hip", "solve_rows", []),
     ("loss.hip", "loss", []),
     ("topk.hip", "topk", VGPR_FORM),
+    ("quantize.hip", "quantize", []),
+    ("scores.hip", "scores", []),
+    ("adjust.hip", "adjust", []),
+    ("select.hip", "select", []),
     ("cg_free.hip", "cg_free", []),
     ("dual_prepare.hip", "dual_prepare", []),
     ("dual_rows.hip", "dual_rows", VGPR_FORM),

@@ -1,5 +1,6 @@
 // C-ABI entry points of libals: argument validation, context and workspace management, and the
 // epoch / loss glue.  All arithmetic of the method lives in the kernel translation units.
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -125,6 +126,76 @@ static als_status check_solve_args(als_ctx *ctx, const als_csr *Y, const als_tab
     return ALS_OK;
 }
 
+static size_t elem_size(als_dtype t) { return t == ALS_F32 ? 4 : 2; }
+
+// Bytes [first, last) of a buffer; nothing where it is empty.
+struct Span {
+    uintptr_t first, last;
+    Span(const void *p, int64_t bytes) : first((uintptr_t)p), last((uintptr_t)p + (p && bytes > 0 ? (uintptr_t)bytes : 0)) {}
+    explicit Span(const als_table *t) : Span(t->data, t->rows > 0 ? ((t->rows - 1) * t->ld + t->d) * (int64_t)elem_size(t->dtype) : 0) {}
+    explicit Span(const als_matrix *m)
+        : Span(m->data, m->rows > 0 && m->cols > 0 ? ((m->rows - 1) * m->ld + m->cols) * (int64_t)elem_size(m->dtype) : 0) {}
+    bool meets(const Span &o) const { return first < last && o.first < o.last && first < o.last && o.first < last; }
+};
+static Span codes_span(const als_qtable *t) { return Span(t->codes, t->rows * (t->d / 2)); }
+static Span scales_span(const als_qtable *t) { return Span(t->scales, t->rows * (t->d / t->group) * 2); }
+
+static als_status check_qtable(als_ctx *ctx, const als_qtable *t) {
+    if (!t) return fail(ctx, ALS_EINVAL, "T is null");
+    if (!d_supported(t->d)) return fail(ctx, ALS_EDTYPE, "T: d must be 16, 32, 64 or 128");
+    if (!d_supported(t->group) || t->group > t->d) return fail(ctx, ALS_ESHAPE, "T: group must be 16, 32, 64 or 128 and at most d");
+    if (t->rows < 0) return fail(ctx, ALS_EINVAL, "T: negative row count");
+    if (t->rows > 0 && (!t->codes || !t->scales)) return fail(ctx, ALS_EINVAL, "T: codes or scales is null");
+    const uintptr_t row = t->d / 2 < 16 ? t->d / 2 : 16;
+    if ((uintptr_t)t->codes % row || (uintptr_t)t->scales % (uintptr_t)(2 * (t->d / t->group)))
+        return fail(ctx, ALS_ESHAPE, "T: codes and scales must start at a multiple of their row's size");
+    return ALS_OK;
+}
+
+static als_status check_matrix(als_ctx *ctx, const als_matrix *m, const char *name) {
+    if (!m) return fail(ctx, ALS_EINVAL, std::string(name) + " is null");
+    if (m->dtype != ALS_F32 && m->dtype != ALS_BF16) return fail(ctx, ALS_EDTYPE, std::string(name) + ": unknown dtype");
+    if (m->rows < 0 || m->cols < 0) return fail(ctx, ALS_EINVAL, std::string(name) + ": negative size");
+    if (m->cols > INT32_MAX) return fail(ctx, ALS_ESHAPE, std::string(name) + ": item ids must fit int32");
+    if (m->ld < m->cols) return fail(ctx, ALS_ESHAPE, std::string(name) + ": ld < cols");
+    if (m->rows > 0 && m->ld > INT64_MAX / 4 / m->rows) return fail(ctx, ALS_ESHAPE, std::string(name) + ": rows * ld is too large");
+    if (m->rows > 0 && m->cols > 0 && !m->data) return fail(ctx, ALS_EINVAL, std::string(name) + ": data is null");
+    if ((uintptr_t)m->data % elem_size(m->dtype)) return fail(ctx, ALS_ESHAPE, std::string(name) + ": data is not aligned to its elements");
+    return ALS_OK;
+}
+
+static als_status check_row_list(als_ctx *ctx, const als_csr *y, const als_matrix *X, const char *name) {
+    als_status st = check_csr_args(ctx, y, name);
+    if (st == ALS_OK && (y->rows != X->rows || y->cols != X->cols))
+        st = fail(ctx, ALS_ESHAPE, std::string(name) + " must have one row per row of scores and one column per item");
+    return st;
+}
+
+static als_status check_rules(als_ctx *ctx, const als_rules *r, const als_matrix *X) {
+    if (!r) return fail(ctx, ALS_EINVAL, "rules is null");
+    als_status st;
+    if (r->history && (st = check_row_list(ctx, r->history, X, "history")) != ALS_OK) return st;
+    if (r->entries && (st = check_row_list(ctx, r->entries, X, "entries")) != ALS_OK) return st;
+    if (r->allowed && r->allowed_ld != 0 && r->allowed_ld < (X->cols + 31) / 32)
+        return fail(ctx, ALS_ESHAPE, "allowed_ld must be 0 or at least (cols + 31) / 32");
+    if ((uintptr_t)r->bias % 4 || (uintptr_t)r->allowed % 4 || (uintptr_t)r->penalties % 4)
+        return fail(ctx, ALS_ESHAPE, "bias, allowed and penalties must be 4-byte aligned");
+    if (!(r->repetition > 0.f) || !std::isfinite(r->repetition)) return fail(ctx, ALS_EINVAL, "repetition must be > 0 and finite");
+    if (!std::isfinite(r->presence) || !std::isfinite(r->frequency)) return fail(ctx, ALS_EINVAL, "presence and frequency must be finite");
+    return ALS_OK;
+}
+
+static bool rules_meet(const als_rules *r, const als_matrix *X, const Span &out) {
+    auto list = [&](const als_csr *y) {
+        return y && (out.meets(Span(y->indptr, (y->rows + 1) * 8)) || out.meets(Span(y->indices, y->nnz * 4)) ||
+                     out.meets(Span(y->values, y->nnz * 4)));
+    };
+    const int64_t words = (X->cols + 31) / 32;
+    return list(r->history) || list(r->entries) || out.meets(Span(r->bias, X->cols * 4)) ||
+           out.meets(Span(r->allowed, (r->allowed_ld ? (X->rows - 1) * r->allowed_ld + words : words) * 4)) ||
+           out.meets(Span(r->penalties, X->rows * 12));
+}
+
 }  // namespace als
 
 using namespace als;
@@ -172,7 +243,7 @@ als_status als_destroy(als_ctx *ctx) {
     (void)hipSetDevice(ctx->device);
     (void)hipDeviceSynchronize();
     DevBuf *bufs[] = {&ctx->gram_partials, &ctx->lists, &ctx->seg_partials, &ctx->ztable, &ctx->entry_ids, &ctx->rtable, &ctx->small,
-                      &ctx->loss_partials, &ctx->topk_partials, &ctx->gram_w, &ctx->gram_h};
+                      &ctx->loss_partials, &ctx->topk_partials, &ctx->select_partials, &ctx->gram_w, &ctx->gram_h};
     for (DevBuf *b : bufs)
         if (b->p) (void)hipFree(b->p);
     if (ctx->hint_counts) (void)hipHostFree(ctx->hint_counts);
@@ -301,6 +372,75 @@ als_status als_topk(als_ctx *ctx, const als_table *Q, const als_table *H, const 
     }
     if (Q->rows == 0) return ALS_OK;
     return launch_topk(ctx, Q, H, exclude, k, ids, scores, (hipStream_t)stream);
+}
+
+als_status als_quantize(als_ctx *ctx, const als_table *X, const als_qtable *T, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if ((st = check_table(ctx, X, "X")) != ALS_OK) return st;
+    if ((st = check_qtable(ctx, T)) != ALS_OK) return st;
+    if (X->d != T->d || X->rows != T->rows) return fail(ctx, ALS_ESHAPE, "X and T differ in shape");
+    const Span x(X), codes = codes_span(T), scales = scales_span(T);
+    if (x.meets(codes) || x.meets(scales) || codes.meets(scales)) return fail(ctx, ALS_EALIAS, "T's buffers overlap X or each other");
+    if (X->rows == 0) return ALS_OK;
+    return launch_quantize(ctx, X, T, (hipStream_t)stream);
+}
+
+als_status als_dequantize(als_ctx *ctx, const als_qtable *T, const als_table *X, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if ((st = check_qtable(ctx, T)) != ALS_OK) return st;
+    if ((st = check_table(ctx, X, "X")) != ALS_OK) return st;
+    if (X->d != T->d || X->rows != T->rows) return fail(ctx, ALS_ESHAPE, "X and T differ in shape");
+    const Span x(X);
+    if (x.meets(codes_span(T)) || x.meets(scales_span(T))) return fail(ctx, ALS_EALIAS, "X overlaps T");
+    if (X->rows == 0) return ALS_OK;
+    return launch_dequantize(ctx, T, X, (hipStream_t)stream);
+}
+
+als_status als_scores(als_ctx *ctx, const als_table *Q, const als_qtable *T, const als_matrix *S, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if ((st = check_table(ctx, Q, "Q")) != ALS_OK) return st;
+    if ((st = check_qtable(ctx, T)) != ALS_OK) return st;
+    if ((st = check_matrix(ctx, S, "S")) != ALS_OK) return st;
+    if (Q->d != T->d) return fail(ctx, ALS_ESHAPE, "Q and T differ in d");
+    if (S->rows != Q->rows || S->cols != T->rows) return fail(ctx, ALS_ESHAPE, "S must have one row per query and one column per item");
+    const Span out(S);
+    if (out.meets(Span(Q)) || out.meets(codes_span(T)) || out.meets(scales_span(T))) return fail(ctx, ALS_EALIAS, "S overlaps Q or T");
+    if (S->rows == 0 || S->cols == 0) return ALS_OK;
+    return launch_scores(ctx, Q, T, S, (hipStream_t)stream);
+}
+
+als_status als_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rules, const als_matrix *Y, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if ((st = check_matrix(ctx, X, "X")) != ALS_OK) return st;
+    if ((st = check_rules(ctx, rules, X)) != ALS_OK) return st;
+    if ((st = check_matrix(ctx, Y, "Y")) != ALS_OK) return st;
+    if (X->rows != Y->rows || X->cols != Y->cols) return fail(ctx, ALS_ESHAPE, "X and Y differ in shape");
+    const Span out(Y);
+    const bool in_place = X->data == Y->data && X->ld == Y->ld && X->dtype == Y->dtype;
+    if ((!in_place && out.meets(Span(X))) || rules_meet(rules, X, out)) return fail(ctx, ALS_EALIAS, "Y overlaps X or the rules");
+    if (X->rows == 0 || X->cols == 0) return ALS_OK;
+    return launch_adjust(ctx, X, rules, Y, (hipStream_t)stream);
+}
+
+als_status als_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int32_t k, int32_t *ids,
+                      float *scores, float *lse, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if ((st = check_matrix(ctx, X, "X")) != ALS_OK) return st;
+    if (rules && (st = check_rules(ctx, rules, X)) != ALS_OK) return st;
+    if (!(temperature > 0.f) || !std::isfinite(temperature)) return fail(ctx, ALS_EINVAL, "temperature must be > 0 and finite");
+    if (k < 1 || k > ALS_TOPK_MAX_K) return fail(ctx, ALS_EINVAL, "k must be in [1, ALS_TOPK_MAX_K]");
+    if (X->rows > 0 && (!ids || !scores)) return fail(ctx, ALS_EINVAL, "ids or scores is null");
+    const Span in(X), out[3] = {Span(ids, X->rows * k * 4), Span(scores, X->rows * k * 4), Span(lse, X->rows * 4)};
+    for (int i = 0; i < 3; ++i)
+        if (out[i].meets(in) || (rules && rules_meet(rules, X, out[i])) || out[i].meets(out[(i + 1) % 3]))
+            return fail(ctx, ALS_EALIAS, "ids, scores and lse must not overlap X, the rules or each other");
+    if (X->rows == 0) return ALS_OK;
+    return launch_select(ctx, X, rules, temperature, k, ids, scores, lse, (hipStream_t)stream);
 }
 
 als_status als_check_csr(als_ctx *ctx, const als_csr *Y, void *stream) {
