@@ -30,7 +30,7 @@ UNITS = [
     ("loss.hip", "loss", []),
     ("topk.hip", "topk", VGPR_FORM),
     ("quantize.hip", "quantize", []),
-    ("scores.hip", "scores", []),
+    ("scores.hip", "scores", VGPR_FORM),
     ("adjust.hip", "adjust", []),
     ("select.hip", "select", []),
     ("cg_free.hip", "cg_free", []),
