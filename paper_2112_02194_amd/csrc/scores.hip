@@ -23,15 +23,18 @@ typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// The eight codes of a word as fp16 numbers: element e of the word is c[e % 4][e / 4].
+// The eight codes of a word as fp16 numbers: element e of the word is c[e % 4][e / 4].  (w & mask) ^ bits in one instruction:
+// the exclusive or turns two's complement into code + 8 beside filling in the exponent.
 __device__ __forceinline__ void unpack8(uint32_t w, halfx2 (&c)[4]) {
-    w ^= 0x88888888u;  // two's complement to code + 8
     const halfx2 k1 = {(_Float16)1032.f, (_Float16)1032.f}, k2 = {(_Float16)0.0625f, (_Float16)0.0625f}, k3 = {(_Float16)72.f, (_Float16)72.f};
     const uint32_t v = w >> 8;
-    c[0] = __builtin_bit_cast(halfx2, (w & 0x000f000fu) | 0x64006400u) - k1;
-    c[1] = __builtin_bit_cast(halfx2, (w & 0x00f000f0u) | 0x64006400u) * k2 - k3;
-    c[2] = __builtin_bit_cast(halfx2, (v & 0x000f000fu) | 0x64006400u) - k1;
-    c[3] = __builtin_bit_cast(halfx2, (v & 0x00f000f0u) | 0x64006400u) * k2 - k3;
+    auto put = [](uint32_t x, uint32_t mask, uint32_t bits) {
+        return __builtin_bit_cast(halfx2, (uint32_t)__builtin_amdgcn_bitop3_b32(x, mask, bits, 0x6a));
+    };
+    c[0] = put(w, 0x000f000fu, 0x64086408u) - k1;
+    c[1] = put(w, 0x00f000f0u, 0x64806480u) * k2 - k3;
+    c[2] = put(v, 0x000f000fu, 0x64086408u) - k1;
+    c[3] = put(v, 0x00f000f0u, 0x64806480u) * k2 - k3;
 }
 
 // ------------------------------------------------------------------------------------------------ few queries
@@ -128,177 +131,272 @@ template <int D, int G> struct ScoreSteps {
     static __device__ __forceinline__ int word(int t, int s, int h) { return t * (PART / 8) + h * STEPS + s; }  // of the row's D / 8
 };
 
+// How the results of a round, 32 queries x 64 items, are stored: a lane has items 2 a and 2 a + 1 of the round, so that it
+// stores two neighbours and half a wavefront 128 or 256 bytes of a row.  Loads and stores of a wavefront are counted together
+// and in order, and where a store may or may not have happened the compiler waits for all of them before it uses a load: on the
+// way from round to round there is no branch around a store.  Rows beyond the last query have an empty buffer behind them and are
+// dropped by the bounds check.
+enum class StoreAs {
+    BUFFER,  // fp32, or bf16 with rows that are 4-byte aligned
+    PLAIN,   // bf16 rows of any alignment: unaligned words without a bounds check, for 32 whole queries
+    GUARDED  // a branch around every element: the rest
+};
+
 template <bool BF_Q, bool BF_S, int D, int G>
-__global__ __launch_bounds__(256, 2) void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq,
-                                                             const uint32_t *__restrict__ codes, const uint16_t *__restrict__ scales,
-                                                             int64_t n, void *__restrict__ S, int64_t lds, int64_t qgroups,
-                                                             int64_t tiles_per_wave, int64_t units) {
+__global__ __launch_bounds__(256, 3)
+void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, const uint32_t *__restrict__ codes,
+                        const uint16_t *__restrict__ scales, int64_t n, void *__restrict__ S, int64_t lds, StoreAs as, unsigned qgroups,
+                        unsigned stretch, unsigned rounds, unsigned units) {
     typedef ScoreSteps<D, G> T;
     constexpr int NP = BF_Q ? 1 : 2, NS = D / G;  // parts of a query entry, scales of an item
     const int lane = threadIdx.x & 63, a = lane & 31, h = lane >> 5;
-    // Consecutive workgroups go to different XCDs: wavefronts that read the same items for other queries are kept on one.
-    const int64_t per_xcd = ((units + 7) / 8 + 3) / 4 * 4;
-    const int64_t in_xcd = (int64_t)(blockIdx.x >> 3) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t unit = (blockIdx.x & 7) * per_xcd + in_xcd;
-    if (in_xcd >= per_xcd || unit >= units) return;
-    const int64_t q0 = unit % qgroups * 32, first = unit / qgroups * tiles_per_wave;
-    const int64_t tiles = (n + 31) / 32, last = std::min(tiles, first + tiles_per_wave);
+    // Units of work, a workgroup's each: a block of `stretch` x `rounds` x 4 x 64 items is walked by `stretch` workgroups side by side
+    // for one group of 32 queries, then for the next group.  So what is written at one time lies close together in few rows,
+    // and a block's codes are read from the L2 by all but the first group (consecutive workgroups go to different XCDs, which
+    // have an L2 each: every XCD has its own run of units).
+    const unsigned per_xcd = (units + 7) / 8, unit = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per_xcd || unit >= units) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned block = unit / (qgroups * stretch), in_block = unit % (qgroups * stretch);
+    const int64_t q0 = (int64_t)(in_block / stretch) * 32, spans = (n + 63) / 64;
+    const int64_t step = 4 * (int64_t)stretch, begin = block * (step * rounds);
+    const int64_t first = begin + 4 * (in_block % stretch) + wave, last = std::min(spans, begin + step * rounds);
 
-    // the queries as operands, shifted so that the largest finite entry of a row lies in [2^13, 2^14)
-    halfx8 A[T::PARTS][T::STEPS][NP];
+    // The queries as operands, in LDS for the four wavefronts (registers for them would halve the wavefronts), shifted so that
+    // the largest finite entry of a row lies in [2^13, 2^14).  Each wavefront makes every fourth step's.
+    constexpr int NSTEP = D / 16, MINE = (NSTEP + 3) / 4;
+    __shared__ u32x4 operand[NSTEP * NP * 64];
+    __shared__ uint32_t row_top[4][32];
+    __shared__ __align__(16) float back[32];  // 2^-shift of every row
     int shift;
     {
-        float x[T::PARTS][T::STEPS][8];
-        uint32_t top = 0;
+        float x[MINE][8];
+        uint32_t top = 0;  // the largest magnitude as bits, which order like the values
 #pragma unroll
-        for (int t = 0; t < T::PARTS; ++t)
+        for (int j = 0; j < MINE; ++j) {
+            const int i = 4 * j + wave;
+            Piece<BF_Q> p = piece_zero<BF_Q>();
+            if (i < NSTEP && q0 + a < nq) p = piece_load<BF_Q>(Q, (q0 + a) * ldq + 8 * T::word(i / T::STEPS, i % T::STEPS, h));
+            piece_floats<BF_Q>(p, x[j]);
 #pragma unroll
-            for (int s = 0; s < T::STEPS; ++s) {
-                Piece<BF_Q> p = piece_zero<BF_Q>();
-                if (q0 + a < nq) p = piece_load<BF_Q>(Q, (q0 + a) * ldq + 8 * T::word(t, s, h));
-                piece_floats<BF_Q>(p, x[t][s]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t m = __float_as_uint(x[t][s][e]) & 0x7fffffffu;
-                    top = max(top, m < 0x7f800000u ? m : 0u);
-                }
-            }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        shift = top ? 14 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) : 0;
-#pragma unroll
-        for (int t = 0; t < T::PARTS; ++t)
-#pragma unroll
-            for (int s = 0; s < T::STEPS; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int at = 2 * (e % 4) + e / 4;  // the order in which unpack8 leaves a word's codes
-                    const float v = ldexpf(x[t][s][e], shift);
-                    const _Float16 hi = (_Float16)v;
-                    A[t][s][0][at] = hi;
-                    if constexpr (NP == 2) {
-                        const float rest = v - (float)hi;  // NaN where v is not finite
-                        A[t][s][1][at] = rest == rest ? (_Float16)rest : (_Float16)0.f;
-                    }
-                }
-    }
-    // 2^-shift of the rows that this lane's results belong to: result v is <query 8 (v / 4) + 4 h + v % 4, item a>
-    auto shift_of = [&](int v) { return __shfl(shift, 8 * (v >> 2) + 4 * h + (v & 3)); };
-    float back[16];
-#pragma unroll
-    for (int v = 0; v < 16; ++v) back[v] = ldexpf(1.f, -shift_of(v));
-    const bool q_wide = __any(shift > 60 || shift < -60);
-
-    uint32_t w[T::PARTS][T::STEPS];
-    float sc[NS];
-    auto fetch = [&](int64_t tile) {
-        const int64_t item = std::min<int64_t>(tile * 32 + a, n - 1);
-#pragma unroll
-        for (int t = 0; t < T::PARTS; ++t) {
-            const uint32_t *at = codes + item * (D / 8) + T::word(t, 0, h);
-            if constexpr (T::STEPS == 2) {
-                const u32x2 v = *(const u32x2 *)at;
-                w[t][0] = v[0];
-                w[t][1] = v[1];
-            } else {
-                w[t][0] = *at;
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t m = __float_as_uint(x[j][e]) & 0x7fffffffu;
+                top = max(top, m < 0x7f800000u ? m : 0u);
             }
         }
-        const uint16_t *ps = scales + item * NS;
-        if constexpr (NS == 1) {
-            sc[0] = bf16_to_f32(*ps);
-        } else {
-            uint32_t raw[NS / 2];
-            __builtin_memcpy(raw, __builtin_assume_aligned(ps, NS < 8 ? 2 * NS : 16), 2 * NS);
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        if (h == 0) row_top[wave][a] = top;
+        __syncthreads();
 #pragma unroll
-            for (int g = 0; g < NS; ++g) sc[g] = __uint_as_float(g & 1 ? raw[g / 2] & 0xffff0000u : raw[g / 2] << 16);
+        for (int i = 0; i < 4; ++i) top = max(top, row_top[i][a]);
+        shift = top ? 14 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) : 0;
+        if (threadIdx.x < 32) back[a] = ldexpf(1.f, -shift);
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const int i = 4 * j + wave;
+            halfx8 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int at = 2 * (e % 4) + e / 4;  // the order in which unpack8 leaves a word's codes
+                const float v = ldexpf(x[j][e], shift);
+                hi[at] = (_Float16)v;
+                const float rest = v - (float)hi[at];  // NaN where v is not finite
+                lo[at] = rest == rest ? (_Float16)rest : (_Float16)0.f;
+            }
+            if (i < NSTEP) {
+                operand[(i * NP) * 64 + lane] = __builtin_bit_cast(u32x4, hi);
+                if constexpr (NP == 2) operand[(i * NP + 1) * 64 + lane] = __builtin_bit_cast(u32x4, lo);
+            }
+        }
+        __syncthreads();
+    }
+    const bool q_wide = __any(shift > 60 || shift < -60);
+    if (first >= last) return;
+
+    uint32_t w[2][T::PARTS][T::STEPS], raw[2][(NS + 1) / 2];
+    auto fetch = [&](int64_t span) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int64_t item = std::min<int64_t>(span * 64 + 2 * a + c, n - 1);
+#pragma unroll
+            for (int t = 0; t < T::PARTS; ++t) {
+                const uint32_t *at = codes + item * (D / 8) + T::word(t, 0, h);
+                if constexpr (T::STEPS == 2) {
+                    const u32x2 v = *(const u32x2 *)at;
+                    w[c][t][0] = v[0];
+                    w[c][t][1] = v[1];
+                } else {
+                    w[c][t][0] = *at;
+                }
+            }
+            const uint16_t *ps = scales + item * NS;
+            if constexpr (NS == 1) raw[c][0] = *ps;
+            else __builtin_memcpy(raw[c], __builtin_assume_aligned(ps, NS < 8 ? 2 * NS : 16), 2 * NS);
+        }
+    };
+    // Waits for fetch's loads: at the end of a round the compiler knows how many stores came after them and lets those be.
+    auto arrived = [&] {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int t = 0; t < T::PARTS; ++t)
+#pragma unroll
+                for (int s = 0; s < T::STEPS; ++s) asm volatile("" : "+v"(w[c][t][s]));
+#pragma unroll
+            for (int i = 0; i < (NS + 1) / 2; ++i) asm volatile("" : "+v"(raw[c][i]));
         }
     };
 
-    fetch(first);
-    for (int64_t tile = first; tile < last; ++tile) {
-        float total[16];
-#pragma unroll
-        for (int v = 0; v < 16; ++v) total[v] = 0.f;
-        uint32_t cw[T::PARTS][T::STEPS];
-        float cs[NS];
-#pragma unroll
-        for (int t = 0; t < T::PARTS; ++t)
-#pragma unroll
-            for (int s = 0; s < T::STEPS; ++s) cw[t][s] = w[t][s];
-#pragma unroll
-        for (int g = 0; g < NS; ++g) cs[g] = sc[g];
-        if (tile + 1 < last) fetch(tile + 1);
+    float total[2][16];
+    // the round's sums, and the next round's codes on their way
+    auto compute = [&](int64_t next) {
+        uint32_t cw[2][T::PARTS][T::STEPS];
+        float cs[2][NS];
+        uint32_t top[2] = {0, 0};
         // Sums of shifted queries times a scale stay in fp32's range while neither factor is beyond 2^60 or below 2^-60.
         // Elsewhere the scales of an item are shifted too, and the results back in one step.
-        int k = 0;
         bool wide = q_wide;
-        {
-            uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int t = 0; t < T::PARTS; ++t)
+#pragma unroll
+                for (int s = 0; s < T::STEPS; ++s) cw[c][t][s] = w[c][t][s];
 #pragma unroll
             for (int g = 0; g < NS; ++g) {
-                const uint32_t m = __float_as_uint(cs[g]) & 0x7fffffffu;
-                top = max(top, m < 0x7f800000u ? m : 0u);
+                const uint32_t bits = g & 1 ? raw[c][g / 2] & 0xffff0000u : raw[c][g / 2] << 16, m = bits & 0x7fffffffu;
+                cs[c][g] = __uint_as_float(bits);
+                top[c] = max(top[c], m < 0x7f800000u ? m : 0u);
             }
-            wide = __any(wide || (top && (top > 0x5d800000u || top < 0x21800000u)));
-            if (wide) {
-                k = top ? __builtin_amdgcn_frexp_expf(__uint_as_float(top)) : 0;
-#pragma unroll
-                for (int g = 0; g < NS; ++g) cs[g] = ldexpf(cs[g], -k);
-            }
+            wide = wide || (top[c] && (top[c] > 0x5d800000u || top[c] < 0x21800000u));
         }
-#pragma unroll
-        for (int t = 0; t < T::PARTS; ++t) {
-            floatx16 acc;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[v] = 0.f;
-#pragma unroll
-            for (int s = 0; s < T::STEPS; ++s) {
-                halfx2 c[4];
-                unpack8(cw[t][s], c);
-                const u32x4 bits = {__builtin_bit_cast(uint32_t, c[0]), __builtin_bit_cast(uint32_t, c[1]),
-                                    __builtin_bit_cast(uint32_t, c[2]), __builtin_bit_cast(uint32_t, c[3])};
-                const halfx8 B = __builtin_bit_cast(halfx8, bits);
-#pragma unroll
-                for (int p = 0; p < NP; ++p) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(A[t][s][p], B, acc, 0, 0, 0);
-            }
-            const float scale = cs[t * T::PART / G];
-#pragma unroll
-            for (int v = 0; v < 16; ++v) total[v] = fmaf(acc[v], scale, total[v]);
-        }
+        fetch(next);
+        asm volatile("" ::: "memory");  // the operands are read from LDS in every round, not kept in registers
+        int k[2] = {0, 0};
+        wide = __any(wide);
         if (wide) {
 #pragma unroll
-            for (int v = 0; v < 16; ++v) total[v] = ldexpf(total[v], k - shift_of(v));
-        } else {
+            for (int c = 0; c < 2; ++c) {
+                k[c] = top[c] ? __builtin_amdgcn_frexp_expf(__uint_as_float(top[c])) : 0;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) total[v] *= back[v];
-        }
-        const int64_t item = tile * 32 + a;
-        if (q0 + 32 <= nq && tile * 32 + 32 <= n) {
-            if constexpr (BF_S) {
-                // neighbouring lanes swap so that each stores two items of one row: the even one row v, the odd one row v + 1
-                const uint32_t pick = lane & 1 ? 0x07060302u : 0x01000504u;
-                typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-                typedef float floatx2 __attribute__((ext_vector_type(2)));
-                typedef uint32_t u32_any __attribute__((aligned(2)));
-#pragma unroll
-                for (int v = 0; v < 16; v += 2) {
-                    const floatx2 f = {total[v], total[v + 1]};
-                    const uint32_t own = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
-                    const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)own, 0xB1, 0xf, 0xf, true);
-                    const uint32_t pair = __builtin_amdgcn_perm(own, other, pick);
-                    const int64_t row = q0 + 8 * (v >> 2) + 4 * h + (v & 3) + (lane & 1);
-                    *(u32_any *)((uint16_t *)S + row * lds + (item & ~(int64_t)1)) = pair;
-                }
-            } else {
-#pragma unroll
-                for (int v = 0; v < 16; ++v) ((float *)S)[(q0 + 8 * (v >> 2) + 4 * h + (v & 3)) * lds + item] = total[v];
+                for (int g = 0; g < NS; ++g) cs[c][g] = ldexpf(cs[c][g], -k[c]);
             }
-        } else if (item < n) {
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) total[c][v] = 0.f;
+#pragma unroll
+        for (int t = 0; t < T::PARTS; ++t) {
+            floatx16 acc[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[c][v] = 0.f;
+#pragma unroll
+            for (int s = 0; s < T::STEPS; ++s) {
+                halfx8 A[NP];
+#pragma unroll
+                for (int p = 0; p < NP; ++p) A[p] = __builtin_bit_cast(halfx8, operand[((t * T::STEPS + s) * NP + p) * 64 + lane]);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    halfx2 e[4];
+                    unpack8(cw[c][t][s], e);
+                    const u32x4 bits = {__builtin_bit_cast(uint32_t, e[0]), __builtin_bit_cast(uint32_t, e[1]),
+                                        __builtin_bit_cast(uint32_t, e[2]), __builtin_bit_cast(uint32_t, e[3])};
+                    const halfx8 B = __builtin_bit_cast(halfx8, bits);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A[p], B, acc[c], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float scale = cs[c][t * T::PART / G];
+#pragma unroll
+                for (int v = 0; v < 16; ++v) total[c][v] = fmaf(acc[c][v], scale, total[c][v]);
+            }
+        }
+        // result v is <query 8 (v / 4) + 4 h + v % 4, item 2 a + c>
+        if (wide) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const int64_t row = q0 + 8 * (v >> 2) + 4 * h + (v & 3);
-                if (row < nq) store_elem<BF_S>(S, row * lds + item, total[v]);
+                const int r = __shfl(shift, 8 * (v >> 2) + 4 * h + (v & 3));
+                total[0][v] = ldexpf(total[0][v], k[0] - r);
+                total[1][v] = ldexpf(total[1][v], k[1] - r);
             }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 b4 = *(const float4 *)(back + 8 * j + 4 * h);
+                const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    total[0][4 * j + v] *= b[v];
+                    total[1][4 * j + v] *= b[v];
+                }
+            }
+        }
+    };
+
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float floatx2 __attribute__((ext_vector_type(2)));
+    constexpr int ES = BF_S ? 2 : 4;
+    const int rows = (int)std::min<int64_t>(32, nq - q0);
+    int64_t span = first;
+    const int64_t whole = std::min(last, n / 64);
+    fetch(first);
+    arrived();
+    if (as == StoreAs::BUFFER) {
+        const uint32_t half = (uint32_t)(4 * lds * ES);  // bytes from a row to that of the upper half's lanes
+        const uint32_t place = h * half + a * 2 * ES;
+        for (; span < whole; span += step) {
+            compute(std::min(span + step, last - 1));
+            char *at = (char *)S + (q0 * lds + span * 64) * ES;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int row = 8 * (v >> 2) + (v & 3);  // and row + 4 in the upper half
+                // up to the end of the last of the two that exists
+                const uint32_t bytes = rows > row + 4 ? half + 64 * ES : rows > row ? 64 * ES : 0;
+                const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(at, 0, (int)bytes, 0x00020000);
+                const floatx2 f = {total[0][v], total[1][v]};
+                if constexpr (BF_S) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2)), rsrc, (int)place, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f), rsrc, (int)place, 0, 0);
+                at += lds * (ES * ((v & 3) == 3 ? 5 : 1));
+            }
+            arrived();
+        }
+    } else if (BF_S && as == StoreAs::PLAIN && rows == 32) {
+        for (; span < whole; span += step) {
+            compute(std::min(span + step, last - 1));
+            char *at = (char *)S + ((q0 + 4 * h) * lds + span * 64 + 2 * a) * ES;
+            asm volatile("" : "+v"(at));  // sixteen addresses are not kept from round to round
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                typedef uint32_t u32_any __attribute__((aligned(2)));
+                const floatx2 f = {total[0][v], total[1][v]};
+                *(u32_any *)at = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+                at += lds * (ES * ((v & 3) == 3 ? 5 : 1));
+            }
+            arrived();
+        }
+    }
+    for (; span < last; span += step) {
+        compute(std::min(span + step, last - 1));
+        const int64_t item = span * 64 + 2 * a;
+        char *at = (char *)S + ((q0 + 4 * h) * lds + item) * ES;
+        asm volatile("" : "+v"(at));
+        const int left = rows - 4 * h;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            if (8 * (v >> 2) + (v & 3) < left) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (item + c < n) {
+                        if constexpr (BF_S) ((__bf16 *)at)[c] = (__bf16)total[c][v];
+                        else ((float *)at)[c] = total[c][v];
+                    }
+            }
+            at += lds * (ES * ((v & 3) == 3 ? 5 : 1));
         }
     }
 }
@@ -319,11 +417,20 @@ static void scores_typed(const als_ctx *ctx, const als_table *Q, const als_qtabl
         else go(std::integral_constant<int, 2>{});
         return;
     }
-    const int64_t qgroups = (nq + 31) / 32, tiles = (n + 31) / 32;
-    const int64_t per = std::max<int64_t>(1, std::min<int64_t>(64, tiles * qgroups / ((int64_t)ctx->num_cu * 16)));
-    const int64_t units = (tiles + per - 1) / per * qgroups, per_xcd = ((units + 7) / 8 + 3) / 4 * 4;
-    hipLaunchKernelGGL((scores_tile_kernel<BF_Q, BF_S, D, G>), dim3((unsigned)(per_xcd / 4 * 8)), dim3(256), 0, s, Q->data, Q->ld, nq,
-                       (const uint32_t *)T->codes, (const uint16_t *)T->scales, n, S->data, S->ld, qgroups, per, units);
+    const int64_t qgroups = (nq + 31) / 32, spans = (n + 63) / 64;
+    // Rounds per wavefront and workgroups side by side, where the table is long enough for 16 wavefronts per compute unit.  What
+    // counts is how close together the writes under way are: 4 x 16, 16 x 16, 16 x 32: 246, 237, 267 us (512 queries x 1M items,
+    // d = 64, bf16), 562, 549, 656 us (d = 128, fp32), with rows at odd places, whose ends share lines, 270, 411, 412 us and 655,
+    // 786, 870 us.  Workgroups of one item stretch and all query groups at one time instead: 424, 898 us.
+    const int64_t rounds = std::max<int64_t>(1, std::min<int64_t>(4, spans * qgroups / ((int64_t)ctx->num_cu * 16)));
+    const int64_t stretch = std::max<int64_t>(1, std::min<int64_t>(16, spans / (32 * rounds)));
+    const int64_t units = (spans + 4 * rounds * stretch - 1) / (4 * rounds * stretch) * stretch * qgroups;
+    // a buffer's offsets have 32 bits: five rows must fit
+    const bool near = S->ld < (int64_t)1 << 27, words = !BF_S || (S->ld % 2 == 0 && (uintptr_t)S->data % 4 == 0);
+    const StoreAs as = !near ? StoreAs::GUARDED : words ? StoreAs::BUFFER : StoreAs::PLAIN;
+    hipLaunchKernelGGL((scores_tile_kernel<BF_Q, BF_S, D, G>), dim3((unsigned)((units + 7) / 8 * 8)), dim3(256), 0, s, Q->data, Q->ld, nq,
+                       (const uint32_t *)T->codes, (const uint16_t *)T->scales, n, S->data, S->ld, as, (unsigned)qgroups,
+                       (unsigned)stretch, (unsigned)rounds, (unsigned)units);
 }
 
 template <bool BF_Q, bool BF_S>
