@@ -10,28 +10,42 @@ namespace als {
 template <bool BF_IN, bool BF_OUT>
 __global__ __launch_bounds__(TILE_THREADS) void adjust_kernel(const void *X, int64_t ldx, void *Y, int64_t ldy, int64_t rows,
                                                               int64_t cols, int64_t work, RuleArgs rules) {
+    typedef TileRow<BF_IN> Row;
     extern __shared__ __align__(16) uint32_t words[];
-    uint32_t *count = words, *place = words + (rules.history.indptr ? TILE : 0);
     const int tid = threadIdx.x;
     for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
         const int64_t row = w % rows, first = w / rows * TILE;
-        const RowRules mine(rules, row);
-        float x[TILE_EPT / 4][4];
+        Row in;
+        in.load((const char *)X + row * ldx * (BF_IN ? 2 : 4), first, cols, tid);
+        RowRules<Row> mine;
+        mine.begin(rules, row, words, tid);
+        float x[Row::PIECES][Row::PER];
+        in.floats(x);
+        mine.apply(rules, first, cols, tid, x);
+        char *out = (char *)Y + (row * ldy + first) * (BF_OUT ? 2 : 4);
 #pragma unroll
-        for (int j = 0; j < TILE_EPT / 4; ++j) {
-            const int64_t at = first + tile_item(j, tid);
-            const int valid = (int)std::max<int64_t>(0, std::min<int64_t>(4, cols - at));
-            load4<BF_IN>(X, row * ldx + at, valid, x[j]);
-        }
-        tile_lists(rules, mine, first, count, place, tid);
+        for (int j = 0; j < Row::PIECES; ++j)
 #pragma unroll
-        for (int j = 0; j < TILE_EPT / 4; ++j) {
-            const int item = tile_item(j, tid);
-            const int64_t at = first + item;
-            const int valid = (int)std::max<int64_t>(0, std::min<int64_t>(4, cols - at));
-            apply_rules(rules, mine, first, item, valid, count, place, x[j]);
-            store4<BF_OUT>(Y, row * ldy + at, valid, x[j]);
-        }
+            for (int q = 0; q < Row::PER; q += 4) {
+                const int at = Row::item(j, tid) + q;
+                typedef __bf16 Half __attribute__((ext_vector_type(4)));
+                typedef Half AnyHalf __attribute__((aligned(2)));
+                typedef float Full __attribute__((ext_vector_type(4)));
+                typedef Full AnyFull __attribute__((aligned(4)));
+                const Full v = {x[j][q], x[j][q + 1], x[j][q + 2], x[j][q + 3]};
+                if (first + at + 4 <= cols) {
+                    if constexpr (BF_OUT) *(AnyHalf *)(out + at * 2) = __builtin_convertvector(v, Half);
+                    else *(AnyFull *)(out + at * 4) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (first + at + e < cols) {
+                            if constexpr (BF_OUT) ((__bf16 *)out)[at + e] = (__bf16)v[e];
+                            else ((float *)out)[at + e] = v[e];
+                        }
+                }
+            }
+        if (gridDim.x < work) __syncthreads();  // the next row's lists take the same words
     }
 }
 
@@ -39,15 +53,15 @@ als_status launch_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rul
     const RuleArgs a = rule_args(rules);
     const int64_t work = (X->cols + TILE - 1) / TILE * X->rows;
     const dim3 grid((unsigned)std::min<int64_t>(work, 1 << 22)), block(TILE_THREADS);
-    const size_t lds = (size_t)rule_words(a) * 4;
     const bool bi = X->dtype == ALS_BF16, bo = Y->dtype == ALS_BF16;
-#define ADJUST(I, O) \
-    hipLaunchKernelGGL((adjust_kernel<I, O>), grid, block, lds, s, X->data, X->ld, Y->data, Y->ld, X->rows, X->cols, work, a)
-    if (bi && bo) ADJUST(true, true);
-    else if (bi) ADJUST(true, false);
-    else if (bo) ADJUST(false, true);
-    else ADJUST(false, false);
-#undef ADJUST
+    auto go = [&](auto in, auto out) {
+        hipLaunchKernelGGL((adjust_kernel<in(), out()>), grid, block, rule_bytes(a), s, X->data, X->ld, Y->data, Y->ld, X->rows, X->cols,
+                           work, a);
+    };
+    if (bi && bo) go(std::true_type{}, std::true_type{});
+    else if (bi) go(std::true_type{}, std::false_type{});
+    else if (bo) go(std::false_type{}, std::true_type{});
+    else go(std::false_type{}, std::false_type{});
     ALS_HIP(ctx, hipGetLastError());
     return ALS_OK;
 }

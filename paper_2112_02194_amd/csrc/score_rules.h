@@ -1,9 +1,11 @@
 // Rules on scores (als_rules) as als_adjust and als_select evaluate them, a tile of one row at a time.
 //
-// A workgroup of 256 threads works on TILE consecutive items of one row.  Lists (history, entries) hold a row's items in any
-// order, so nothing says which of them lie in the tile: the workgroup walks the whole list once per tile and counts, in LDS,
-// how often every item of the tile occurs (history) and where it is stored last (entries).  Integer atomics: the result does
-// not depend on their order.  An element then reads its two words.
+// A workgroup of 256 threads works on TILE consecutive items of one row, a thread on pieces of 16 bytes of scores.  Lists
+// (history, entries) hold a row's items in any order, so nothing says which of them lie in the tile.  A word per item in LDS counts how
+// often it occurs (history) or tells where it is stored last (entries); integer atomics, so the order does not matter.
+//   short lists (up to LIST_REGS per lane): every wavefront holds the row's whole list in registers and enters the items that
+//                its own elements cover, so that a tile needs no barrier, and none of this where the list has no item in it
+//   long lists   the workgroup walks the list together, once per tile
 #pragma once
 
 #include "als_internal.h"
@@ -11,6 +13,7 @@
 namespace als {
 
 constexpr int TILE = 4096, TILE_THREADS = 256, TILE_EPT = TILE / TILE_THREADS;  // items per tile, threads, items per thread
+constexpr int LIST_REGS = 4;
 
 struct RowList {
     const int64_t *indptr;  // null: no such list
@@ -45,138 +48,200 @@ inline RuleArgs rule_args(const als_rules *r) {
     a.frequency = r->frequency;
     return a;
 }
-// LDS words that the lists need
-inline int rule_words(const RuleArgs &a) { return (a.history.indptr ? TILE : 0) + (a.entries.indptr ? TILE : 0); }
+// LDS bytes that the lists need
+inline size_t rule_bytes(const RuleArgs &a) { return ((a.history.indptr ? TILE : 0) + (a.entries.indptr ? TILE : 0)) * sizeof(uint32_t); }
 
-// Four consecutive elements; rows need not be aligned beyond their elements.
-template <bool BF16> __device__ __forceinline__ void load4(const void *base, int64_t off, int valid, float (&x)[4]) {
-    if (valid >= 4) {
-        if constexpr (BF16) {
-            typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
-            const u16x4 t = *(const u16x4 *)((const uint16_t *)base + off);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = bf16_to_f32(t[e]);
-        } else {
-            typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
-            const f32x4 t = *(const f32x4 *)((const float *)base + off);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = t[e];
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = e < valid ? load_elem<BF16>(base, off + e) : 0.f;
-    }
-}
-template <bool BF16> __device__ __forceinline__ void store4(void *base, int64_t off, int valid, const float (&x)[4]) {
-    if (valid >= 4) {
-        if constexpr (BF16) {
-            typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
-            u16x4 t;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = f32_to_bf16_rne(x[e]);
-            *(u16x4 *)((uint16_t *)base + off) = t;
-        } else {
-            typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
-            *(f32x4 *)((float *)base + off) = f32x4{x[0], x[1], x[2], x[3]};
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < valid) store_elem<BF16>(base, off + e, x[e]);
-    }
+// A value that all lanes read and no kernel of the call writes, through the scalar cache.
+template <class T> __device__ __forceinline__ T uniform_load(const T *p) {
+    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
 }
 
-// Item of element e of piece j of a thread, relative to its tile
-__device__ __forceinline__ int tile_item(int j, int tid) { return (j * TILE_THREADS + tid) * 4; }
+// A thread's elements of a tile: PIECES times PER consecutive ones, 16 bytes.  Rows need not be aligned beyond their elements.
+template <bool BF16> struct TileRow {
+    static constexpr int PER = BF16 ? 8 : 4, PIECES = TILE_EPT / PER;
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    Words raw[PIECES];
+    static __device__ __forceinline__ int item(int j, int tid) { return (j * TILE_THREADS + tid) * PER; }  // relative to the tile
+    // wavefront that has item `at` of the tile
+    static __device__ __forceinline__ int owner(int at) { return (at / (64 * PER)) % (TILE_THREADS / 64); }
 
-// The rules of one row.
-struct RowRules {
-    int64_t h0, h1, e0, e1;  // the row's parts of the lists; empty without a list
+    // `row`: the row's scores; items beyond cols are not read
+    __device__ __forceinline__ void load(const void *row, int64_t first, int64_t cols, int tid) {
+        typedef uint32_t Any __attribute__((ext_vector_type(4), aligned(2)));
+        if (first + TILE <= cols) {
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) raw[j] = *(const Any *)((const char *)row + (first + item(j, tid)) * (BF16 ? 2 : 4));
+        } else {
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) {
+                const int64_t at = first + item(j, tid);
+                if (at + PER <= cols) {
+                    raw[j] = *(const Any *)((const char *)row + at * (BF16 ? 2 : 4));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t w = 0;
+                        if constexpr (BF16) {
+                            if (at + 2 * e < cols) w = ((const uint16_t *)row)[at + 2 * e];
+                            if (at + 2 * e + 1 < cols) w |= (uint32_t)((const uint16_t *)row)[at + 2 * e + 1] << 16;
+                        } else if (at + e < cols) {
+                            w = ((const uint32_t *)row)[at + e];
+                        }
+                        raw[j][e] = w;
+                    }
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void floats(float (&x)[PIECES][PER]) const {
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+                x[j][e] = !BF16 ? __uint_as_float(raw[j][e]) : __uint_as_float(e & 1 ? raw[j][e / 2] & 0xffff0000u : raw[j][e / 2] << 16);
+    }
+};
+
+// One of a row's lists over the tiles that a workgroup works on.
+template <class Row, bool PLACES> struct TileList {
+    int64_t b = 0, e = 0;  // the row's part of the list; empty without a list
+    bool in_regs = false;
+    int32_t id[LIST_REGS];
+    uint32_t *words;  // TILE words in LDS
+
+    __device__ __forceinline__ void begin(const RowList &l, int64_t row, uint32_t *lds, int tid) {
+        words = lds;
+        b = e = 0;
+        if (l.indptr) {
+            b = uniform_load(l.indptr + row);
+            e = uniform_load(l.indptr + row + 1);
+            if (b < 0) b = 0;
+            if (e > l.nnz) e = l.nnz;
+        }
+        in_regs = e - b <= 64 * LIST_REGS;
+        if (b >= e || !in_regs) return;
+#pragma unroll
+        for (int r = 0; r < LIST_REGS; ++r) id[r] = b + 64 * r + (tid & 63) < e ? l.indices[b + 64 * r + (tid & 63)] : -1;
+        // the words of the wavefront's own elements
+#pragma unroll
+        for (int j = 0; j < Row::PIECES; ++j)
+#pragma unroll
+            for (int c = 0; c < Row::PER; c += 4) *(uint4 *)(words + Row::item(j, tid) + c) = make_uint4(0, 0, 0, 0);
+    }
+    // Enters the tile's items; true where the wavefront's words may be other than 0.  Long lists: all threads come here, with barriers.
+    __device__ __forceinline__ bool enter(const RowList &l, int64_t first, int tid) {
+        if (b >= e) return false;
+        if (in_regs) {
+            bool any = false;
+#pragma unroll
+            for (int r = 0; r < LIST_REGS; ++r) {
+                const int64_t at = (int64_t)id[r] - first;
+                const bool mine = at >= 0 && at < TILE && Row::owner((int)at) == tid >> 6;
+                if (__any(mine)) {
+                    any = true;
+                    if (mine) {
+                        if constexpr (PLACES) atomicMax(words + at, (uint32_t)(64 * r + (tid & 63)) + 1u);
+                        else atomicAdd(words + at, 1u);
+                    }
+                }
+            }
+            return any;
+        }
+        __syncthreads();  // the last tile's words have been read
+        for (int i = tid * 4; i < TILE; i += TILE_THREADS * 4) *(uint4 *)(words + i) = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+        for (int64_t i = b + tid; i < e; i += TILE_THREADS) {
+            const int64_t at = (int64_t)l.indices[i] - first;
+            if (at >= 0 && at < TILE) {
+                if constexpr (PLACES) atomicMax(words + at, (uint32_t)(i - b) + 1u);
+                else atomicAdd(words + at, 1u);
+            }
+        }
+        __syncthreads();
+        return true;
+    }
+    // The words are read: those that were entered become 0 again.
+    __device__ __forceinline__ void leave(int64_t first, int tid) {
+        if (b >= e || !in_regs) return;
+#pragma unroll
+        for (int r = 0; r < LIST_REGS; ++r) {
+            const int64_t at = (int64_t)id[r] - first;
+            if (at >= 0 && at < TILE && Row::owner((int)at) == tid >> 6) words[at] = 0;
+        }
+    }
+};
+
+// The rules of one row over the tiles that a workgroup works on.
+template <class Row> struct RowRules {
+    TileList<Row, false> history;
+    TileList<Row, true> entries;
     float r, p, f;
     const uint32_t *allowed;
-    __device__ RowRules(const RuleArgs &a, int64_t row) {
-        auto part = [row](const RowList &l, int64_t &b, int64_t &e) {
-            b = e = 0;
-            if (l.indptr) {
-                b = l.indptr[row];
-                e = l.indptr[row + 1];
-                if (b < 0) b = 0;
-                if (e > l.nnz) e = l.nnz;
-            }
-        };
-        part(a.history, h0, h1);
-        part(a.entries, e0, e1);
+    __device__ __forceinline__ void begin(const RuleArgs &a, int64_t row, uint32_t *lds, int tid) {
+        history.begin(a.history, row, lds, tid);
+        entries.begin(a.entries, row, lds + (a.history.indptr ? TILE : 0), tid);
         r = a.repetition; p = a.presence; f = a.frequency;
         if (a.penalties) {
-            r = a.penalties[3 * row];
-            p = a.penalties[3 * row + 1];
-            f = a.penalties[3 * row + 2];
+            r = uniform_load(a.penalties + 3 * row);
+            p = uniform_load(a.penalties + 3 * row + 1);
+            f = uniform_load(a.penalties + 3 * row + 2);
         }
         allowed = a.allowed ? a.allowed + row * a.allowed_ld : nullptr;
     }
-    __device__ bool listed() const { return h0 < h1 || e0 < e1; }
-};
-
-// Counts and places of the tile's items: `count` and `place` hold TILE words each (place: 0, or 1 + the entry's index in its row).
-// All threads of the workgroup call it; it ends with a barrier.
-__device__ __forceinline__ void tile_lists(const RuleArgs &a, const RowRules &row, int64_t first, uint32_t *count, uint32_t *place, int tid) {
-    const bool h = row.h0 < row.h1, e = row.e0 < row.e1;
-    if (!h && !e) return;
-    __syncthreads();  // the last tile's words have been read
-    for (int i = tid * 4; i < TILE; i += TILE_THREADS * 4) {
-        if (h) *(uint4 *)(count + i) = make_uint4(0, 0, 0, 0);
-        if (e) *(uint4 *)(place + i) = make_uint4(0, 0, 0, 0);
-    }
-    __syncthreads();
-    if (h)
-        for (int64_t i = row.h0 + tid; i < row.h1; i += TILE_THREADS) {
-            const int64_t at = (int64_t)a.history.indices[i] - first;
-            if (at >= 0 && at < TILE) atomicAdd(count + at, 1u);
-        }
-    if (e)
-        for (int64_t i = row.e0 + tid; i < row.e1; i += TILE_THREADS) {
-            const int64_t at = (int64_t)a.entries.indices[i] - first;
-            if (at >= 0 && at < TILE) atomicMax(place + at, (uint32_t)(i - row.e0) + 1u);
-        }
-    __syncthreads();
-}
-
-// x changed by the rules; `at`: items relative to the tile, a multiple of 4.  Every operation rounds by itself, as it is defined.
-__device__ __forceinline__ void apply_rules(const RuleArgs &a, const RowRules &row, int64_t first, int at, int valid,
-                                            const uint32_t *count, const uint32_t *place, float (&x)[4]) {
+    // x changed by the rules.  All threads of the workgroup come here.  Every operation rounds by itself, as it is defined.
+    __device__ __forceinline__ void apply(const RuleArgs &a, int64_t first, int64_t cols, int tid, float (&x)[Row::PIECES][Row::PER]) {
 #pragma clang fp contract(off)
-    if (row.h0 < row.h1) {
-        const uint4 c4 = *(const uint4 *)(count + at);
-        const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
-        if (c4.x | c4.y | c4.z | c4.w) {
+        const bool had = history.enter(a.history, first, tid), added = entries.enter(a.entries, first, tid);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c[e]) {
-                    const float v = x[e] > 0.f ? x[e] / row.r : x[e] * row.r;
-                    const float t = row.f * (float)c[e];
-                    x[e] = (v - t) - row.p;
+        for (int j = 0; j < Row::PIECES; ++j)
+#pragma unroll
+            for (int q = 0; q < Row::PER; q += 4) {
+                const int at = Row::item(j, tid) + q;
+                float *v = x[j] + q;
+                if (had) {
+                    const uint4 c4 = *(const uint4 *)(history.words + at);
+                    const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
+                    if (c4.x | c4.y | c4.z | c4.w) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (c[e]) {
+                                const float t = v[e] > 0.f ? v[e] / r : v[e] * r, u = f * (float)c[e];
+                                v[e] = (t - u) - p;
+                            }
+                    }
                 }
-        }
-    }
-    if (a.bias) {
-        float b[4];
-        load4<false>(a.bias, first + at, valid, b);
+                if (a.bias) {
+                    const float *bias = a.bias + first + at;
+                    if (first + at + 4 <= cols) {
+                        typedef float Any __attribute__((ext_vector_type(4), aligned(4)));
+                        const Any b4 = *(const Any *)bias;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = x[e] + b[e];
-    }
-    if (row.e0 < row.e1) {
-        const uint4 p4 = *(const uint4 *)(place + at);
-        const uint32_t p[4] = {p4.x, p4.y, p4.z, p4.w};
+                        for (int e = 0; e < 4; ++e) v[e] = v[e] + b4[e];
+                    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (p[e]) x[e] = x[e] + (a.entries.values ? a.entries.values[row.e0 + p[e] - 1] : 1.f);
-    }
-    if (row.allowed && valid > 0) {
-        const uint32_t bits = row.allowed[(first + at) >> 5] >> (at & 31);
+                        for (int e = 0; e < 4; ++e)
+                            if (first + at + e < cols) v[e] = v[e] + bias[e];
+                    }
+                }
+                if (added) {
+                    const uint4 p4 = *(const uint4 *)(entries.words + at);
+                    const uint32_t place[4] = {p4.x, p4.y, p4.z, p4.w};
+                    if (p4.x | p4.y | p4.z | p4.w) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (!((bits >> e) & 1u)) x[e] = -INFINITY;
+                        for (int e = 0; e < 4; ++e)
+                            if (place[e]) v[e] = v[e] + (a.entries.values ? a.entries.values[entries.b + place[e] - 1] : 1.f);
+                    }
+                }
+                if (allowed && first + at < cols) {
+                    const uint32_t bits = allowed[(first + at) >> 5] >> (at & 31);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!((bits >> e) & 1u)) v[e] = -INFINITY;
+                }
+            }
+        if (had) history.leave(first, tid);
+        if (added) entries.leave(first, tid);
     }
-}
+};
 
 }  // namespace als

@@ -1,11 +1,17 @@
 // The best k of every row of scores after the rules, and the log of the sum of the exponentials (als_select).
 //
 // A candidate is one whole number: the score as ordered bits above, the complement of the item id below, so that a larger
-// number is a better score, or an equal one with a smaller id.  A part of a row is walked a tile at a time: every thread keeps
-// the running maximum and sum of its elements' exponentials, and elements at least as good as the bar are appended to a buffer in
-// LDS.  The bar is a candidate that at least k of the part's reach: on the first tile the smallest of the four wavefronts'
-// ceil(k / 4)-th best lanes, later the k-th best of the buffer, found whenever that is full enough and then cut back to k.
-// The buffer has room for a whole tile beside what is kept, so no order of the scores and no number of equal ones overflows it.
+// number is a better score, or an equal one with a smaller id.
+//
+// select kernel  a part of a row (several parts where there are few rows), a tile at a time, one read of the scores.  Every
+//                thread keeps the running maximum and sum of its elements' exponentials.  Scores above the bar are appended
+//                to a buffer in LDS.  The bar is a score that at least k of the part reach: on the first tile just below the
+//                smallest of the four wavefronts' ceil(k / 4)-th best lanes, later the k-th best of the buffer, found whenever
+//                that is full enough and then cut back to k.  Items come in ascending order, so a later score that equals the
+//                bar's loses against the k that are there.  A tile with more candidates than there is room for (an ascending
+//                row) goes in a quarter or half at a time with the buffer cut back between: nothing overflows, whatever the
+//                order or the number of equal scores.
+// merge kernel   one workgroup per row: the parts' candidates, and their sums in a fixed order.
 #include <algorithm>
 #include <cmath>
 
@@ -13,237 +19,327 @@
 
 namespace als {
 
-constexpr int SELECT_KEEP = 1024;                // the buffer is cut back to k before a tile when it holds more
-constexpr int SELECT_CAP = SELECT_KEEP + TILE;   // candidates in LDS
 typedef unsigned long long Cand;
+constexpr int SELECT_KEEP = 1024;  // the buffer is cut back to k when it holds more than this after a tile
+constexpr int SELECT_CAP = 3072;   // room: what is kept and the largest piece of a tile, 2048
+constexpr int PART_SLOTS = 128;    // candidates that a part hands on at most
+constexpr int MERGE_THREADS = 1024;
+static_assert(SELECT_KEEP + TILE_THREADS * 8 <= SELECT_CAP && ALS_TOPK_MAX_K <= 64 && 4 * ALS_TOPK_MAX_K <= TILE_THREADS, "");
 
 __device__ __forceinline__ uint32_t ordered_bits(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);  // -0 becomes 0: equal scores
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
-__device__ __forceinline__ Cand candidate(float v, int64_t item) { return (Cand)ordered_bits(v) << 32 | (uint32_t)~(uint32_t)item; }
-constexpr uint32_t ORDERED_LOWEST = 0x007fffffu;  // ordered_bits(-inf): never a candidate
+__device__ __forceinline__ Cand candidate(float v, uint32_t item) { return (Cand)ordered_bits(v) << 32 | ~item; }
+constexpr uint32_t ORDERED_LOWEST = 0x007fffffu, ORDERED_ZERO = 0x80000000u;  // of -inf, which is never a candidate, and of 0
+// Scores equal to `o` are above the first, those equal to it are not above the second (`o` may be below -inf's).
+__device__ __forceinline__ float bar_below(uint32_t o) { return from_ordered(max(o == ORDERED_ZERO ? o - 1 : o, ORDERED_LOWEST + 1) - 1); }
+__device__ __forceinline__ float bar_at(Cand c) { return from_ordered(max((uint32_t)(c >> 32), ORDERED_LOWEST)); }
 
 // The j-th largest of the wavefront's 64 values, 1 <= j <= 64.
 __device__ __forceinline__ uint32_t wave_nth(uint32_t v, int j) {
     unsigned long long in = ~0ull;
     uint32_t result = 0;
+#pragma unroll
     for (int bit = 31; bit >= 0; --bit) {
         const unsigned long long ones = __ballot((v >> bit) & 1u) & in;
         const int c = __popcll(ones);
-        if (c >= j) {
-            in = ones;
-            result |= 1u << bit;
-        } else {
-            j -= c;
-            in &= ~ones;
-        }
+        const bool up = c >= j;
+        in = up ? ones : in & ~ones;
+        result |= up ? 1u << bit : 0u;
+        j -= up ? 0 : c;
     }
     return result;
 }
 
-struct SelectShared {
-    Cand buf[SELECT_CAP];
-    uint32_t hist[256];
-    uint32_t wave_bar[TILE_THREADS / 64];
-    float wave_m[TILE_THREADS / 64], wave_s[TILE_THREADS / 64];
-    Cand keep[ALS_TOPK_MAX_K];
-    int count, kept, digit, rest;
+template <int CAP> struct Buffer {
+    Cand cand[CAP], keep[ALS_TOPK_MAX_K];
+    uint32_t hist[256], wave_sum[4];
+    int kept, digit, rest, exact;
+
+    // The k best of cand[0, count) to its front (count > k), by counting digits from the top; candidates are all different.
+    // Returns a number that exactly k candidates reach.  All NT threads call it; it ends with a barrier.
+    template <int NT> __device__ Cand cut_back(int count, int k, int tid) {
+        Cand prefix = 0, mask = 0;
+        int want = k;
+        if (tid == 0) kept = 0;
+        for (int shift = 56; shift >= 0; shift -= 8) {
+            if (tid < 256) hist[tid] = 0;
+            __syncthreads();
+            for (int i = tid; i < count; i += NT)
+                if ((cand[i] & mask) == prefix) atomicAdd(&hist[(cand[i] >> shift) & 255], 1u);
+            __syncthreads();
+            uint32_t mine = 0, upto = 0;  // candidates with digit 255 - tid, and with that or a larger one
+            if (tid < 256) {
+                mine = upto = hist[255 - tid];
+                for (int m = 1; m < 64; m <<= 1) {
+                    const uint32_t o = __shfl_up(upto, m);
+                    if ((tid & 63) >= m) upto += o;
+                }
+                if ((tid & 63) == 63) wave_sum[tid >> 6] = upto;
+            }
+            __syncthreads();
+            if (tid < 256) {
+                for (int i = 0; i < tid >> 6; ++i) upto += wave_sum[i];
+                if ((int)upto >= want && (int)(upto - mine) < want) {
+                    digit = 255 - tid;
+                    rest = want - (int)(upto - mine);
+                    exact = (int)upto == want;
+                }
+            }
+            __syncthreads();
+            prefix |= (Cand)digit << shift;
+            mask |= (Cand)255 << shift;
+            want = rest;
+            if (exact) break;
+        }
+        for (int i = tid; i < count; i += NT)
+            if (cand[i] >= prefix) keep[atomicAdd(&kept, 1)] = cand[i];
+        __syncthreads();
+        if (tid < k) cand[tid] = keep[tid];
+        __syncthreads();
+        return prefix;
+    }
+    // The best k of cand[0, count), count <= the workgroup's threads, in order, as the row's answer.
+    __device__ void write_row(int count, int k, int64_t row, int32_t *ids, float *scores, int tid) const {
+        if (tid < k && tid >= count) {
+            ids[row * k + tid] = -1;
+            scores[row * k + tid] = -INFINITY;
+        }
+        if (tid < count) {
+            const Cand mine = cand[tid];
+            int rank = 0;
+            for (int i = 0; i < count; ++i) rank += cand[i] > mine;
+            if (rank < k) {
+                ids[row * k + rank] = (int32_t)~(uint32_t)mine;
+                scores[row * k + rank] = from_ordered((uint32_t)(mine >> 32));
+            }
+        }
+    }
 };
 
-// The k best of buf[0, count) to the front of buf (count > k) by counting the candidates' digits from the top; they are all
-// different.  Returns the k-th best.  All threads call it; it ends with a barrier.
-__device__ Cand cut_back(SelectShared &sh, int count, int k, int tid) {
-    Cand prefix = 0, mask = 0;
-    int want = k;
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        sh.hist[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < count; i += TILE_THREADS)
-            if ((sh.buf[i] & mask) == prefix) atomicAdd(&sh.hist[(sh.buf[i] >> shift) & 255], 1u);
-        __syncthreads();
-        int above = 0;  // candidates with a larger digit than tid
-        for (int d = 255; d > tid; --d) above += (int)sh.hist[d];
-        if (above < want && above + (int)sh.hist[tid] >= want) {
-            sh.digit = tid;
-            sh.rest = want - above;
-        }
-        __syncthreads();
-        prefix |= (Cand)sh.digit << shift;
-        mask |= (Cand)255 << shift;
-        want = sh.rest;
-        __syncthreads();
-    }
-    if (tid == 0) sh.kept = 0;
-    __syncthreads();
-    for (int i = tid; i < count; i += TILE_THREADS)
-        if (sh.buf[i] >= prefix) sh.keep[atomicAdd(&sh.kept, 1)] = sh.buf[i];
-    __syncthreads();
-    if (tid < k) sh.buf[tid] = sh.keep[tid];
-    if (tid == 0) sh.count = k;
-    __syncthreads();
-    return prefix;
-}
-
-// Running maximum and sum of exponentials, in units of exp2(scale * x).
+// Running maximum and sum of exponentials exp2(scale * (x - m)).
 struct ExpSum {
     float m = -INFINITY, s = 0.f;
-    __device__ void add(float om, float os, float scale) {
+    __device__ __forceinline__ void add(float om, float os, float scale) {
         const float top = fmaxf(m, om);
         if (top == -INFINITY) {  // nothing yet, but for a NaN
             s += os;
             return;
         }
-        s = (m == top ? s : s * exp2f((m - top) * scale)) + (om == top ? os : os * exp2f((om - top) * scale));
+        s = (m == top ? s : s * __builtin_amdgcn_exp2f((m - top) * scale)) + (om == top ? os : os * __builtin_amdgcn_exp2f((om - top) * scale));
         m = top;
+    }
+    __device__ __forceinline__ void over_lanes(float scale) {
+        for (int i = 1; i < 64; i <<= 1) add(__shfl_xor(m, i), __shfl_xor(s, i), scale);
+    }
+    __device__ __forceinline__ float log(float temperature) const {
+        return s != s ? s : m == -INFINITY || m == INFINITY ? m : m / temperature + logf(s);
     }
 };
 
-// Ends a row: the best k of buf[0, count), count <= 64 or cut back to k, in order.
-__device__ void write_row(SelectShared &sh, int k, int64_t row, int32_t *ids, float *scores, int tid) {
-    const int count = sh.count;
-    if (tid < k && tid >= count) {
-        ids[row * k + tid] = -1;
-        scores[row * k + tid] = -INFINITY;
-    }
-    if (tid < count) {
-        const Cand mine = sh.buf[tid];
-        int rank = 0;
-        for (int i = 0; i < count; ++i) rank += sh.buf[i] > mine;
-        if (rank < k) {
-            ids[row * k + rank] = (int32_t)~(uint32_t)mine;
-            scores[row * k + rank] = from_ordered((uint32_t)(mine >> 32));
-        }
-    }
-}
-__device__ __forceinline__ float log_sum(float m, float s, float temperature) {
-    if (s != s || m == -INFINITY || m == INFINITY) return s != s ? s : m;
-    return m / temperature + logf(s);
-}
+struct PartSum {
+    float m, s;
+    int count, unused;
+};
 
 // Workgroup w: part w % parts (tiles_per_part tiles) of row w / parts.  With one part a row it writes the answer, otherwise the
-// part's k best (0: none) and its exponential sum.
+// part's candidates and its exponential sum.
 template <bool BF16>
-__global__ __launch_bounds__(TILE_THREADS) void select_kernel(const void *__restrict__ X, int64_t ld, int64_t rows, int64_t cols, int k,
-                                                              int parts, int64_t tiles_per_part, float temperature, float scale,
-                                                              RuleArgs rules, Cand *__restrict__ part_cand, float2 *__restrict__ part_sum,
-                                                              int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
+__global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const void *__restrict__ X, int64_t ld, int64_t rows, int64_t cols, int k,
+                                                                 int parts, int64_t tiles_per_part, float temperature, float scale,
+                                                                 RuleArgs rules, Cand *__restrict__ part_cand, PartSum *__restrict__ part_sum,
+                                                                 int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
+    typedef TileRow<BF16> Row;
+    constexpr int PER = Row::PER, PIECES = Row::PIECES, WAVES = TILE_THREADS / 64;
     extern __shared__ __align__(16) uint32_t words[];
-    __shared__ SelectShared sh;
-    uint32_t *count = words, *place = words + (rules.history.indptr ? TILE : 0);
+    __shared__ Buffer<SELECT_CAP> buf;
+    __shared__ uint32_t wave_bar[WAVES];
+    __shared__ float wave_m[WAVES], wave_s[WAVES];
+    __shared__ int added[3];  // candidates of a tile, by turns: the next but one is cleared while this one is read
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t tiles = (cols + TILE - 1) / TILE;
     for (int64_t w = blockIdx.x; w < rows * parts; w += gridDim.x) {
         const int64_t row = w / parts;
-        const int part = (int)(w % parts);
-        const int64_t t0 = part * tiles_per_part, t1 = std::min<int64_t>(tiles, t0 + tiles_per_part);
-        const RowRules mine(rules, row);
+        const int64_t t0 = w % parts * tiles_per_part, t1 = std::min<int64_t>(tiles, t0 + tiles_per_part);
+        const char *scores_row = (const char *)X + row * ld * (BF16 ? 2 : 4);
+        Row in;
+        if (t0 < t1) in.load(scores_row, t0 * TILE, cols, tid);
+        RowRules<Row> mine;
+        mine.begin(rules, row, words, tid);
         ExpSum sum;
-        Cand bar = 0;
-        if (tid == 0) sh.count = 0;
+        float bar = -INFINITY;
+        int have = 0, turn = 0;
+        const int most = parts > 1 ? PART_SLOTS : TILE_THREADS;  // candidates at the end
+        if (tid < 3) added[tid] = 0;
         __syncthreads();
         for (int64_t t = t0; t < t1; ++t) {
             const int64_t first = t * TILE;
-            float x[TILE_EPT / 4][4];
+            float x[PIECES][PER];
+            in.floats(x);
+            if (t + 1 < t1) in.load(scores_row, first + TILE, cols, tid);
+            mine.apply(rules, first, cols, tid, x);
+            if (first + TILE > cols) {
 #pragma unroll
-            for (int j = 0; j < TILE_EPT / 4; ++j) {
-                const int64_t at = first + tile_item(j, tid);
-                const int valid = (int)std::max<int64_t>(0, std::min<int64_t>(4, cols - at));
-                load4<BF16>(X, row * ld + at, valid, x[j]);
+                for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        if (first + Row::item(j, tid) + e >= cols) x[j][e] = -INFINITY;
             }
-            tile_lists(rules, mine, first, count, place, tid);
             float top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < TILE_EPT / 4; ++j) {
-                const int item = tile_item(j, tid);
-                const int valid = (int)std::max<int64_t>(0, std::min<int64_t>(4, cols - first - item));
-                apply_rules(rules, mine, first, item, valid, count, place, x[j]);
+            for (int j = 0; j < PIECES; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (e >= valid) x[j][e] = -INFINITY;
-                    top = fmaxf(top, x[j][e]);
-                }
+                for (int e = 0; e < PER; ++e) top = fmaxf(top, x[j][e]);
+            const float m = fmaxf(sum.m, top), from = m == -INFINITY ? 0.f : m;
+            float part[2] = {0.f, 0.f};
+            if (__any(m == INFINITY)) {  // infinity - infinity below
+#pragma unroll
+                for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) part[0] += x[j][e] == from ? 1.f : __builtin_amdgcn_exp2f((x[j][e] - from) * scale);
+            } else {
+#pragma unroll
+                for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) part[e & 1] += __builtin_amdgcn_exp2f((x[j][e] - from) * scale);
             }
-            float part_s = 0.f;
-            const float from = top == -INFINITY ? 0.f : top;
-#pragma unroll
-            for (int j = 0; j < TILE_EPT / 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) part_s += x[j][e] == from ? 1.f : exp2f((x[j][e] - from) * scale);
-            sum.add(top, part_s, scale);
+            sum.s = (sum.m == m ? sum.s : sum.s * __builtin_amdgcn_exp2f((sum.m - from) * scale)) + (part[0] + part[1]);
+            sum.m = m;
 
-            if (bar == 0) {  // the part's first tile
-                const uint32_t nth = wave_nth(ordered_bits(top), (k + 3) / 4);
-                if (lane == 0) sh.wave_bar[wave] = nth;
+            if (t == t0) {
+                const uint32_t nth = wave_nth(ordered_bits(top), (k + WAVES - 1) / WAVES);
+                if (lane == 0) wave_bar[wave] = nth;
                 __syncthreads();
-                uint32_t least = sh.wave_bar[0];
-                for (int i = 1; i < TILE_THREADS / 64; ++i) least = min(least, sh.wave_bar[i]);
-                bar = (Cand)(least > ORDERED_LOWEST ? least : ORDERED_LOWEST + 1) << 32;
+                uint32_t least = wave_bar[0];
+#pragma unroll
+                for (int i = 1; i < WAVES; ++i) least = min(least, wave_bar[i]);
+                bar = bar_below(least);
             }
+            // The scores above the bar into the buffer: all pieces at once, or, if they do not fit, one after the other.
+            for (int j0 = 0, j1 = PIECES; j0 < PIECES;) {
+                int mine_above = 0;
+                if (__any(top > bar)) {
 #pragma unroll
-            for (int j = 0; j < TILE_EPT / 4; ++j)
+                    for (int j = 0; j < PIECES; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const Cand c = candidate(x[j][e], first + tile_item(j, tid) + e);
-                    if (x[j][e] > -INFINITY && c >= bar) sh.buf[atomicAdd(&sh.count, 1)] = c;
+                        for (int e = 0; e < PER; ++e) mine_above += j >= j0 && j < j1 && x[j][e] > bar;
                 }
-            __syncthreads();
-            const int have = sh.count;
-            __syncthreads();
-            if (have > SELECT_KEEP) bar = cut_back(sh, have, k, tid);
+                if (__any(mine_above)) {
+                    int upto = mine_above;
+#pragma unroll
+                    for (int m = 1; m < 64; m <<= 1) {
+                        const int o = __shfl_up(upto, m);
+                        if (lane >= m) upto += o;
+                    }
+                    int at = 0;
+                    if (lane == 63) at = atomicAdd(&added[turn], upto);
+                    at = have + __builtin_amdgcn_readlane(at, 63) + upto - mine_above;
+#pragma unroll
+                    for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                        for (int e = 0; e < PER; ++e)
+                            if (j >= j0 && j < j1 && x[j][e] > bar) {
+                                if (at < SELECT_CAP) buf.cand[at] = candidate(x[j][e], (uint32_t)(first + Row::item(j, tid) + e));
+                                ++at;
+                            }
+                }
+                __syncthreads();
+                int count = have + added[turn];
+                if (tid == 0) added[turn == 0 ? 2 : turn - 1] = 0;
+                turn = turn == 2 ? 0 : turn + 1;
+                if (count > SELECT_CAP) {
+                    j1 = 1;
+                    continue;
+                }
+                j0 = j1;
+                j1 = j0 + 1;
+                if (count > (t + 1 == t1 && j0 == PIECES ? most : SELECT_KEEP)) {
+                    bar = bar_at(buf.template cut_back<TILE_THREADS>(count, k, tid));
+                    count = k;
+                }
+                have = count;
+            }
         }
-        const int have = sh.count;
-        __syncthreads();
-        if (have > k) cut_back(sh, have, k, tid);
-
-        for (int m = 1; m < 64; m <<= 1) sum.add(__shfl_xor(sum.m, m), __shfl_xor(sum.s, m), scale);
+        sum.over_lanes(scale);
         if (lane == 0) {
-            sh.wave_m[wave] = sum.m;
-            sh.wave_s[wave] = sum.s;
+            wave_m[wave] = sum.m;
+            wave_s[wave] = sum.s;
         }
         __syncthreads();
         if (tid == 0) {
             ExpSum all;
-            for (int i = 0; i < TILE_THREADS / 64; ++i) all.add(sh.wave_m[i], sh.wave_s[i], scale);
-            if (parts > 1) part_sum[w] = make_float2(all.m, all.s);
-            else if (lse) lse[row] = log_sum(all.m, all.s, temperature);
+            for (int i = 0; i < WAVES; ++i) all.add(wave_m[i], wave_s[i], scale);
+            if (parts > 1) part_sum[w] = PartSum{all.m, all.s, have, 0};
+            else if (lse) lse[row] = all.log(temperature);
         }
         if (parts > 1) {
-            if (tid < k) part_cand[w * k + tid] = tid < sh.count ? sh.buf[tid] : 0;
+            if (tid < have) part_cand[w * PART_SLOTS + tid] = buf.cand[tid];
         } else {
-            write_row(sh, k, row, ids, scores, tid);
+            buf.write_row(have, k, row, ids, scores, tid);
         }
         __syncthreads();
     }
 }
 
 // The parts of a row together, one workgroup per row.
-__global__ __launch_bounds__(TILE_THREADS) void select_merge_kernel(int64_t rows, int k, int parts, float temperature, float scale,
-                                                                    const Cand *__restrict__ part_cand, const float2 *__restrict__ part_sum,
-                                                                    int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
-    __shared__ SelectShared sh;
-    const int tid = threadIdx.x;
+__global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t rows, int k, int parts, float temperature, float scale,
+                                                                     const Cand *__restrict__ part_cand, const PartSum *__restrict__ part_sum,
+                                                                     int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
+    constexpr int WAVES = MERGE_THREADS / 64, CAP = 2 * MERGE_THREADS;
+    __shared__ Buffer<CAP> buf;
+    __shared__ uint32_t wave_bar[WAVES];
+    __shared__ int count;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        Cand bar = 1;  // 0 stands for none
-        if (tid == 0) sh.count = 0;
+        const int total = parts * PART_SLOTS;
+        const Cand *cand = part_cand + row * total;
+        const PartSum *part = part_sum + row * parts;
+        uint32_t best = 0;
+        for (int i = tid; i < total; i += MERGE_THREADS)
+            if (i % PART_SLOTS < part[i / PART_SLOTS].count) best = max(best, (uint32_t)(cand[i] >> 32));
+        const uint32_t nth = wave_nth(best, (k + WAVES - 1) / WAVES);
+        if (lane == 0) wave_bar[wave] = nth;
+        if (tid == 0) count = 0;
         __syncthreads();
-        const int64_t total = (int64_t)parts * k;
-        for (int64_t i0 = 0; i0 < total; i0 += TILE) {
-            for (int i = tid; i < TILE && i0 + i < total; i += TILE_THREADS) {
-                const Cand c = part_cand[row * total + i0 + i];
-                if (c >= bar) sh.buf[atomicAdd(&sh.count, 1)] = c;
+        uint32_t least = wave_bar[0];  // at least k candidates reach it
+        for (int i = 1; i < WAVES; ++i) least = min(least, wave_bar[i]);
+        Cand bar = (Cand)least << 32;
+        for (int i = tid; i < total; i += MERGE_THREADS)
+            if (i % PART_SLOTS < part[i / PART_SLOTS].count && cand[i] >= bar) {
+                const int at = atomicAdd(&count, 1);
+                if (at < CAP) buf.cand[at] = cand[i];
             }
-            __syncthreads();
-            const int have = sh.count;
-            __syncthreads();
-            if (have > SELECT_KEEP || (have > k && i0 + TILE >= total)) bar = cut_back(sh, have, k, tid);
+        __syncthreads();
+        int have = count;
+        if (have > CAP) {  // more than there is room for (equal scores): 1024 at a time
+            have = 0;
+            for (int i0 = 0; i0 < total; i0 += MERGE_THREADS) {
+                __syncthreads();
+                if (tid == 0) count = have;
+                __syncthreads();
+                const int i = i0 + tid;
+                if (i < total && i % PART_SLOTS < part[i / PART_SLOTS].count && cand[i] >= bar) buf.cand[atomicAdd(&count, 1)] = cand[i];
+                __syncthreads();
+                have = count;
+                if (have > MERGE_THREADS) {
+                    bar = buf.cut_back<MERGE_THREADS>(have, k, tid);
+                    have = k;
+                }
+            }
         }
-        write_row(sh, k, row, ids, scores, tid);
-        if (tid == 0 && lse) {
+        __syncthreads();
+        if (have > 256) {
+            buf.cut_back<MERGE_THREADS>(have, k, tid);
+            have = k;
+        }
+        buf.write_row(have, k, row, ids, scores, tid);
+        if (wave == 0 && lse) {
             ExpSum all;
-            for (int i = 0; i < parts; ++i) all.add(part_sum[row * parts + i].x, part_sum[row * parts + i].y, scale);
-            lse[row] = log_sum(all.m, all.s, temperature);
+            for (int i = lane; i < parts; i += 64) all.add(part[i].m, part[i].s, scale);
+            all.over_lanes(scale);
+            if (lane == 0) lse[row] = all.log(temperature);
         }
         __syncthreads();
     }
@@ -253,33 +349,31 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
                          float *scores, float *lse, hipStream_t s) {
     const RuleArgs a = rule_args(rules);
     const int64_t tiles = (X->cols + TILE - 1) / TILE;
-    // enough workgroups to fill the card
-    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(tiles, (int64_t)ctx->num_cu * 2 / X->rows));
+    // parts of a row: about six workgroups per compute unit
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(tiles, (int64_t)ctx->num_cu * 6 / X->rows));
     const int64_t per = std::max<int64_t>(1, (tiles + parts - 1) / parts);
     parts = std::max<int64_t>(1, (tiles + per - 1) / per);
     const float scale = 1.44269504f / temperature;
     Cand *cand = nullptr;
-    float2 *sums = nullptr;
+    PartSum *sums = nullptr;
     if (parts > 1) {
-        const size_t cand_bytes = ((size_t)X->rows * parts * k * sizeof(Cand) + 255) / 256 * 256;
-        als_status st = ensure(ctx, ctx->select_partials, cand_bytes + (size_t)X->rows * parts * sizeof(float2));
+        const size_t cand_bytes = (size_t)X->rows * parts * PART_SLOTS * sizeof(Cand);
+        als_status st = ensure(ctx, ctx->select_partials, cand_bytes + (size_t)X->rows * parts * sizeof(PartSum));
         if (st != ALS_OK) return st;
         cand = (Cand *)ctx->select_partials.p;
-        sums = (float2 *)((char *)ctx->select_partials.p + cand_bytes);
+        sums = (PartSum *)((char *)ctx->select_partials.p + cand_bytes);
     }
     const dim3 grid((unsigned)std::min<int64_t>(X->rows * parts, 1 << 22)), block(TILE_THREADS);
-    const size_t lds = (size_t)rule_words(a) * 4;
-    const void *f = X->dtype == ALS_BF16 ? (const void *)select_kernel<true> : (const void *)select_kernel<false>;
-    ALS_HIP(ctx, hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * TILE * 4));
-    if (X->dtype == ALS_BF16)
-        hipLaunchKernelGGL((select_kernel<true>), grid, block, lds, s, X->data, X->ld, X->rows, X->cols, k, (int)parts, per, temperature,
+    const size_t lds = rule_bytes(a);
+    auto go = [&](auto bf) {
+        hipLaunchKernelGGL((select_kernel<bf()>), grid, block, lds, s, X->data, X->ld, X->rows, X->cols, k, (int)parts, per, temperature,
                            scale, a, cand, sums, ids, scores, lse);
-    else
-        hipLaunchKernelGGL((select_kernel<false>), grid, block, lds, s, X->data, X->ld, X->rows, X->cols, k, (int)parts, per, temperature,
-                           scale, a, cand, sums, ids, scores, lse);
+    };
+    if (X->dtype == ALS_BF16) go(std::true_type{});
+    else go(std::false_type{});
     if (parts > 1)
-        hipLaunchKernelGGL(select_merge_kernel, dim3((unsigned)std::min<int64_t>(X->rows, 1 << 22)), block, 0, s, X->rows, k, (int)parts,
-                           temperature, scale, (const Cand *)cand, (const float2 *)sums, ids, scores, lse);
+        hipLaunchKernelGGL(select_merge_kernel, dim3((unsigned)std::min<int64_t>(X->rows, 1 << 22)), dim3(MERGE_THREADS), 0, s, X->rows, k,
+                           (int)parts, temperature, scale, (const Cand *)cand, (const PartSum *)sums, ids, scores, lse);
     ALS_HIP(ctx, hipGetLastError());
     return ALS_OK;
 }
