@@ -6,15 +6,15 @@
 
 namespace als {
 
-// Workgroup w works on tile w / rows of row w % rows: the rows of one tile share its biases and a shared set of allowed items.
+// Workgroup (x, y) works on tile y of row x: the rows of one tile share its biases and a shared set of allowed items.
 template <bool BF_IN, bool BF_OUT>
 __global__ __launch_bounds__(TILE_THREADS) void adjust_kernel(const void *X, int64_t ldx, void *Y, int64_t ldy, int64_t rows,
-                                                              int64_t cols, int64_t work, RuleArgs rules) {
+                                                              uint32_t cols, RuleArgs rules) {
     typedef TileRow<BF_IN> Row;
     extern __shared__ __align__(16) uint32_t words[];
     const int tid = threadIdx.x;
-    for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
-        const int64_t row = w % rows, first = w / rows * TILE;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
+    for (uint32_t first = blockIdx.y * TILE; first < cols; first += gridDim.y * TILE) {
         Row in;
         in.load((const char *)X + row * ldx * (BF_IN ? 2 : 4), first, cols, tid);
         RowRules<Row> mine;
@@ -23,40 +23,41 @@ __global__ __launch_bounds__(TILE_THREADS) void adjust_kernel(const void *X, int
         in.floats(x);
         mine.apply(rules, first, cols, tid, x);
         char *out = (char *)Y + (row * ldy + first) * (BF_OUT ? 2 : 4);
+        const uint32_t left = cols - first;
 #pragma unroll
         for (int j = 0; j < Row::PIECES; ++j)
 #pragma unroll
             for (int q = 0; q < Row::PER; q += 4) {
-                const int at = Row::item(j, tid) + q;
+                const uint32_t at = Row::item(j, tid) + q;
                 typedef __bf16 Half __attribute__((ext_vector_type(4)));
                 typedef Half AnyHalf __attribute__((aligned(2)));
                 typedef float Full __attribute__((ext_vector_type(4)));
                 typedef Full AnyFull __attribute__((aligned(4)));
                 const Full v = {x[j][q], x[j][q + 1], x[j][q + 2], x[j][q + 3]};
-                if (first + at + 4 <= cols) {
+                if (at + 4 <= left) {
                     if constexpr (BF_OUT) *(AnyHalf *)(out + at * 2) = __builtin_convertvector(v, Half);
                     else *(AnyFull *)(out + at * 4) = v;
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (first + at + e < cols) {
+                        if (at + e < left) {
                             if constexpr (BF_OUT) ((__bf16 *)out)[at + e] = (__bf16)v[e];
                             else ((float *)out)[at + e] = v[e];
                         }
                 }
             }
-        if (gridDim.x < work) __syncthreads();  // the next row's lists take the same words
+        __syncthreads();  // the next tile's lists take the same words
     }
 }
 
 als_status launch_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rules, const als_matrix *Y, hipStream_t s) {
     const RuleArgs a = rule_args(rules);
-    const int64_t work = (X->cols + TILE - 1) / TILE * X->rows;
-    const dim3 grid((unsigned)std::min<int64_t>(work, 1 << 22)), block(TILE_THREADS);
+    const dim3 grid((unsigned)std::min<int64_t>(X->rows, 1 << 16), (unsigned)std::min<int64_t>((X->cols + TILE - 1) / TILE, 1 << 15));
+    const dim3 block(TILE_THREADS);
     const bool bi = X->dtype == ALS_BF16, bo = Y->dtype == ALS_BF16;
     auto go = [&](auto in, auto out) {
-        hipLaunchKernelGGL((adjust_kernel<in(), out()>), grid, block, rule_bytes(a), s, X->data, X->ld, Y->data, Y->ld, X->rows, X->cols,
-                           work, a);
+        hipLaunchKernelGGL((adjust_kernel<in(), out()>), grid, block, rule_bytes(a), s, X->data, X->ld, Y->data, Y->ld, X->rows,
+                           (uint32_t)X->cols, a);
     };
     if (bi && bo) go(std::true_type{}, std::true_type{});
     else if (bi) go(std::true_type{}, std::false_type{});

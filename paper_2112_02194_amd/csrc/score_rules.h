@@ -65,29 +65,30 @@ template <bool BF16> struct TileRow {
     // wavefront that has item `at` of the tile
     static __device__ __forceinline__ int owner(int at) { return (at / (64 * PER)) % (TILE_THREADS / 64); }
 
-    // `row`: the row's scores; items beyond cols are not read
-    __device__ __forceinline__ void load(const void *row, int64_t first, int64_t cols, int tid) {
+    // `row`: the row's scores; items from cols on are not read
+    __device__ __forceinline__ void load(const char *row, uint32_t first, uint32_t cols, int tid) {
         typedef uint32_t Any __attribute__((ext_vector_type(4), aligned(2)));
+        constexpr uint32_t ES = BF16 ? 2 : 4;
+        const char *tile = row + (uint64_t)first * ES;
         if (first + TILE <= cols) {
 #pragma unroll
-            for (int j = 0; j < PIECES; ++j) raw[j] = *(const Any *)((const char *)row + (first + item(j, tid)) * (BF16 ? 2 : 4));
+            for (int j = 0; j < PIECES; ++j) raw[j] = *(const Any *)(tile + (uint32_t)item(j, tid) * ES);
         } else {
 #pragma unroll
             for (int j = 0; j < PIECES; ++j) {
-                const int64_t at = first + item(j, tid);
-                if (at + PER <= cols) {
-                    raw[j] = *(const Any *)((const char *)row + at * (BF16 ? 2 : 4));
-                } else {
+                const uint32_t at = item(j, tid), left = cols - first;
+                raw[j] = Words{0, 0, 0, 0};
+                if (at + PER <= left) {
+                    raw[j] = *(const Any *)(tile + at * ES);
+                } else if (at < left) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        uint32_t w = 0;
                         if constexpr (BF16) {
-                            if (at + 2 * e < cols) w = ((const uint16_t *)row)[at + 2 * e];
-                            if (at + 2 * e + 1 < cols) w |= (uint32_t)((const uint16_t *)row)[at + 2 * e + 1] << 16;
-                        } else if (at + e < cols) {
-                            w = ((const uint32_t *)row)[at + e];
+                            if (at + 2 * e < left) raw[j][e] = ((const uint16_t *)tile)[at + 2 * e];
+                            if (at + 2 * e + 1 < left) raw[j][e] |= (uint32_t)((const uint16_t *)tile)[at + 2 * e + 1] << 16;
+                        } else if (at + e < left) {
+                            raw[j][e] = ((const uint32_t *)tile)[at + e];
                         }
-                        raw[j][e] = w;
                     }
                 }
             }
@@ -104,24 +105,28 @@ template <bool BF16> struct TileRow {
 
 // One of a row's lists over the tiles that a workgroup works on.
 template <class Row, bool PLACES> struct TileList {
-    int64_t b = 0, e = 0;  // the row's part of the list; empty without a list
-    bool in_regs = false;
-    int32_t id[LIST_REGS];
-    uint32_t *words;  // TILE words in LDS
+    const int32_t *ids;
+    int64_t begins = 0, count = 0;  // the row's part of the list; none without a list
+    int32_t id[LIST_REGS];          // short lists: entry 64 r + lane, -1 beyond
+    uint32_t *words;                // TILE words in LDS
 
+    __device__ __forceinline__ bool in_regs() const { return count <= 64 * LIST_REGS; }
     __device__ __forceinline__ void begin(const RowList &l, int64_t row, uint32_t *lds, int tid) {
         words = lds;
-        b = e = 0;
+        begins = count = 0;
         if (l.indptr) {
-            b = uniform_load(l.indptr + row);
-            e = uniform_load(l.indptr + row + 1);
+            int64_t b = uniform_load(l.indptr + row), e = uniform_load(l.indptr + row + 1);
             if (b < 0) b = 0;
             if (e > l.nnz) e = l.nnz;
+            if (e > b) {
+                begins = b;
+                count = e - b;
+            }
         }
-        in_regs = e - b <= 64 * LIST_REGS;
-        if (b >= e || !in_regs) return;
+        ids = l.indices + begins;
+        if (count == 0 || !in_regs()) return;
 #pragma unroll
-        for (int r = 0; r < LIST_REGS; ++r) id[r] = b + 64 * r + (tid & 63) < e ? l.indices[b + 64 * r + (tid & 63)] : -1;
+        for (int r = 0; r < LIST_REGS; ++r) id[r] = 64 * r + (tid & 63) < (int)count ? ids[64 * r + (tid & 63)] : -1;
         // the words of the wavefront's own elements
 #pragma unroll
         for (int j = 0; j < Row::PIECES; ++j)
@@ -129,14 +134,15 @@ template <class Row, bool PLACES> struct TileList {
             for (int c = 0; c < Row::PER; c += 4) *(uint4 *)(words + Row::item(j, tid) + c) = make_uint4(0, 0, 0, 0);
     }
     // Enters the tile's items; true where the wavefront's words may be other than 0.  Long lists: all threads come here, with barriers.
-    __device__ __forceinline__ bool enter(const RowList &l, int64_t first, int tid) {
-        if (b >= e) return false;
-        if (in_regs) {
+    __device__ __forceinline__ bool enter(uint32_t first, int tid) {
+        if (count == 0) return false;
+        if (in_regs()) {
             bool any = false;
 #pragma unroll
             for (int r = 0; r < LIST_REGS; ++r) {
-                const int64_t at = (int64_t)id[r] - first;
-                const bool mine = at >= 0 && at < TILE && Row::owner((int)at) == tid >> 6;
+                if (64 * r >= (int)count) break;
+                const uint32_t at = (uint32_t)id[r] - first;
+                const bool mine = at < TILE && Row::owner((int)at) == tid >> 6;
                 if (__any(mine)) {
                     any = true;
                     if (mine) {
@@ -150,10 +156,10 @@ template <class Row, bool PLACES> struct TileList {
         __syncthreads();  // the last tile's words have been read
         for (int i = tid * 4; i < TILE; i += TILE_THREADS * 4) *(uint4 *)(words + i) = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        for (int64_t i = b + tid; i < e; i += TILE_THREADS) {
-            const int64_t at = (int64_t)l.indices[i] - first;
-            if (at >= 0 && at < TILE) {
-                if constexpr (PLACES) atomicMax(words + at, (uint32_t)(i - b) + 1u);
+        for (int64_t i = tid; i < count; i += TILE_THREADS) {
+            const uint32_t at = (uint32_t)ids[i] - first;
+            if (at < TILE) {
+                if constexpr (PLACES) atomicMax(words + at, (uint32_t)i + 1u);
                 else atomicAdd(words + at, 1u);
             }
         }
@@ -161,12 +167,13 @@ template <class Row, bool PLACES> struct TileList {
         return true;
     }
     // The words are read: those that were entered become 0 again.
-    __device__ __forceinline__ void leave(int64_t first, int tid) {
-        if (b >= e || !in_regs) return;
+    __device__ __forceinline__ void leave(uint32_t first, int tid) {
+        if (!in_regs()) return;
 #pragma unroll
         for (int r = 0; r < LIST_REGS; ++r) {
-            const int64_t at = (int64_t)id[r] - first;
-            if (at >= 0 && at < TILE && Row::owner((int)at) == tid >> 6) words[at] = 0;
+            if (64 * r >= (int)count) break;
+            const uint32_t at = (uint32_t)id[r] - first;
+            if (at < TILE && Row::owner((int)at) == tid >> 6) words[at] = 0;
         }
     }
 };
@@ -189,58 +196,75 @@ template <class Row> struct RowRules {
         allowed = a.allowed ? a.allowed + row * a.allowed_ld : nullptr;
     }
     // x changed by the rules.  All threads of the workgroup come here.  Every operation rounds by itself, as it is defined.
-    __device__ __forceinline__ void apply(const RuleArgs &a, int64_t first, int64_t cols, int tid, float (&x)[Row::PIECES][Row::PER]) {
+    __device__ __forceinline__ void apply(const RuleArgs &a, uint32_t first, uint32_t cols, int tid, float (&x)[Row::PIECES][Row::PER]) {
 #pragma clang fp contract(off)
-        const bool had = history.enter(a.history, first, tid), added = entries.enter(a.entries, first, tid);
+        const bool had = history.enter(first, tid), added = entries.enter(first, tid);
+        const uint32_t left = cols - first;
+        if (had) {
 #pragma unroll
-        for (int j = 0; j < Row::PIECES; ++j)
+            for (int j = 0; j < Row::PIECES; ++j)
 #pragma unroll
-            for (int q = 0; q < Row::PER; q += 4) {
-                const int at = Row::item(j, tid) + q;
-                float *v = x[j] + q;
-                if (had) {
-                    const uint4 c4 = *(const uint4 *)(history.words + at);
+                for (int q = 0; q < Row::PER; q += 4) {
+                    const uint4 c4 = *(const uint4 *)(history.words + Row::item(j, tid) + q);
                     const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
                     if (c4.x | c4.y | c4.z | c4.w) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             if (c[e]) {
-                                const float t = v[e] > 0.f ? v[e] / r : v[e] * r, u = f * (float)c[e];
-                                v[e] = (t - u) - p;
+                                float &v = x[j][q + e];
+                                const float t = v > 0.f ? v / r : v * r, u = f * (float)c[e];
+                                v = (t - u) - p;
                             }
                     }
                 }
-                if (a.bias) {
-                    const float *bias = a.bias + first + at;
-                    if (first + at + 4 <= cols) {
-                        typedef float Any __attribute__((ext_vector_type(4), aligned(4)));
-                        const Any b4 = *(const Any *)bias;
+            history.leave(first, tid);
+        }
+        if (a.bias) {
+            const float *bias = a.bias + first;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = v[e] + b4[e];
+            for (int j = 0; j < Row::PIECES; ++j)
+#pragma unroll
+                for (int q = 0; q < Row::PER; q += 4) {
+                    const uint32_t at = Row::item(j, tid) + q;
+                    if (at + 4 <= left) {
+                        typedef float Any __attribute__((ext_vector_type(4), aligned(4)));
+                        const Any b4 = *(const Any *)(bias + at);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[j][q + e] = x[j][q + e] + b4[e];
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (first + at + e < cols) v[e] = v[e] + bias[e];
+                        for (int e = 0; e < 3; ++e)
+                            if (at + e < left) x[j][q + e] = x[j][q + e] + bias[at + e];
                     }
                 }
-                if (added) {
-                    const uint4 p4 = *(const uint4 *)(entries.words + at);
+        }
+        if (added) {
+            const float *values = a.entries.values ? a.entries.values + entries.begins - 1 : nullptr;
+#pragma unroll
+            for (int j = 0; j < Row::PIECES; ++j)
+#pragma unroll
+                for (int q = 0; q < Row::PER; q += 4) {
+                    const uint4 p4 = *(const uint4 *)(entries.words + Row::item(j, tid) + q);
                     const uint32_t place[4] = {p4.x, p4.y, p4.z, p4.w};
                     if (p4.x | p4.y | p4.z | p4.w) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (place[e]) v[e] = v[e] + (a.entries.values ? a.entries.values[entries.b + place[e] - 1] : 1.f);
+                            if (place[e]) x[j][q + e] = x[j][q + e] + (values ? values[place[e]] : 1.f);
                     }
                 }
-                if (allowed && first + at < cols) {
-                    const uint32_t bits = allowed[(first + at) >> 5] >> (at & 31);
+            entries.leave(first, tid);
+        }
+        if (allowed) {
+            const uint32_t *bits = allowed + (first >> 5);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!((bits >> e) & 1u)) v[e] = -INFINITY;
-                }
+            for (int j = 0; j < Row::PIECES; ++j) {
+                const uint32_t at = Row::item(j, tid);
+                const uint32_t word = (at < left ? bits[at >> 5] : 0u) >> (at & 31);
+#pragma unroll
+                for (int e = 0; e < Row::PER; ++e)
+                    if (!((word >> e) & 1u)) x[j][e] = -INFINITY;
             }
-        if (had) history.leave(first, tid);
-        if (added) entries.leave(first, tid);
+        }
     }
 };
 

@@ -39,16 +39,17 @@ __device__ __forceinline__ float bar_at(Cand c) { return from_ordered(max((uint3
 
 // The j-th largest of the wavefront's 64 values, 1 <= j <= 64.
 __device__ __forceinline__ uint32_t wave_nth(uint32_t v, int j) {
-    unsigned long long in = ~0ull;
+    unsigned long long in = ~0ull;  // lanes that agree with the bits found so far
     uint32_t result = 0;
-#pragma unroll
-    for (int bit = 31; bit >= 0; --bit) {
-        const unsigned long long ones = __ballot((v >> bit) & 1u) & in;
+#pragma unroll 4
+    for (int i = 0; i < 32; ++i) {
+        const unsigned long long ones = __ballot((int)v < 0) & in;
         const int c = __popcll(ones);
         const bool up = c >= j;
         in = up ? ones : in & ~ones;
-        result |= up ? 1u << bit : 0u;
+        result = 2 * result + up;
         j -= up ? 0 : c;
+        v <<= 1;
     }
     return result;
 }
@@ -119,37 +120,43 @@ template <int CAP> struct Buffer {
     }
 };
 
-// Running maximum and sum of exponentials exp2(scale * (x - m)).
+// Sum of exp(x / temperature) over some x, relative to the largest of them, m (-inf: none).  With c = m * scale as it was rounded
+// (scale = log2(e) / temperature) the sum is s 2^c: an element costs one multiply-add and one exponential, and the rounding
+// of c does no harm, since the same c is added in the end.  Where that product is out of range (scores near the type's
+// limits, infinities) the sum is s exp(m / temperature), its terms are 2^((x - m) scale), 1 for x = m.
 struct ExpSum {
     float m = -INFINITY, s = 0.f;
+    static __device__ __forceinline__ bool plain(float m, float scale) { return fabsf(m * scale) < 1e30f; }
+    // what a sum relative to m is multiplied by to be relative to top >= m
+    static __device__ __forceinline__ float factor(float m, float top, float scale) {
+        return m == top ? 1.f : __builtin_amdgcn_exp2f(plain(m, scale) && plain(top, scale) ? m * scale - top * scale : (m - top) * scale);
+    }
     __device__ __forceinline__ void add(float om, float os, float scale) {
         const float top = fmaxf(m, om);
-        if (top == -INFINITY) {  // nothing yet, but for a NaN
-            s += os;
-            return;
-        }
-        s = (m == top ? s : s * __builtin_amdgcn_exp2f((m - top) * scale)) + (om == top ? os : os * __builtin_amdgcn_exp2f((om - top) * scale));
+        s = s * factor(m, top, scale) + os * factor(om, top, scale);
         m = top;
     }
     __device__ __forceinline__ void over_lanes(float scale) {
+#pragma unroll 1
         for (int i = 1; i < 64; i <<= 1) add(__shfl_xor(m, i), __shfl_xor(s, i), scale);
     }
-    __device__ __forceinline__ float log(float temperature) const {
-        return s != s ? s : m == -INFINITY || m == INFINITY ? m : m / temperature + logf(s);
+    __device__ __forceinline__ float log(float temperature, float scale) const {
+        if (s != s || m == -INFINITY || m == INFINITY) return s != s ? s : m;
+        return plain(m, scale) ? (m * scale + log2f(s)) * 0.693147181f : m / temperature + logf(s);
     }
 };
 
 struct PartSum {
     float m, s;
-    int count, unused;
+    uint32_t best, unused;  // the best candidate's score, ordered; 0: none
 };
 
-// Workgroup w: part w % parts (tiles_per_part tiles) of row w / parts.  With one part a row it writes the answer, otherwise the
-// part's candidates and its exponential sum.
-template <bool BF16>
-__global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const void *__restrict__ X, int64_t ld, int64_t rows, int64_t cols, int k,
-                                                                 int parts, int64_t tiles_per_part, float temperature, float scale,
-                                                                 RuleArgs rules, Cand *__restrict__ part_cand, PartSum *__restrict__ part_sum,
+// Workgroup (x, y): part x (tiles_per_part tiles) of row y.  With one part a row it writes the answer, otherwise the part's
+// candidates, 0 in the slots that are left, and its exponential sum.
+template <bool BF16, bool RULES>
+__global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const char *__restrict__ X, int64_t row_bytes, int64_t rows, uint32_t cols, int k,
+                                                                 uint32_t tiles_per_part, float temperature, float scale, RuleArgs rules,
+                                                                 Cand *__restrict__ part_cand, PartSum *__restrict__ part_sum,
                                                                  int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
     typedef TileRow<BF16> Row;
     constexpr int PER = Row::PER, PIECES = Row::PIECES, WAVES = TILE_THREADS / 64;
@@ -157,58 +164,60 @@ __global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const void *__r
     __shared__ Buffer<SELECT_CAP> buf;
     __shared__ uint32_t wave_bar[WAVES];
     __shared__ float wave_m[WAVES], wave_s[WAVES];
-    __shared__ int added[3];  // candidates of a tile, by turns: the next but one is cleared while this one is read
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t tiles = (cols + TILE - 1) / TILE;
-    for (int64_t w = blockIdx.x; w < rows * parts; w += gridDim.x) {
-        const int64_t row = w / parts;
-        const int64_t t0 = w % parts * tiles_per_part, t1 = std::min<int64_t>(tiles, t0 + tiles_per_part);
-        const char *scores_row = (const char *)X + row * ld * (BF16 ? 2 : 4);
+    __shared__ int added[3];  // candidates of a tile, by turns: the last one is cleared while this one is read
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, parts = gridDim.x;
+    const uint32_t begin = blockIdx.x * tiles_per_part * TILE;
+    const uint32_t end = min(cols, (blockIdx.x + 1) * tiles_per_part * TILE);  // items of the part
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        const char *scores_row = X + row * row_bytes;
         Row in;
-        if (t0 < t1) in.load(scores_row, t0 * TILE, cols, tid);
+        if (begin < end) in.load(scores_row, begin, cols, tid);
         RowRules<Row> mine;
-        mine.begin(rules, row, words, tid);
+        if constexpr (RULES) mine.begin(rules, row, words, tid);
         ExpSum sum;
         float bar = -INFINITY;
         int have = 0, turn = 0;
         const int most = parts > 1 ? PART_SLOTS : TILE_THREADS;  // candidates at the end
         if (tid < 3) added[tid] = 0;
         __syncthreads();
-        for (int64_t t = t0; t < t1; ++t) {
-            const int64_t first = t * TILE;
+        for (uint32_t first = begin; first < end; first += TILE) {
             float x[PIECES][PER];
             in.floats(x);
-            if (t + 1 < t1) in.load(scores_row, first + TILE, cols, tid);
-            mine.apply(rules, first, cols, tid, x);
+            const bool last = first + TILE >= end;
+            if (!last) in.load(scores_row, first + TILE, cols, tid);
+            if constexpr (RULES) mine.apply(rules, first, cols, tid, x);
             if (first + TILE > cols) {
+                const uint32_t left = cols - first;
 #pragma unroll
                 for (int j = 0; j < PIECES; ++j)
 #pragma unroll
                     for (int e = 0; e < PER; ++e)
-                        if (first + Row::item(j, tid) + e >= cols) x[j][e] = -INFINITY;
+                        if (Row::item(j, tid) + e >= left) x[j][e] = -INFINITY;
             }
             float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < PIECES; ++j)
 #pragma unroll
                 for (int e = 0; e < PER; ++e) top = fmaxf(top, x[j][e]);
-            const float m = fmaxf(sum.m, top), from = m == -INFINITY ? 0.f : m;
+            const float m = fmaxf(sum.m, top);
             float part[2] = {0.f, 0.f};
-            if (__any(m == INFINITY)) {  // infinity - infinity below
+            if (__any(!ExpSum::plain(m, scale) && m != -INFINITY)) {
+                const float from = m == -INFINITY ? 0.f : m;
 #pragma unroll
                 for (int j = 0; j < PIECES; ++j)
 #pragma unroll
                     for (int e = 0; e < PER; ++e) part[0] += x[j][e] == from ? 1.f : __builtin_amdgcn_exp2f((x[j][e] - from) * scale);
             } else {
+                const float c = m == -INFINITY ? 0.f : m * scale;
 #pragma unroll
                 for (int j = 0; j < PIECES; ++j)
 #pragma unroll
-                    for (int e = 0; e < PER; ++e) part[e & 1] += __builtin_amdgcn_exp2f((x[j][e] - from) * scale);
+                    for (int e = 0; e < PER; ++e) part[e & 1] += __builtin_amdgcn_exp2f(fmaf(x[j][e], scale, -c));
             }
-            sum.s = (sum.m == m ? sum.s : sum.s * __builtin_amdgcn_exp2f((sum.m - from) * scale)) + (part[0] + part[1]);
+            sum.s = sum.s * ExpSum::factor(sum.m, m, scale) + (part[0] + part[1]);
             sum.m = m;
 
-            if (t == t0) {
+            if (first == begin) {
                 const uint32_t nth = wave_nth(ordered_bits(top), (k + WAVES - 1) / WAVES);
                 if (lane == 0) wave_bar[wave] = nth;
                 __syncthreads();
@@ -219,14 +228,12 @@ __global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const void *__r
             }
             // The scores above the bar into the buffer: all pieces at once, or, if they do not fit, one after the other.
             for (int j0 = 0, j1 = PIECES; j0 < PIECES;) {
-                int mine_above = 0;
                 if (__any(top > bar)) {
+                    int mine_above = 0;
 #pragma unroll
                     for (int j = 0; j < PIECES; ++j)
 #pragma unroll
                         for (int e = 0; e < PER; ++e) mine_above += j >= j0 && j < j1 && x[j][e] > bar;
-                }
-                if (__any(mine_above)) {
                     int upto = mine_above;
 #pragma unroll
                     for (int m = 1; m < 64; m <<= 1) {
@@ -241,7 +248,7 @@ __global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const void *__r
 #pragma unroll
                         for (int e = 0; e < PER; ++e)
                             if (j >= j0 && j < j1 && x[j][e] > bar) {
-                                if (at < SELECT_CAP) buf.cand[at] = candidate(x[j][e], (uint32_t)(first + Row::item(j, tid) + e));
+                                if (at < SELECT_CAP) buf.cand[at] = candidate(x[j][e], first + Row::item(j, tid) + e);
                                 ++at;
                             }
                 }
@@ -255,7 +262,7 @@ __global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const void *__r
                 }
                 j0 = j1;
                 j1 = j0 + 1;
-                if (count > (t + 1 == t1 && j0 == PIECES ? most : SELECT_KEEP)) {
+                if (count > (last && j0 == PIECES ? most : SELECT_KEEP)) {
                     bar = bar_at(buf.template cut_back<TILE_THREADS>(count, k, tid));
                     count = k;
                 }
@@ -268,26 +275,33 @@ __global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const void *__r
             wave_s[wave] = sum.s;
         }
         __syncthreads();
-        if (tid == 0) {
-            ExpSum all;
-            for (int i = 0; i < WAVES; ++i) all.add(wave_m[i], wave_s[i], scale);
-            if (parts > 1) part_sum[w] = PartSum{all.m, all.s, have, 0};
-            else if (lse) lse[row] = all.log(temperature);
-        }
+        ExpSum all;
+#pragma unroll 1
+        for (int i = 0; i < WAVES; ++i) all.add(wave_m[i], wave_s[i], scale);
         if (parts > 1) {
-            if (tid < have) part_cand[w * PART_SLOTS + tid] = buf.cand[tid];
+            const int64_t w = row * parts + blockIdx.x;
+            if (tid < PART_SLOTS) part_cand[w * PART_SLOTS + tid] = tid < have ? buf.cand[tid] : 0;
+            if (wave == 0) {
+                uint32_t best = 0;
+                for (int i = lane; i < have; i += 64) best = max(best, (uint32_t)(buf.cand[i] >> 32));
+                for (int m = 1; m < 64; m <<= 1) best = max(best, (uint32_t)__shfl_xor((int)best, m));
+                if (lane == 0) part_sum[w] = PartSum{all.m, all.s, best, 0};
+            }
         } else {
             buf.write_row(have, k, row, ids, scores, tid);
+            if (tid == 0 && lse) lse[row] = all.log(temperature, scale);
         }
         __syncthreads();
     }
 }
 
-// The parts of a row together, one workgroup per row.
-__global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t rows, int k, int parts, float temperature, float scale,
-                                                                     const Cand *__restrict__ part_cand, const PartSum *__restrict__ part_sum,
-                                                                     int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
-    constexpr int WAVES = MERGE_THREADS / 64, CAP = 2 * MERGE_THREADS;
+// The parts of a row together, one workgroup per row.  A score that at least k candidates reach rules almost all of them out
+// unread where there are many parts: the k-th best of the parts' best.  Where there are few they are all read once.
+constexpr int MERGE_FEW = 64;  // parts; they give a thread MERGE_FEW * PART_SLOTS / MERGE_THREADS = 8 slots
+__global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t rows, int k, int parts, float temperature, float scale, const Cand *__restrict__ part_cand,
+                                                                     const PartSum *__restrict__ part_sum, int32_t *__restrict__ ids,
+                                                                     float *__restrict__ scores, float *__restrict__ lse) {
+    constexpr int WAVES = MERGE_THREADS / 64, CAP = 2 * MERGE_THREADS, SLOTS = MERGE_FEW * PART_SLOTS / MERGE_THREADS;
     __shared__ Buffer<CAP> buf;
     __shared__ uint32_t wave_bar[WAVES];
     __shared__ int count;
@@ -296,21 +310,55 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
         const int total = parts * PART_SLOTS;
         const Cand *cand = part_cand + row * total;
         const PartSum *part = part_sum + row * parts;
-        uint32_t best = 0;
-        for (int i = tid; i < total; i += MERGE_THREADS)
-            if (i % PART_SLOTS < part[i / PART_SLOTS].count) best = max(best, (uint32_t)(cand[i] >> 32));
-        const uint32_t nth = wave_nth(best, (k + WAVES - 1) / WAVES);
-        if (lane == 0) wave_bar[wave] = nth;
         if (tid == 0) count = 0;
-        __syncthreads();
-        uint32_t least = wave_bar[0];  // at least k candidates reach it
-        for (int i = 1; i < WAVES; ++i) least = min(least, wave_bar[i]);
-        Cand bar = (Cand)least << 32;
-        for (int i = tid; i < total; i += MERGE_THREADS)
-            if (i % PART_SLOTS < part[i / PART_SLOTS].count && cand[i] >= bar) {
+        auto put = [&](Cand c, Cand bar) {
+            if (c >= bar) {
                 const int at = atomicAdd(&count, 1);
-                if (at < CAP) buf.cand[at] = cand[i];
+                if (at < CAP) buf.cand[at] = c;
             }
+        };
+        Cand bar;
+        ExpSum all;
+        if (parts <= MERGE_FEW) {
+            Cand c[SLOTS];
+            uint32_t best = 0;
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) {
+                c[i] = i * MERGE_THREADS + tid < total ? cand[i * MERGE_THREADS + tid] : 0;
+                best = max(best, (uint32_t)(c[i] >> 32));
+            }
+            if (wave == 0 && lane < parts) all.add(part[lane].m, part[lane].s, scale);
+            const uint32_t nth = wave_nth(best, (k + WAVES - 1) / WAVES);
+            if (lane == 0) wave_bar[wave] = nth;
+            __syncthreads();
+            uint32_t least = wave_bar[0];  // at least k candidates reach it, if there are as many
+            for (int i = 1; i < WAVES; ++i) least = min(least, wave_bar[i]);
+            bar = max((Cand)least << 32, (Cand)1);
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) put(c[i], bar);
+        } else {
+            // every wavefront for itself: the k-th best of the lanes' best, each of a few parts
+            uint32_t best = 0;
+            for (int i = lane; i < parts; i += 64) {
+                const PartSum p = part[i];
+                best = max(best, p.best);
+                if (wave == 0) all.add(p.m, p.s, scale);
+            }
+            bar = max((Cand)wave_nth(best, k) << 32, (Cand)1);
+            __syncthreads();
+            int taken = 0;  // parts that reach the bar so far: the wavefronts take turns
+            for (int i0 = 0; i0 < parts; i0 += 64) {
+                unsigned long long who = __ballot(i0 + lane < parts && part[min(i0 + lane, parts - 1)].best >= (uint32_t)(bar >> 32));
+                while (who) {
+                    const int p = i0 + __ffsll((long long)who) - 1;
+                    who &= who - 1;
+                    if (taken++ % WAVES != wave) continue;
+                    const Cand c0 = cand[p * PART_SLOTS + lane], c1 = cand[p * PART_SLOTS + 64 + lane];
+                    put(c0, bar);
+                    put(c1, bar);
+                }
+            }
+        }
         __syncthreads();
         int have = count;
         if (have > CAP) {  // more than there is room for (equal scores): 1024 at a time
@@ -319,8 +367,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
                 __syncthreads();
                 if (tid == 0) count = have;
                 __syncthreads();
-                const int i = i0 + tid;
-                if (i < total && i % PART_SLOTS < part[i / PART_SLOTS].count && cand[i] >= bar) buf.cand[atomicAdd(&count, 1)] = cand[i];
+                if (i0 + tid < total) put(cand[i0 + tid], bar);
                 __syncthreads();
                 have = count;
                 if (have > MERGE_THREADS) {
@@ -336,10 +383,8 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
         }
         buf.write_row(have, k, row, ids, scores, tid);
         if (wave == 0 && lse) {
-            ExpSum all;
-            for (int i = lane; i < parts; i += 64) all.add(part[i].m, part[i].s, scale);
             all.over_lanes(scale);
-            if (lane == 0) lse[row] = all.log(temperature);
+            if (lane == 0) lse[row] = all.log(temperature, scale);
         }
         __syncthreads();
     }
@@ -349,8 +394,8 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
                          float *scores, float *lse, hipStream_t s) {
     const RuleArgs a = rule_args(rules);
     const int64_t tiles = (X->cols + TILE - 1) / TILE;
-    // parts of a row: about six workgroups per compute unit
-    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(tiles, (int64_t)ctx->num_cu * 6 / X->rows));
+    // parts of a row: as many workgroups as the card holds at a time, four per compute unit
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(tiles, ((int64_t)ctx->num_cu * 4 + X->rows - 1) / X->rows));
     const int64_t per = std::max<int64_t>(1, (tiles + parts - 1) / parts);
     parts = std::max<int64_t>(1, (tiles + per - 1) / per);
     const float scale = 1.44269504f / temperature;
@@ -363,14 +408,17 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
         cand = (Cand *)ctx->select_partials.p;
         sums = (PartSum *)((char *)ctx->select_partials.p + cand_bytes);
     }
-    const dim3 grid((unsigned)std::min<int64_t>(X->rows * parts, 1 << 22)), block(TILE_THREADS);
-    const size_t lds = rule_bytes(a);
-    auto go = [&](auto bf) {
-        hipLaunchKernelGGL((select_kernel<bf()>), grid, block, lds, s, X->data, X->ld, X->rows, X->cols, k, (int)parts, per, temperature,
-                           scale, a, cand, sums, ids, scores, lse);
+    const dim3 grid((unsigned)parts, (unsigned)std::min<int64_t>(X->rows, 65535)), block(TILE_THREADS);
+    auto go = [&](auto bf, auto with_rules) {
+        hipLaunchKernelGGL((select_kernel<bf(), with_rules()>), grid, block, rule_bytes(a), s, (const char *)X->data,
+                           X->ld * (bf() ? 2 : 4), X->rows, (uint32_t)X->cols, k, (uint32_t)per, temperature, scale, a, cand, sums, ids,
+                           scores, lse);
     };
-    if (X->dtype == ALS_BF16) go(std::true_type{});
-    else go(std::false_type{});
+    const bool bf = X->dtype == ALS_BF16, any = a.history.indptr || a.entries.indptr || a.bias || a.allowed;
+    if (bf && any) go(std::true_type{}, std::true_type{});
+    else if (bf) go(std::true_type{}, std::false_type{});
+    else if (any) go(std::false_type{}, std::true_type{});
+    else go(std::false_type{}, std::false_type{});
     if (parts > 1)
         hipLaunchKernelGGL(select_merge_kernel, dim3((unsigned)std::min<int64_t>(X->rows, 1 << 22)), dim3(MERGE_THREADS), 0, s, X->rows, k,
                            (int)parts, temperature, scale, (const Cand *)cand, (const PartSum *)sums, ids, scores, lse);
