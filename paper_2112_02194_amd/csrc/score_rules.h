@@ -74,20 +74,21 @@ template <bool BF16> struct TileRow {
 #pragma unroll
             for (int j = 0; j < PIECES; ++j) raw[j] = *(const Any *)(tile + (uint32_t)item(j, tid) * ES);
         } else {
+            // the row's last tile: what is read beyond its end is the last element again
+            const uint32_t left = cols - first;
 #pragma unroll
             for (int j = 0; j < PIECES; ++j) {
-                const uint32_t at = item(j, tid), left = cols - first;
-                raw[j] = Words{0, 0, 0, 0};
+                const uint32_t at = item(j, tid);
                 if (at + PER <= left) {
                     raw[j] = *(const Any *)(tile + at * ES);
-                } else if (at < left) {
+                } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         if constexpr (BF16) {
-                            if (at + 2 * e < left) raw[j][e] = ((const uint16_t *)tile)[at + 2 * e];
-                            if (at + 2 * e + 1 < left) raw[j][e] |= (uint32_t)((const uint16_t *)tile)[at + 2 * e + 1] << 16;
-                        } else if (at + e < left) {
-                            raw[j][e] = ((const uint32_t *)tile)[at + e];
+                            const uint16_t *t = (const uint16_t *)tile;
+                            raw[j][e] = t[min(at + 2 * e, left - 1)] | (uint32_t)t[min(at + 2 * e + 1, left - 1)] << 16;
+                        } else {
+                            raw[j][e] = ((const uint32_t *)tile)[min(at + e, left - 1)];
                         }
                     }
                 }
@@ -219,6 +220,7 @@ template <class Row> struct RowRules {
                 }
             history.leave(first, tid);
         }
+        __builtin_amdgcn_sched_barrier(0);  // one rule after the other: their loads together take more registers than there are
         if (a.bias) {
             const float *bias = a.bias + first;
 #pragma unroll
@@ -233,11 +235,11 @@ template <class Row> struct RowRules {
                         for (int e = 0; e < 4; ++e) x[j][q + e] = x[j][q + e] + b4[e];
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 3; ++e)
-                            if (at + e < left) x[j][q + e] = x[j][q + e] + bias[at + e];
+                        for (int e = 0; e < 4; ++e) x[j][q + e] = x[j][q + e] + bias[min(at + e, left - 1)];
                     }
                 }
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (added) {
             const float *values = a.entries.values ? a.entries.values + entries.begins - 1 : nullptr;
 #pragma unroll
@@ -254,6 +256,7 @@ template <class Row> struct RowRules {
                 }
             entries.leave(first, tid);
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (allowed) {
             const uint32_t *bits = allowed + (first >> 5);
 #pragma unroll

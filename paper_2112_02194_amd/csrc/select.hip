@@ -37,21 +37,33 @@ constexpr uint32_t ORDERED_LOWEST = 0x007fffffu, ORDERED_ZERO = 0x80000000u;  //
 __device__ __forceinline__ float bar_below(uint32_t o) { return from_ordered(max(o == ORDERED_ZERO ? o - 1 : o, ORDERED_LOWEST + 1) - 1); }
 __device__ __forceinline__ float bar_at(Cand c) { return from_ordered(max((uint32_t)(c >> 32), ORDERED_LOWEST)); }
 
-// The j-th largest of the wavefront's 64 values, 1 <= j <= 64.
+// One value from lanes of the wavefront by lane moves (v_add_f32_dpp and the like): rows of 16 lanes first, then across them.
+// F is associative and commutative; the result is in lane 63.
+template <class T, class F> __device__ __forceinline__ T wave_scan(T x, T none, F &&f) {
+    auto step = [&](auto ctrl, auto rows) {
+        const int moved = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, x), ctrl(), rows(), 0xf, false);
+        x = f(x, __builtin_bit_cast(T, moved));
+    };
+    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});  // from 1, 2, 4, 8 lanes below in the row
+    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // the row's end to the next row: rows 1 and 3
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // lane 31 to rows 2 and 3
+    return x;  // of the lanes up to this one
+}
+template <class T, class F> __device__ __forceinline__ T wave_all(T x, T none, F &&f) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(x, none, f)), 63));
+}
+
+// A value that at least j of the wavefront's 64 reach, 1 <= j <= 64: the j-th largest without its last six bits (the lanes'
+// numbers take their place, so that no two values are equal and a rank has one owner).
 __device__ __forceinline__ uint32_t wave_nth(uint32_t v, int j) {
-    unsigned long long in = ~0ull;  // lanes that agree with the bits found so far
-    uint32_t result = 0;
-#pragma unroll 4
-    for (int i = 0; i < 32; ++i) {
-        const unsigned long long ones = __ballot((int)v < 0) & in;
-        const int c = __popcll(ones);
-        const bool up = c >= j;
-        in = up ? ones : in & ~ones;
-        result = 2 * result + up;
-        j -= up ? 0 : c;
-        v <<= 1;
-    }
-    return result;
+    v = (v & ~63u) | (63u - (threadIdx.x & 63));
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) before += (uint32_t)__builtin_amdgcn_readlane((int)v, i) > v;
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, __ffsll((long long)__ballot(before == j - 1)) - 1) & ~63u;
 }
 
 template <int CAP> struct Buffer {
@@ -111,7 +123,12 @@ template <int CAP> struct Buffer {
         if (tid < count) {
             const Cand mine = cand[tid];
             int rank = 0;
-            for (int i = 0; i < count; ++i) rank += cand[i] > mine;
+            int i = 0;
+            for (; i + 8 <= count; i += 8) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) rank += cand[i + u] > mine;
+            }
+            for (; i < count; ++i) rank += cand[i] > mine;
             if (rank < k) {
                 ids[row * k + rank] = (int32_t)~(uint32_t)mine;
                 scores[row * k + rank] = from_ordered((uint32_t)(mine >> 32));
@@ -137,8 +154,9 @@ struct ExpSum {
         m = top;
     }
     __device__ __forceinline__ void over_lanes(float scale) {
-#pragma unroll 1
-        for (int i = 1; i < 64; i <<= 1) add(__shfl_xor(m, i), __shfl_xor(s, i), scale);
+        const float top = wave_all(m, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+        s = wave_all(s * factor(m, top, scale), 0.f, [](float a, float b) { return a + b; });
+        m = top;
     }
     __device__ __forceinline__ float log(float temperature, float scale) const {
         if (s != s || m == -INFINITY || m == INFINITY) return s != s ? s : m;
@@ -154,7 +172,7 @@ struct PartSum {
 // Workgroup (x, y): part x (tiles_per_part tiles) of row y.  With one part a row it writes the answer, otherwise the part's
 // candidates, 0 in the slots that are left, and its exponential sum.
 template <bool BF16, bool RULES>
-__global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const char *__restrict__ X, int64_t row_bytes, int64_t rows, uint32_t cols, int k,
+__global__ __launch_bounds__(TILE_THREADS, RULES ? 4 : 6) void select_kernel(const char *__restrict__ X, int64_t row_bytes, int64_t first_row, uint32_t cols, int k,
                                                                  uint32_t tiles_per_part, float temperature, float scale, RuleArgs rules,
                                                                  Cand *__restrict__ part_cand, PartSum *__restrict__ part_sum,
                                                                  int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
@@ -168,130 +186,128 @@ __global__ __launch_bounds__(TILE_THREADS, 4) void select_kernel(const char *__r
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, parts = gridDim.x;
     const uint32_t begin = blockIdx.x * tiles_per_part * TILE;
     const uint32_t end = min(cols, (blockIdx.x + 1) * tiles_per_part * TILE);  // items of the part
-    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-        const char *scores_row = X + row * row_bytes;
-        Row in;
-        if (begin < end) in.load(scores_row, begin, cols, tid);
-        RowRules<Row> mine;
-        if constexpr (RULES) mine.begin(rules, row, words, tid);
-        ExpSum sum;
-        float bar = -INFINITY;
-        int have = 0, turn = 0;
-        const int most = parts > 1 ? PART_SLOTS : TILE_THREADS;  // candidates at the end
-        if (tid < 3) added[tid] = 0;
-        __syncthreads();
-        for (uint32_t first = begin; first < end; first += TILE) {
-            float x[PIECES][PER];
-            in.floats(x);
-            const bool last = first + TILE >= end;
-            if (!last) in.load(scores_row, first + TILE, cols, tid);
-            if constexpr (RULES) mine.apply(rules, first, cols, tid, x);
-            if (first + TILE > cols) {
-                const uint32_t left = cols - first;
+    const int64_t row = first_row + blockIdx.y;
+    const char *scores_row = X + row * row_bytes;
+    Row in;
+    if (begin < end) in.load(scores_row, begin, cols, tid);
+    RowRules<Row> mine;
+    if constexpr (RULES) mine.begin(rules, row, words, tid);
+    ExpSum sum;
+    float bar = -INFINITY;
+    int have = 0, turn = 0;
+    const int most = parts > 1 ? PART_SLOTS : TILE_THREADS;  // candidates at the end
+    if (tid < 3) added[tid] = 0;
+    __syncthreads();
+    for (uint32_t first = begin; first < end; first += TILE) {
+        float x[PIECES][PER];
+        in.floats(x);
+        const bool last = first + TILE >= end;
+        if (!last) in.load(scores_row, first + TILE, cols, tid);
+        if constexpr (RULES) mine.apply(rules, first, cols, tid, x);
+        if (first + TILE > cols) {
+            const uint32_t left = cols - first;
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    if (Row::item(j, tid) + e >= left) x[j][e] = -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) top = fmaxf(top, x[j][e]);
+        const float m = fmaxf(sum.m, top);
+        float part[2] = {0.f, 0.f};
+        if (__any(!ExpSum::plain(m, scale) && m != -INFINITY)) {
+            const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                for (int e = 0; e < PER; ++e) part[0] += x[j][e] == from ? 1.f : __builtin_amdgcn_exp2f((x[j][e] - from) * scale);
+        } else {
+            const float c = m == -INFINITY ? 0.f : m * scale;
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                for (int e = 0; e < PER; ++e) part[e & 1] += __builtin_amdgcn_exp2f(fmaf(x[j][e], scale, -c));
+        }
+        sum.s = sum.s * ExpSum::factor(sum.m, m, scale) + (part[0] + part[1]);
+        sum.m = m;
+
+        if (first == begin) {
+            const uint32_t nth = wave_nth(ordered_bits(top), (k + WAVES - 1) / WAVES);
+            if (lane == 0) wave_bar[wave] = nth;
+            __syncthreads();
+            uint32_t least = wave_bar[0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) least = min(least, wave_bar[i]);
+            bar = bar_below(least);
+        }
+        // The scores above the bar into the buffer: all pieces at once, or, if they do not fit, one after the other.
+        for (int j0 = 0, j1 = PIECES; j0 < PIECES;) {
+            if (__any(top > bar)) {
+                int mine_above = 0;
+#pragma unroll
+                for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) mine_above += j >= j0 && j < j1 && x[j][e] > bar;
+                const int upto = wave_scan(mine_above, 0, [](int a, int b) { return a + b; });
+                int at = 0;
+                if (lane == 63) at = atomicAdd(&added[turn], upto);
+                at = have + __builtin_amdgcn_readlane(at, 63) + upto - mine_above;
 #pragma unroll
                 for (int j = 0; j < PIECES; ++j)
 #pragma unroll
                     for (int e = 0; e < PER; ++e)
-                        if (Row::item(j, tid) + e >= left) x[j][e] = -INFINITY;
+                        if (j >= j0 && j < j1 && x[j][e] > bar) {
+                            float v = x[j][e];
+                            uint32_t from = first;
+                            asm volatile("" : "+v"(v), "+s"(from));  // nothing is prepared for those that do not come here
+                            if (at < SELECT_CAP) buf.cand[at] = candidate(v, from + Row::item(j, tid) + e);
+                            ++at;
+                        }
             }
-            float top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < PIECES; ++j)
-#pragma unroll
-                for (int e = 0; e < PER; ++e) top = fmaxf(top, x[j][e]);
-            const float m = fmaxf(sum.m, top);
-            float part[2] = {0.f, 0.f};
-            if (__any(!ExpSum::plain(m, scale) && m != -INFINITY)) {
-                const float from = m == -INFINITY ? 0.f : m;
-#pragma unroll
-                for (int j = 0; j < PIECES; ++j)
-#pragma unroll
-                    for (int e = 0; e < PER; ++e) part[0] += x[j][e] == from ? 1.f : __builtin_amdgcn_exp2f((x[j][e] - from) * scale);
-            } else {
-                const float c = m == -INFINITY ? 0.f : m * scale;
-#pragma unroll
-                for (int j = 0; j < PIECES; ++j)
-#pragma unroll
-                    for (int e = 0; e < PER; ++e) part[e & 1] += __builtin_amdgcn_exp2f(fmaf(x[j][e], scale, -c));
+            __syncthreads();
+            int count = have + added[turn];
+            if (tid == 0) added[turn == 0 ? 2 : turn - 1] = 0;
+            turn = turn == 2 ? 0 : turn + 1;
+            if (count > SELECT_CAP) {
+                j1 = 1;
+                continue;
             }
-            sum.s = sum.s * ExpSum::factor(sum.m, m, scale) + (part[0] + part[1]);
-            sum.m = m;
-
-            if (first == begin) {
-                const uint32_t nth = wave_nth(ordered_bits(top), (k + WAVES - 1) / WAVES);
-                if (lane == 0) wave_bar[wave] = nth;
-                __syncthreads();
-                uint32_t least = wave_bar[0];
-#pragma unroll
-                for (int i = 1; i < WAVES; ++i) least = min(least, wave_bar[i]);
-                bar = bar_below(least);
+            j0 = j1;
+            j1 = j0 + 1;
+            if (count > (last && j0 == PIECES ? most : SELECT_KEEP)) {
+                bar = bar_at(buf.template cut_back<TILE_THREADS>(count, k, tid));
+                count = k;
             }
-            // The scores above the bar into the buffer: all pieces at once, or, if they do not fit, one after the other.
-            for (int j0 = 0, j1 = PIECES; j0 < PIECES;) {
-                if (__any(top > bar)) {
-                    int mine_above = 0;
-#pragma unroll
-                    for (int j = 0; j < PIECES; ++j)
-#pragma unroll
-                        for (int e = 0; e < PER; ++e) mine_above += j >= j0 && j < j1 && x[j][e] > bar;
-                    int upto = mine_above;
-#pragma unroll
-                    for (int m = 1; m < 64; m <<= 1) {
-                        const int o = __shfl_up(upto, m);
-                        if (lane >= m) upto += o;
-                    }
-                    int at = 0;
-                    if (lane == 63) at = atomicAdd(&added[turn], upto);
-                    at = have + __builtin_amdgcn_readlane(at, 63) + upto - mine_above;
-#pragma unroll
-                    for (int j = 0; j < PIECES; ++j)
-#pragma unroll
-                        for (int e = 0; e < PER; ++e)
-                            if (j >= j0 && j < j1 && x[j][e] > bar) {
-                                if (at < SELECT_CAP) buf.cand[at] = candidate(x[j][e], first + Row::item(j, tid) + e);
-                                ++at;
-                            }
-                }
-                __syncthreads();
-                int count = have + added[turn];
-                if (tid == 0) added[turn == 0 ? 2 : turn - 1] = 0;
-                turn = turn == 2 ? 0 : turn + 1;
-                if (count > SELECT_CAP) {
-                    j1 = 1;
-                    continue;
-                }
-                j0 = j1;
-                j1 = j0 + 1;
-                if (count > (last && j0 == PIECES ? most : SELECT_KEEP)) {
-                    bar = bar_at(buf.template cut_back<TILE_THREADS>(count, k, tid));
-                    count = k;
-                }
-                have = count;
-            }
+            have = count;
         }
-        sum.over_lanes(scale);
-        if (lane == 0) {
-            wave_m[wave] = sum.m;
-            wave_s[wave] = sum.s;
-        }
-        __syncthreads();
-        ExpSum all;
-#pragma unroll 1
-        for (int i = 0; i < WAVES; ++i) all.add(wave_m[i], wave_s[i], scale);
-        if (parts > 1) {
-            const int64_t w = row * parts + blockIdx.x;
-            if (tid < PART_SLOTS) part_cand[w * PART_SLOTS + tid] = tid < have ? buf.cand[tid] : 0;
-            if (wave == 0) {
-                uint32_t best = 0;
-                for (int i = lane; i < have; i += 64) best = max(best, (uint32_t)(buf.cand[i] >> 32));
-                for (int m = 1; m < 64; m <<= 1) best = max(best, (uint32_t)__shfl_xor((int)best, m));
-                if (lane == 0) part_sum[w] = PartSum{all.m, all.s, best, 0};
-            }
-        } else {
-            buf.write_row(have, k, row, ids, scores, tid);
-            if (tid == 0 && lse) lse[row] = all.log(temperature, scale);
-        }
-        __syncthreads();
+    }
+    sum.over_lanes(scale);
+    if (lane == 0) {
+        wave_m[wave] = sum.m;
+        wave_s[wave] = sum.s;
+    }
+    __syncthreads();
+    ExpSum all;
+    {
+        float top = wave_m[0], total = 0.f;
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) top = fmaxf(top, wave_m[i]);
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) total += wave_s[i] * ExpSum::factor(wave_m[i], top, scale);
+        all.m = top;
+        all.s = total;
+    }
+    if (parts > 1) {
+        const int64_t w = row * parts + blockIdx.x;
+        if (tid < PART_SLOTS) part_cand[w * PART_SLOTS + tid] = tid < have ? buf.cand[tid] : 0;
+        if (tid == 0) part_sum[w] = PartSum{all.m, all.s, have ? ordered_bits(all.m) : 0, 0};
+    } else {
+        buf.write_row(have, k, row, ids, scores, tid);
+        if (tid == 0 && lse) lse[row] = all.log(temperature, scale);
     }
 }
 
@@ -394,8 +410,9 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
                          float *scores, float *lse, hipStream_t s) {
     const RuleArgs a = rule_args(rules);
     const int64_t tiles = (X->cols + TILE - 1) / TILE;
-    // parts of a row: as many workgroups as the card holds at a time, four per compute unit
-    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(tiles, ((int64_t)ctx->num_cu * 4 + X->rows - 1) / X->rows));
+    const bool bf = X->dtype == ALS_BF16, any = a.history.indptr || a.entries.indptr || a.bias || a.allowed;
+    // parts of a row: as many workgroups as the card holds at a time, four or six per compute unit
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(tiles, ((int64_t)ctx->num_cu * (any ? 4 : 6) + X->rows - 1) / X->rows));
     const int64_t per = std::max<int64_t>(1, (tiles + parts - 1) / parts);
     parts = std::max<int64_t>(1, (tiles + per - 1) / per);
     const float scale = 1.44269504f / temperature;
@@ -408,13 +425,12 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
         cand = (Cand *)ctx->select_partials.p;
         sums = (PartSum *)((char *)ctx->select_partials.p + cand_bytes);
     }
-    const dim3 grid((unsigned)parts, (unsigned)std::min<int64_t>(X->rows, 65535)), block(TILE_THREADS);
     auto go = [&](auto bf, auto with_rules) {
-        hipLaunchKernelGGL((select_kernel<bf(), with_rules()>), grid, block, rule_bytes(a), s, (const char *)X->data,
-                           X->ld * (bf() ? 2 : 4), X->rows, (uint32_t)X->cols, k, (uint32_t)per, temperature, scale, a, cand, sums, ids,
+        for (int64_t row = 0; row < X->rows; row += 65535)  // a grid's second dimension
+            hipLaunchKernelGGL((select_kernel<bf(), with_rules()>), dim3((unsigned)parts, (unsigned)std::min<int64_t>(X->rows - row, 65535)),
+                           dim3(TILE_THREADS), rule_bytes(a), s, (const char *)X->data, X->ld * (bf() ? 2 : 4), row, (uint32_t)X->cols, k, (uint32_t)per, temperature, scale, a, cand, sums, ids,
                            scores, lse);
     };
-    const bool bf = X->dtype == ALS_BF16, any = a.history.indptr || a.entries.indptr || a.bias || a.allowed;
     if (bf && any) go(std::true_type{}, std::true_type{});
     else if (bf) go(std::true_type{}, std::false_type{});
     else if (any) go(std::false_type{}, std::true_type{});
