@@ -55,7 +55,7 @@ class c_als_matrix(ctypes.Structure):
 
 
 class c_als_rules(ctypes.Structure):
-    _fields_ = [("history", ctypes.POINTER(c_als_csr)), ("entries", ctypes.POINTER(c_als_csr)), ("bias", ctypes.c_void_p),
+    _fields_ = [("history", ctypes.c_void_p), ("entries", ctypes.c_void_p), ("bias", ctypes.c_void_p),  # the lists: to c_als_csr
                 ("allowed", ctypes.c_void_p), ("allowed_ld", ctypes.c_int64), ("penalties", ctypes.c_void_p),
                 ("repetition", ctypes.c_float), ("presence", ctypes.c_float), ("frequency", ctypes.c_float)]
 
@@ -127,16 +127,16 @@ class Csr:
         return int(self.indices.numel())
 
     def c(self) -> c_als_csr:
-        assert self.indptr.dtype == torch.int64 and self.indices.dtype == torch.int32
-        assert self.indptr.is_contiguous() and self.indices.is_contiguous()
-        assert self.indptr.numel() == self.rows + 1
-        vals = None
-        if self.values is not None:
-            assert self.values.dtype == torch.float32 and self.values.is_contiguous()
-            assert self.values.numel() == self.indices.numel()
-            vals = self.values.data_ptr()
-        return c_als_csr(self.rows, self.cols, self.nnz, self.indptr.data_ptr(),
-                         self.indices.data_ptr() if self.nnz else None, vals)
+        indptr, indices, values = self.indptr, self.indices, self.values
+        nnz, vals = indices.numel(), None
+        assert indptr.dtype is torch.int64 and indices.dtype is torch.int32
+        assert indptr.is_contiguous() and indices.is_contiguous()
+        assert indptr.numel() == self.rows + 1
+        if values is not None:
+            assert values.dtype is torch.float32 and values.is_contiguous()
+            assert values.numel() == nnz
+            vals = values.data_ptr()
+        return c_als_csr(self.rows, self.cols, nnz, indptr.data_ptr(), indices.data_ptr() if nnz else None, vals)
 
 
 def _table(t: torch.Tensor) -> c_als_table:
@@ -152,8 +152,9 @@ def _table(t: torch.Tensor) -> c_als_table:
     return c_als_table(t.data_ptr() if t.numel() else None, t.shape[0], t.shape[1], ld, dt)
 
 
-def _stream() -> ctypes.c_void_p:
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+def _stream() -> int:
+    """Handle of torch's current stream on the current device."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 class Context:
@@ -290,42 +291,54 @@ class Rules:
     allowed: Optional[torch.Tensor] = None
 
     def c(self, rows: int, cols: int) -> c_als_rules:
-        out = c_als_rules(repetition=self.repetition, presence=self.presence, frequency=self.frequency)
+        out = c_als_rules()
+        out.repetition, out.presence, out.frequency = self.repetition, self.presence, self.frequency
+        out.lists = lists = []  # keeps what the structure points to
         if self.history is not None:
-            out.history = ctypes.pointer(self.history.c())
+            lists.append(self.history.c())
+            out.history = ctypes.addressof(lists[-1])
         if self.entries is not None:
-            out.entries = ctypes.pointer(self.entries.c())
-        if self.bias is not None:
-            if self.bias.dtype != torch.float32 or not self.bias.is_contiguous() or self.bias.shape != (cols,):
+            lists.append(self.entries.c())
+            out.entries = ctypes.addressof(lists[-1])
+        bias, penalties, allowed = self.bias, self.penalties, self.allowed
+        if bias is not None:
+            if bias.dtype is not torch.float32 or bias.dim() != 1 or bias.numel() != cols or not bias.is_contiguous():
                 raise ValueError("bias must be contiguous float32 [cols]")
-            out.bias = self.bias.data_ptr()
-        if self.penalties is not None:
-            if self.penalties.dtype != torch.float32 or not self.penalties.is_contiguous() or self.penalties.shape != (rows, 3):
+            out.bias = bias.data_ptr()
+        if penalties is not None:
+            if penalties.dtype is not torch.float32 or penalties.shape != (rows, 3) or not penalties.is_contiguous():
                 raise ValueError("penalties must be contiguous float32 [rows, 3]")
-            out.penalties = self.penalties.data_ptr()
-        if self.allowed is not None:
-            a = self.allowed
-            if a.dtype != torch.int32 or a.dim() != 2 or a.shape[0] not in (1, rows) or a.shape[1] < (cols + 31) // 32:
+            out.penalties = penalties.data_ptr()
+        if allowed is not None:
+            if allowed.dtype is not torch.int32 or allowed.dim() != 2:
                 raise ValueError("allowed must be int32 [rows or 1, at least (cols + 31) // 32]")
-            if a.shape[1] > 1 and a.stride(1) != 1:
+            sets, words = allowed.shape
+            if (sets != rows and sets != 1) or words < (cols + 31) // 32:
+                raise ValueError("allowed must be int32 [rows or 1, at least (cols + 31) // 32]")
+            step, unit = allowed.stride()
+            if words > 1 and unit != 1:
                 raise ValueError("allowed must have unit column stride")
-            out.allowed = a.data_ptr() or None
+            out.allowed = allowed.data_ptr() or None
             # one set for all rows: no step from row to row (an expanded tensor has none by itself)
-            out.allowed_ld = 0 if a.shape[0] == 1 else a.stride(0)
+            out.allowed_ld = 0 if sets == 1 else step
         return out
 
 
 def _matrix(t: torch.Tensor) -> c_als_matrix:
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dim() != 2:
         raise ValueError("scores must be 2-D with unit column stride")
-    if t.dtype == torch.float32:
+    rows, cols = t.shape
+    ld, unit = t.stride()
+    if cols > 1 and unit != 1:
+        raise ValueError("scores must be 2-D with unit column stride")
+    dtype = t.dtype
+    if dtype is torch.float32:
         dt = ALS_F32
-    elif t.dtype == torch.bfloat16:
+    elif dtype is torch.bfloat16:
         dt = ALS_BF16
     else:
         raise TypeError("scores must be float32 or bfloat16")
-    rows, cols = t.shape
-    return c_als_matrix(t.data_ptr() or None, rows, cols, t.stride(0) if rows > 1 else max(t.stride(0), cols), dt)
+    return c_als_matrix(t.data_ptr() or None, rows, cols, ld if rows > 1 else max(ld, cols), dt)
 
 
 def als_quantize(ctx: Context, X: torch.Tensor, group: int = 32, out: Optional[QTable] = None) -> QTable:
