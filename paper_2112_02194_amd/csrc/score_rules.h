@@ -8,6 +8,8 @@
 //   long lists   the workgroup walks the list together, once per tile
 #pragma once
 
+#include <algorithm>
+
 #include "als_internal.h"
 
 namespace als {
@@ -107,7 +109,8 @@ template <bool BF16> struct TileRow {
 // One of a row's lists over the tiles that a workgroup works on.
 template <class Row, bool PLACES> struct TileList {
     const int32_t *ids;
-    int64_t begins = 0, count = 0;  // the row's part of the list; none without a list
+    int64_t begins = 0;  // the row's part of the list; none without a list
+    int count = 0;
     int32_t id[LIST_REGS];          // short lists: entry 64 r + lane, -1 beyond
     uint32_t *words;                // TILE words in LDS
 
@@ -121,13 +124,13 @@ template <class Row, bool PLACES> struct TileList {
             if (e > l.nnz) e = l.nnz;
             if (e > b) {
                 begins = b;
-                count = e - b;
+                count = (int)std::min<int64_t>(e - b, INT32_MAX - 8 * TILE_THREADS);
             }
         }
         ids = l.indices + begins;
         if (count == 0 || !in_regs()) return;
 #pragma unroll
-        for (int r = 0; r < LIST_REGS; ++r) id[r] = 64 * r + (tid & 63) < (int)count ? ids[64 * r + (tid & 63)] : -1;
+        for (int r = 0; r < LIST_REGS; ++r) id[r] = 64 * r + (tid & 63) < count ? ids[64 * r + (tid & 63)] : -1;
         // the words of the wavefront's own elements
 #pragma unroll
         for (int j = 0; j < Row::PIECES; ++j)
@@ -141,7 +144,7 @@ template <class Row, bool PLACES> struct TileList {
             bool any = false;
 #pragma unroll
             for (int r = 0; r < LIST_REGS; ++r) {
-                if (64 * r >= (int)count) break;
+                if (64 * r >= count) break;
                 const uint32_t at = (uint32_t)id[r] - first;
                 const bool mine = at < TILE && Row::owner((int)at) == tid >> 6;
                 if (__any(mine)) {
@@ -157,11 +160,18 @@ template <class Row, bool PLACES> struct TileList {
         __syncthreads();  // the last tile's words have been read
         for (int i = tid * 4; i < TILE; i += TILE_THREADS * 4) *(uint4 *)(words + i) = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        for (int64_t i = tid; i < count; i += TILE_THREADS) {
-            const uint32_t at = (uint32_t)ids[i] - first;
-            if (at < TILE) {
-                if constexpr (PLACES) atomicMax(words + at, (uint32_t)i + 1u);
-                else atomicAdd(words + at, 1u);
+#pragma unroll 1
+        for (int i0 = tid; i0 < count; i0 += 8 * TILE_THREADS) {  // eight loads under way
+            uint32_t at[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) at[u] = (uint32_t)ids[min(i0 + u * TILE_THREADS, count - 1)] - first;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = i0 + u * TILE_THREADS;
+                if (at[u] < TILE && i < count) {
+                    if constexpr (PLACES) atomicMax(words + at[u], (uint32_t)i + 1u);
+                    else atomicAdd(words + at[u], 1u);
+                }
             }
         }
         __syncthreads();
@@ -172,7 +182,7 @@ template <class Row, bool PLACES> struct TileList {
         if (!in_regs()) return;
 #pragma unroll
         for (int r = 0; r < LIST_REGS; ++r) {
-            if (64 * r >= (int)count) break;
+            if (64 * r >= count) break;
             const uint32_t at = (uint32_t)id[r] - first;
             if (at < TILE && Row::owner((int)at) == tid >> 6) words[at] = 0;
         }

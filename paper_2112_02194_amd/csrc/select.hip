@@ -9,8 +9,8 @@
 //                smallest of the four wavefronts' ceil(k / 4)-th best lanes, later the k-th best of the buffer, found whenever
 //                that is full enough and then cut back to k.  Items come in ascending order, so a later score that equals the
 //                bar's loses against the k that are there.  A tile with more candidates than there is room for (an ascending
-//                row) goes in a quarter or half at a time with the buffer cut back between: nothing overflows, whatever the
-//                order or the number of equal scores.
+//                row) goes in a quarter at a time with the buffer cut back between: nothing overflows, whatever the order or
+//                the number of equal scores.
 // merge kernel   one workgroup per row: the parts' candidates, and their sums in a fixed order.
 #include <algorithm>
 #include <cmath>
@@ -20,11 +20,10 @@
 namespace als {
 
 typedef unsigned long long Cand;
-constexpr int SELECT_KEEP = 1024;  // the buffer is cut back to k when it holds more than this after a tile
-constexpr int SELECT_CAP = 3072;   // room: what is kept and the largest piece of a tile, 2048
-constexpr int PART_SLOTS = 128;    // candidates that a part hands on at most
-constexpr int MERGE_THREADS = 1024;
-static_assert(SELECT_KEEP + TILE_THREADS * 8 <= SELECT_CAP && ALS_TOPK_MAX_K <= 64 && 4 * ALS_TOPK_MAX_K <= TILE_THREADS, "");
+constexpr int SELECT_KEEP = 256;                      // the buffer is cut back to k when it holds more than this after a tile
+constexpr int SELECT_CAP = SELECT_KEEP + TILE / 4;    // room: what is kept and a quarter of a tile
+constexpr int PART_SLOTS = 128;                       // candidates that a part hands on at most
+static_assert(TILE_EPT == 16 && SELECT_KEEP <= TILE_THREADS && ALS_TOPK_MAX_K <= 64, "a quarter of a tile is four scores per thread");
 
 __device__ __forceinline__ uint32_t ordered_bits(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);  // -0 becomes 0: equal scores
@@ -172,7 +171,7 @@ struct PartSum {
 // Workgroup (x, y): part x (tiles_per_part tiles) of row y.  With one part a row it writes the answer, otherwise the part's
 // candidates, 0 in the slots that are left, and its exponential sum.
 template <bool BF16, bool RULES>
-__global__ __launch_bounds__(TILE_THREADS, RULES ? 4 : 6) void select_kernel(const char *__restrict__ X, int64_t row_bytes, int64_t first_row, uint32_t cols, int k,
+__global__ __launch_bounds__(TILE_THREADS, RULES ? (BF16 ? 5 : 4) : 6) void select_kernel(const char *__restrict__ X, int64_t row_bytes, int64_t first_row, uint32_t cols, int k,
                                                                  uint32_t tiles_per_part, float temperature, float scale, RuleArgs rules,
                                                                  Cand *__restrict__ part_cand, PartSum *__restrict__ part_sum,
                                                                  int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
@@ -244,43 +243,41 @@ __global__ __launch_bounds__(TILE_THREADS, RULES ? 4 : 6) void select_kernel(con
             for (int i = 1; i < WAVES; ++i) least = min(least, wave_bar[i]);
             bar = bar_below(least);
         }
-        // The scores above the bar into the buffer: all pieces at once, or, if they do not fit, one after the other.
-        for (int j0 = 0, j1 = PIECES; j0 < PIECES;) {
+        // The scores above the bar into the buffer: all at once, or, if they do not fit, a quarter of the tile after the other.
+        for (int q0 = 0, q1 = 4; q0 < 4;) {
             if (__any(top > bar)) {
                 int mine_above = 0;
 #pragma unroll
-                for (int j = 0; j < PIECES; ++j)
-#pragma unroll
-                    for (int e = 0; e < PER; ++e) mine_above += j >= j0 && j < j1 && x[j][e] > bar;
+                for (int i = 0; i < TILE_EPT; ++i) mine_above += i / 4 >= q0 && i / 4 < q1 && x[i / PER][i % PER] > bar;
                 const int upto = wave_scan(mine_above, 0, [](int a, int b) { return a + b; });
                 int at = 0;
                 if (lane == 63) at = atomicAdd(&added[turn], upto);
                 at = have + __builtin_amdgcn_readlane(at, 63) + upto - mine_above;
 #pragma unroll
-                for (int j = 0; j < PIECES; ++j)
-#pragma unroll
-                    for (int e = 0; e < PER; ++e)
-                        if (j >= j0 && j < j1 && x[j][e] > bar) {
-                            float v = x[j][e];
-                            uint32_t from = first;
-                            asm volatile("" : "+v"(v), "+s"(from));  // nothing is prepared for those that do not come here
-                            if (at < SELECT_CAP) buf.cand[at] = candidate(v, from + Row::item(j, tid) + e);
-                            ++at;
-                        }
+                for (int i = 0; i < TILE_EPT; ++i)
+                    if (i / 4 >= q0 && i / 4 < q1 && x[i / PER][i % PER] > bar) {
+                        float v = x[i / PER][i % PER];
+                        uint32_t from = first;
+                        asm volatile("" : "+v"(v), "+s"(from));  // nothing is prepared for those that do not come here
+                        if (at < SELECT_CAP) buf.cand[at] = candidate(v, from + Row::item(i / PER, tid) + i % PER);
+                        ++at;
+                    }
             }
             __syncthreads();
-            int count = have + added[turn];
+            int count = have + __builtin_amdgcn_readfirstlane(added[turn]);
             if (tid == 0) added[turn == 0 ? 2 : turn - 1] = 0;
             turn = turn == 2 ? 0 : turn + 1;
             if (count > SELECT_CAP) {
-                j1 = 1;
+                q1 = 1;
                 continue;
             }
-            j0 = j1;
-            j1 = j0 + 1;
-            if (count > (last && j0 == PIECES ? most : SELECT_KEEP)) {
-                bar = bar_at(buf.template cut_back<TILE_THREADS>(count, k, tid));
+            q0 = q1;
+            q1 = q0 + 1;
+            if (count > (last && q0 == 4 ? most : SELECT_KEEP)) {
+                const Cand nth = buf.template cut_back<TILE_THREADS>(count, k, tid);
                 count = k;
+                // the tile's other quarters may hold an equal score with a smaller id, later tiles may not
+                bar = q0 == 4 ? bar_at(nth) : bar_below((uint32_t)(nth >> 32));
             }
             have = count;
         }
@@ -313,14 +310,17 @@ __global__ __launch_bounds__(TILE_THREADS, RULES ? 4 : 6) void select_kernel(con
 
 // The parts of a row together, one workgroup per row.  A score that at least k candidates reach rules almost all of them out
 // unread where there are many parts: the k-th best of the parts' best.  Where there are few they are all read once.
-constexpr int MERGE_FEW = 64;  // parts; they give a thread MERGE_FEW * PART_SLOTS / MERGE_THREADS = 8 slots
+constexpr int MERGE_SLOTS = 8;  // per thread, where all are read
+template <int MERGE_THREADS> constexpr int merge_few() { return MERGE_SLOTS * MERGE_THREADS / PART_SLOTS; }  // parts of which all are read
+template <int MERGE_THREADS>
 __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t rows, int k, int parts, float temperature, float scale, const Cand *__restrict__ part_cand,
                                                                      const PartSum *__restrict__ part_sum, int32_t *__restrict__ ids,
                                                                      float *__restrict__ scores, float *__restrict__ lse) {
-    constexpr int WAVES = MERGE_THREADS / 64, CAP = 2 * MERGE_THREADS, SLOTS = MERGE_FEW * PART_SLOTS / MERGE_THREADS;
+    constexpr int WAVES = MERGE_THREADS / 64, CAP = 2048, SLOTS = MERGE_SLOTS, LIST = 1024;
+    static_assert(2 * MERGE_THREADS <= CAP, "");
     __shared__ Buffer<CAP> buf;
     __shared__ uint32_t wave_bar[WAVES];
-    __shared__ int count;
+    __shared__ int count, listed, list[LIST];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const int total = parts * PART_SLOTS;
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
         };
         Cand bar;
         ExpSum all;
-        if (parts <= MERGE_FEW) {
+        if (parts <= merge_few<MERGE_THREADS>()) {
             Cand c[SLOTS];
             uint32_t best = 0;
 #pragma unroll
@@ -353,31 +353,43 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) put(c[i], bar);
         } else {
-            // every wavefront for itself: the k-th best of the lanes' best, each of a few parts
+            // the bar from the parts' best, dealt out to the wavefronts evenly, then the parts that reach it
+            if (tid == 0) listed = 0;
             uint32_t best = 0;
-            for (int i = lane; i < parts; i += 64) {
-                const PartSum p = part[i];
-                best = max(best, p.best);
-                if (wave == 0) all.add(p.m, p.s, scale);
-            }
-            bar = max((Cand)wave_nth(best, k) << 32, (Cand)1);
+            for (int p = lane * WAVES + wave; p < parts; p += MERGE_THREADS) best = max(best, part[p].best);
+            const uint32_t nth = wave_nth(best, (k + WAVES - 1) / WAVES);
+            if (lane == 0) wave_bar[wave] = nth;
             __syncthreads();
-            int taken = 0;  // parts that reach the bar so far: the wavefronts take turns
-            for (int i0 = 0; i0 < parts; i0 += 64) {
-                unsigned long long who = __ballot(i0 + lane < parts && part[min(i0 + lane, parts - 1)].best >= (uint32_t)(bar >> 32));
-                while (who) {
-                    const int p = i0 + __ffsll((long long)who) - 1;
-                    who &= who - 1;
-                    if (taken++ % WAVES != wave) continue;
-                    const Cand c0 = cand[p * PART_SLOTS + lane], c1 = cand[p * PART_SLOTS + 64 + lane];
-                    put(c0, bar);
-                    put(c1, bar);
+            uint32_t least = wave_bar[0];
+            for (int i = 1; i < WAVES; ++i) least = min(least, wave_bar[i]);
+            bar = max((Cand)least << 32, (Cand)1);
+            for (int p = tid; p < parts; p += MERGE_THREADS) {
+                const PartSum v = part[p];
+                if (v.best >= least) {
+                    const int at = atomicAdd(&listed, 1);
+                    if (at < LIST) list[at] = p;
                 }
+            }
+            if (wave == 0)
+                for (int p = lane; p < parts; p += 64) all.add(part[p].m, part[p].s, scale);
+            __syncthreads();
+            const bool fits = listed <= LIST;
+            const int slots = (fits ? listed : parts) * PART_SLOTS;
+            for (int i0 = tid; i0 < slots; i0 += MERGE_SLOTS * MERGE_THREADS) {
+                Cand c[MERGE_SLOTS];
+#pragma unroll
+                for (int u = 0; u < MERGE_SLOTS; ++u) {
+                    const int i = min(i0 + u * MERGE_THREADS, slots - 1);
+                    c[u] = cand[(fits ? list[i / PART_SLOTS] : i / PART_SLOTS) * PART_SLOTS + i % PART_SLOTS];
+                }
+#pragma unroll
+                for (int u = 0; u < MERGE_SLOTS; ++u)
+                    if (i0 + u * MERGE_THREADS < slots) put(c[u], bar);
             }
         }
         __syncthreads();
         int have = count;
-        if (have > CAP) {  // more than there is room for (equal scores): 1024 at a time
+        if (have > CAP) {  // more than there is room for (equal scores): a few at a time
             have = 0;
             for (int i0 = 0; i0 < total; i0 += MERGE_THREADS) {
                 __syncthreads();
@@ -386,15 +398,15 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
                 if (i0 + tid < total) put(cand[i0 + tid], bar);
                 __syncthreads();
                 have = count;
-                if (have > MERGE_THREADS) {
-                    bar = buf.cut_back<MERGE_THREADS>(have, k, tid);
+                if (have > CAP - MERGE_THREADS) {
+                    bar = buf.template cut_back<MERGE_THREADS>(have, k, tid);
                     have = k;
                 }
             }
         }
         __syncthreads();
         if (have > 256) {
-            buf.cut_back<MERGE_THREADS>(have, k, tid);
+            buf.template cut_back<MERGE_THREADS>(have, k, tid);
             have = k;
         }
         buf.write_row(have, k, row, ids, scores, tid);
@@ -411,10 +423,21 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
     const RuleArgs a = rule_args(rules);
     const int64_t tiles = (X->cols + TILE - 1) / TILE;
     const bool bf = X->dtype == ALS_BF16, any = a.history.indptr || a.entries.indptr || a.bias || a.allowed;
-    // parts of a row: as many workgroups as the card holds at a time, four or six per compute unit
-    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(tiles, ((int64_t)ctx->num_cu * (any ? 4 : 6) + X->rows - 1) / X->rows));
-    const int64_t per = std::max<int64_t>(1, (tiles + parts - 1) / parts);
-    parts = std::max<int64_t>(1, (tiles + per - 1) / per);
+    // Parts of a row.  The card holds `slots` workgroups at a time (registers for four to six per compute unit, LDS for a buffer
+    // and the lists' words); a row's parts are chosen so that the rounds of workgroups are full: with r rounds a workgroup
+    // walks ceil(tiles / parts) tiles, and beginning and ending a part costs about as much as four more.
+    const int64_t lds_bytes = (int64_t)rule_bytes(a) + (int64_t)sizeof(Buffer<SELECT_CAP>) + 256;
+    const int64_t slots = ctx->num_cu * std::min<int64_t>(any ? (bf ? 5 : 4) : 6, 160 * 1024 / lds_bytes);
+    int64_t per = tiles, least = INT64_MAX;
+    for (int64_t r = 1; r <= 8; ++r) {
+        const int64_t p = std::max<int64_t>(1, std::min<int64_t>(tiles, slots * r / X->rows)), each = std::max<int64_t>(1, (tiles + p - 1) / p);
+        const int64_t cost = (X->rows * ((tiles + each - 1) / each) + slots - 1) / slots * (each + 4);
+        if (cost < least) {
+            least = cost;
+            per = each;
+        }
+    }
+    const int64_t parts = std::max<int64_t>(1, (tiles + per - 1) / std::max<int64_t>(1, per));
     const float scale = 1.44269504f / temperature;
     Cand *cand = nullptr;
     PartSum *sums = nullptr;
@@ -435,9 +458,14 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
     else if (bf) go(std::true_type{}, std::false_type{});
     else if (any) go(std::false_type{}, std::true_type{});
     else go(std::false_type{}, std::false_type{});
-    if (parts > 1)
-        hipLaunchKernelGGL(select_merge_kernel, dim3((unsigned)std::min<int64_t>(X->rows, 1 << 22)), dim3(MERGE_THREADS), 0, s, X->rows, k,
-                           (int)parts, temperature, scale, (const Cand *)cand, (const PartSum *)sums, ids, scores, lse);
+    if (parts > 1) {
+        auto merge = [&](auto threads) {
+            hipLaunchKernelGGL((select_merge_kernel<threads()>), dim3((unsigned)std::min<int64_t>(X->rows, 1 << 20)), dim3(threads()), 0, s, X->rows, k,
+                               (int)parts, temperature, scale, (const Cand *)cand, (const PartSum *)sums, ids, scores, lse);
+        };
+        if (parts <= merge_few<256>()) merge(std::integral_constant<int, 256>{});
+        else merge(std::integral_constant<int, 1024>{});
+    }
     ALS_HIP(ctx, hipGetLastError());
     return ALS_OK;
 }
