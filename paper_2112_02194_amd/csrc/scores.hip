@@ -56,9 +56,9 @@ __global__ __launch_bounds__(256, 4) void scores_few_kernel(const void *__restri
 #pragma unroll
             for (int e = 0; e < 8; ++e) q[r][8 * p + e] = x[e];
         }
-    for (int64_t i0 = wave * (IPS * U); i0 < n; i0 += waves * (IPS * U)) {
-        uint32_t w[U][W];
-        float s[U][NG];
+    uint32_t next_w[U][W];
+    uint32_t next_s[U];
+    auto fetch = [&](int64_t i0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t item = std::min<int64_t>(i0 + u * IPS + lane / LPI, n - 1);
@@ -66,21 +66,29 @@ __global__ __launch_bounds__(256, 4) void scores_few_kernel(const void *__restri
             if constexpr (W == 4) {
                 const u32x4 t = *(const u32x4 *)at;
 #pragma unroll
-                for (int p = 0; p < 4; ++p) w[u][p] = t[p];
+                for (int p = 0; p < 4; ++p) next_w[u][p] = t[p];
             } else {
                 const u32x2 t = *(const u32x2 *)at;
 #pragma unroll
-                for (int p = 0; p < 2; ++p) w[u][p] = t[p];
+                for (int p = 0; p < 2; ++p) next_w[u][p] = t[p];
             }
             const uint16_t *sc = scales + item * (D / G) + chunk * CPL / G;
-            if constexpr (NG == 2) {
-                const uint32_t t = *(const uint32_t *)sc;
-                s[u][0] = __uint_as_float(t << 16);
-                s[u][1] = __uint_as_float(t & 0xffff0000u);
-            } else {
-                s[u][0] = bf16_to_f32(*sc);
-            }
+            next_s[u] = NG == 2 ? *(const uint32_t *)sc : *sc;
         }
+    };
+    int64_t i0 = wave * (IPS * U);
+    if (i0 < n) fetch(i0);
+    for (; i0 < n; i0 += waves * (IPS * U)) {
+        uint32_t w[U][W];
+        float s[U][NG];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int p = 0; p < W; ++p) w[u][p] = next_w[u][p];
+            s[u][0] = __uint_as_float(next_s[u] << 16);
+            if constexpr (NG == 2) s[u][1] = __uint_as_float(next_s[u] & 0xffff0000u);
+        }
+        if (i0 + waves * (IPS * U) < n) fetch(i0 + waves * (IPS * U));
         float sum[NQ][U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -424,13 +432,19 @@ static void scores_typed(const als_ctx *ctx, const als_table *Q, const als_qtabl
     // 786, 870 us.  Workgroups of one item stretch and all query groups at one time instead: 424, 898 us.
     const int64_t rounds = std::max<int64_t>(1, std::min<int64_t>(4, spans * qgroups / ((int64_t)ctx->num_cu * 16)));
     const int64_t stretch = std::max<int64_t>(1, std::min<int64_t>(16, spans / (32 * rounds)));
-    const int64_t units = (spans + 4 * rounds * stretch - 1) / (4 * rounds * stretch) * stretch * qgroups;
     // a buffer's offsets have 32 bits: five rows must fit
     const bool near = S->ld < (int64_t)1 << 27, words = !BF_S || (S->ld % 2 == 0 && (uintptr_t)S->data % 4 == 0);
     const StoreAs as = !near ? StoreAs::GUARDED : words ? StoreAs::BUFFER : StoreAs::PLAIN;
-    hipLaunchKernelGGL((scores_tile_kernel<BF_Q, BF_S, D, G>), dim3((unsigned)((units + 7) / 8 * 8)), dim3(256), 0, s, Q->data, Q->ld, nq,
-                       (const uint32_t *)T->codes, (const uint16_t *)T->scales, n, S->data, S->ld, as, (unsigned)qgroups,
-                       (unsigned)stretch, (unsigned)rounds, (unsigned)units);
+    // units of work, as many groups of queries at a time as a grid holds
+    const int64_t per_group = (spans + 4 * rounds * stretch - 1) / (4 * rounds * stretch) * stretch;
+    const int64_t batch = std::max<int64_t>(1, ((int64_t)1 << 22) / per_group);
+    for (int64_t g = 0; g < qgroups; g += batch) {
+        const int64_t q0 = g * 32, groups = std::min(batch, qgroups - g), units = per_group * groups;
+        hipLaunchKernelGGL((scores_tile_kernel<BF_Q, BF_S, D, G>), dim3((unsigned)((units + 7) / 8 * 8)), dim3(256), 0, s,
+                           (const char *)Q->data + q0 * Q->ld * (BF_Q ? 2 : 4), Q->ld, std::min(nq - q0, groups * 32),
+                           (const uint32_t *)T->codes, (const uint16_t *)T->scales, n, (char *)S->data + q0 * S->ld * (BF_S ? 2 : 4), S->ld, as,
+                           (unsigned)groups, (unsigned)stretch, (unsigned)rounds, (unsigned)units);
+    }
 }
 
 template <bool BF_Q, bool BF_S>

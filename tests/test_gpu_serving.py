@@ -373,6 +373,47 @@ def test_offsets_beyond_32_bits(ctx, gpu_device):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("nq,n", [(40, 130), (1, 70), (2, 300)])
+@pytest.mark.parametrize("ds", [torch.float32, torch.bfloat16])
+def test_scores_into_rows_far_apart(ctx, gpu_device, nq, n, ds):
+    """Rows of scores beyond 2^32 bytes and beyond what a buffer's offsets reach."""
+    ld = (1 << 27) + 1 if ds == torch.bfloat16 else (1 << 27) + 2
+    say(f"als_scores nq={nq} n={n} ld={ld} {ds}")
+    T = als.als_quantize(ctx, table(n, 64, torch.float32, seed=4, special=False).to(gpu_device), 32)
+    Q = init_table(nq, 64, seed=3, stream=2).to(gpu_device)
+    want = als.als_scores(ctx, Q, T, dtype=ds)
+    big = torch.empty(nq * ld, dtype=ds, device=gpu_device)
+    S = big.as_strided((nq, n), (ld, 1))
+    big.as_strided((nq, n + 3), (ld, 1)).fill_(5.0)
+    als.als_scores(ctx, Q, T, out=S)
+    torch.cuda.synchronize()
+    assert torch.equal(S, want) and torch.all(big.as_strided((nq, 3), (ld, 1), n) == 5.0)
+    del S, big
+    torch.cuda.empty_cache()
+
+
+def test_scores_of_many_queries_and_few_items(ctx, gpu_device):
+    say("als_scores: 300000 queries x 3 items")
+    T = als.als_quantize(ctx, table(3, 16, torch.float32, seed=4, special=False).to(gpu_device), 16)
+    Q = init_table(300_000, 16, seed=3, stream=2)
+    S = als.als_scores(ctx, Q.to(gpu_device), T)
+    torch.cuda.synchronize()
+    V = f64(als.als_dequantize(ctx, T))
+    want, bound = f64(Q) @ V.T, (2 * 16 + 16) * 2.0 ** -24 * (np.abs(f64(Q)) @ np.abs(V).T) + 1e-37
+    assert np.all(np.abs(f64(S) - want) <= bound)
+
+
+def test_rules_on_many_rows(ctx, gpu_device):
+    say("als_select, als_adjust: 70000 rows, more than a grid's second dimension")
+    gen = torch.Generator().manual_seed(2)
+    X = (torch.randn((70_000, 40), generator=gen) * 8).round() / 8
+    got = als.als_select(ctx, X.to(gpu_device), 5)
+    Y = als.als_adjust(ctx, X.to(gpu_device), als.Rules(bias=torch.arange(40.0, device=gpu_device)))
+    torch.cuda.synchronize()
+    check_selected(got, f64(X), 5, 1.0, 40)
+    assert np.array_equal(f64(Y), f64(X) + np.arange(40.0))
+
+
 def serve(ctx, Q, T, rules, k):
     S = als.als_scores(ctx, Q, T)
     als.als_adjust(ctx, S, als.Rules(bias=rules.bias))
