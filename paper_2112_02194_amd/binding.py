@@ -140,16 +140,20 @@ class Csr:
 
 
 def _table(t: torch.Tensor) -> c_als_table:
-    if t.dim() != 2 or t.stride(1) != 1:
+    if t.dim() != 2:
         raise ValueError("table must be 2-D with unit column stride")
-    if t.dtype == torch.float32:
+    rows, d = t.shape
+    ld, unit = t.stride()
+    if unit != 1:
+        raise ValueError("table must be 2-D with unit column stride")
+    dtype = t.dtype
+    if dtype is torch.float32:
         dt = ALS_F32
-    elif t.dtype == torch.bfloat16:
+    elif dtype is torch.bfloat16:
         dt = ALS_BF16
     else:
         raise TypeError("table dtype must be float32 or bfloat16")
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    return c_als_table(t.data_ptr() if t.numel() else None, t.shape[0], t.shape[1], ld, dt)
+    return c_als_table(t.data_ptr() if rows and d else None, rows, d, ld if rows > 1 else max(ld, d), dt)
 
 
 def _stream() -> int:
@@ -262,14 +266,17 @@ class QTable:
 
     def c(self) -> c_als_qtable:
         codes, scales = self.codes, self.scales
-        if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16:
+        if codes.dtype is not torch.uint8 or scales.dtype is not torch.bfloat16:
             raise TypeError("codes must be uint8 and scales bfloat16")
         if codes.dim() != 2 or scales.dim() != 2 or not codes.is_contiguous() or not scales.is_contiguous():
             raise ValueError("codes and scales must be 2-D and contiguous")
         rows, half = codes.shape
-        if scales.shape[0] != rows:
+        scale_rows, groups = scales.shape
+        if scale_rows != rows:
             raise ValueError("codes and scales differ in rows")
-        return c_als_qtable(codes.data_ptr() or None, scales.data_ptr() or None, rows, 2 * half, self.group)
+        if groups < 1 or 2 * half % groups:
+            raise ValueError("a row must be a whole number of groups")
+        return c_als_qtable(codes.data_ptr() or None, scales.data_ptr() or None, rows, 2 * half, 2 * half // groups)
 
 
 @dataclass
@@ -345,10 +352,11 @@ def als_quantize(ctx: Context, X: torch.Tensor, group: int = 32, out: Optional[Q
     """X in 4 bits an entry, one bf16 scale per ``group`` entries of a row (at most d, so 16 for d = 16)."""
     tx = _table(X)
     if out is None:
-        if group not in (16, 32, 64, 128) or group > X.shape[1]:
+        rows, d = X.shape
+        if group not in (16, 32, 64, 128) or group > d:
             raise ValueError("group must be 16, 32, 64 or 128 and at most d")
-        out = QTable(torch.empty((X.shape[0], X.shape[1] // 2), dtype=torch.uint8, device=X.device),
-                     torch.empty((X.shape[0], X.shape[1] // group), dtype=torch.bfloat16, device=X.device))
+        out = QTable(torch.empty((rows, d // 2), dtype=torch.uint8, device=X.device),
+                     torch.empty((rows, d // group), dtype=torch.bfloat16, device=X.device))
     ct = out.c()
     ctx._check(ctx.lib.als_quantize(ctx.handle, ctypes.byref(tx), ctypes.byref(ct), _stream()))
     return out

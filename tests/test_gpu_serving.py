@@ -462,6 +462,27 @@ def test_same_bits_every_time(ctx, gpu_device):
             assert torch.equal(a, b)
 
 
+def test_the_example_answers_from_4_bits(gpu_device):
+    say("examples/serve_4bit.py")
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_4bit.py")
+    spec = importlib.util.spec_from_file_location("serve_4bit", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    r = module.main(nodes=12000, epochs=2)
+    say(f"  Recall@20 {r['recall'][0]:.4f} from fp32, {r['recall'][1]:.4f} from 4 bits")
+    assert r["bytes"][1] * 7 < r["bytes"][0]  # 4.5 bits an entry with groups of 32
+    # steps of a seventh of a group's largest entry: an error of about a tenth of an entry, which averages out over a row's 64
+    assert r["recall"][1] > 0.8 * r["recall"][0] > 0.04
+    ids, prob = r["ids"], r["probability"]
+    ptr, idx = r["given"]
+    for q in range(0, ids.shape[0], 7):
+        assert not set(ids[q].tolist()) & set(idx[ptr[q]:ptr[q + 1]].tolist())
+    assert torch.all(prob >= 0) and torch.all(prob.sum(1) <= 1 + 1e-5) and torch.all(prob[:, :-1] >= prob[:, 1:] - 1e-12)
+
+
 def test_refusals(ctx, gpu_device):
     say("what the operators refuse")
     dev = gpu_device
