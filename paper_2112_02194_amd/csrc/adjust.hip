@@ -6,15 +6,18 @@
 
 namespace als {
 
+constexpr int ADJUST_THREADS = 256, ADJUST_TILE = ADJUST_THREADS * TILE_EPT;
+
 // Workgroup (x, y) works on tile y of row x: the rows of one tile share its biases and a shared set of allowed items.
 template <bool BF_IN, bool BF_OUT>
-__global__ __launch_bounds__(TILE_THREADS) void adjust_kernel(const void *X, int64_t ldx, void *Y, int64_t ldy, int64_t rows,
+__global__ __launch_bounds__(ADJUST_THREADS) void adjust_kernel(const void *X, int64_t ldx, void *Y, int64_t ldy, int64_t rows,
                                                               uint32_t cols, RuleArgs rules) {
-    typedef TileRow<BF_IN> Row;
+    typedef TileRow<BF_IN, ADJUST_THREADS> Row;
+    constexpr uint32_t TILE = Row::TILE;
     extern __shared__ __align__(16) uint32_t words[];
     const int tid = threadIdx.x;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
-    for (uint32_t first = blockIdx.y * TILE; first < cols; first += gridDim.y * TILE) {
+        for (uint32_t first = blockIdx.y * TILE; first < cols; first += gridDim.y * TILE) {
         Row in;
         in.load((const char *)X + row * ldx * (BF_IN ? 2 : 4), first, cols, tid);
         RowRules<Row> mine;
@@ -52,11 +55,11 @@ __global__ __launch_bounds__(TILE_THREADS) void adjust_kernel(const void *X, int
 
 als_status launch_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rules, const als_matrix *Y, hipStream_t s) {
     const RuleArgs a = rule_args(rules);
-    const dim3 grid((unsigned)std::min<int64_t>(X->rows, 1 << 16), (unsigned)std::min<int64_t>((X->cols + TILE - 1) / TILE, 1 << 15));
-    const dim3 block(TILE_THREADS);
+    const dim3 grid((unsigned)std::min<int64_t>(X->rows, 1 << 16), (unsigned)std::min<int64_t>((X->cols + ADJUST_TILE - 1) / ADJUST_TILE, 1 << 15));
+    const dim3 block(ADJUST_THREADS);
     const bool bi = X->dtype == ALS_BF16, bo = Y->dtype == ALS_BF16;
     auto go = [&](auto in, auto out) {
-        hipLaunchKernelGGL((adjust_kernel<in(), out()>), grid, block, rule_bytes(a), s, X->data, X->ld, Y->data, Y->ld, X->rows,
+        hipLaunchKernelGGL((adjust_kernel<in(), out()>), grid, block, rule_bytes(a, ADJUST_TILE), s, X->data, X->ld, Y->data, Y->ld, X->rows,
                            (uint32_t)X->cols, a);
     };
     if (bi && bo) go(std::true_type{}, std::true_type{});

@@ -1,6 +1,6 @@
 // Rules on scores (als_rules) as als_adjust and als_select evaluate them, a tile of one row at a time.
 //
-// A workgroup of 256 threads works on TILE consecutive items of one row, a thread on pieces of 16 bytes of scores.  Lists
+// A workgroup works on a tile of consecutive items of one row, sixteen per thread, a thread on pieces of 16 bytes of scores.  Lists
 // (history, entries) hold a row's items in any order, so nothing says which of them lie in the tile.  A word per item in LDS counts how
 // often it occurs (history) or tells where it is stored last (entries); integer atomics, so the order does not matter.
 //   short lists (up to LIST_REGS per lane): every wavefront holds the row's whole list in registers and enters the items that
@@ -14,7 +14,7 @@
 
 namespace als {
 
-constexpr int TILE = 4096, TILE_THREADS = 256, TILE_EPT = TILE / TILE_THREADS;  // items per tile, threads, items per thread
+constexpr int TILE_EPT = 16;  // items of a tile per thread
 constexpr int LIST_REGS = 4;
 
 struct RowList {
@@ -50,8 +50,8 @@ inline RuleArgs rule_args(const als_rules *r) {
     a.frequency = r->frequency;
     return a;
 }
-// LDS bytes that the lists need
-inline size_t rule_bytes(const RuleArgs &a) { return ((a.history.indptr ? TILE : 0) + (a.entries.indptr ? TILE : 0)) * sizeof(uint32_t); }
+// LDS bytes that the lists need for a tile
+inline size_t rule_bytes(const RuleArgs &a, int tile) { return ((a.history.indptr ? tile : 0) + (a.entries.indptr ? tile : 0)) * sizeof(uint32_t); }
 
 // A value that all lanes read and no kernel of the call writes, through the scalar cache.
 template <class T> __device__ __forceinline__ T uniform_load(const T *p) {
@@ -59,13 +59,14 @@ template <class T> __device__ __forceinline__ T uniform_load(const T *p) {
 }
 
 // A thread's elements of a tile: PIECES times PER consecutive ones, 16 bytes.  Rows need not be aligned beyond their elements.
-template <bool BF16> struct TileRow {
+template <bool BF16, int NT> struct TileRow {
+    static constexpr int THREADS = NT, TILE = NT * TILE_EPT;
     static constexpr int PER = BF16 ? 8 : 4, PIECES = TILE_EPT / PER;
     typedef uint32_t Words __attribute__((ext_vector_type(4)));
     Words raw[PIECES];
-    static __device__ __forceinline__ int item(int j, int tid) { return (j * TILE_THREADS + tid) * PER; }  // relative to the tile
+    static __device__ __forceinline__ int item(int j, int tid) { return (j * NT + tid) * PER; }  // relative to the tile
     // wavefront that has item `at` of the tile
-    static __device__ __forceinline__ int owner(int at) { return (at / (64 * PER)) % (TILE_THREADS / 64); }
+    static __device__ __forceinline__ int owner(int at) { return (at / (64 * PER)) % (NT / 64); }
 
     // `row`: the row's scores; items from cols on are not read
     __device__ __forceinline__ void load(const char *row, uint32_t first, uint32_t cols, int tid) {
@@ -112,7 +113,7 @@ template <class Row, bool PLACES> struct TileList {
     int64_t begins = 0;  // the row's part of the list; none without a list
     int count = 0;
     int32_t id[LIST_REGS];          // short lists: entry 64 r + lane, -1 beyond
-    uint32_t *words;                // TILE words in LDS
+    uint32_t *words;                // a tile's words in LDS
 
     __device__ __forceinline__ bool in_regs() const { return count <= 64 * LIST_REGS; }
     __device__ __forceinline__ void begin(const RowList &l, int64_t row, uint32_t *lds, int tid) {
@@ -124,7 +125,7 @@ template <class Row, bool PLACES> struct TileList {
             if (e > l.nnz) e = l.nnz;
             if (e > b) {
                 begins = b;
-                count = (int)std::min<int64_t>(e - b, INT32_MAX - 8 * TILE_THREADS);
+                count = (int)std::min<int64_t>(e - b, INT32_MAX - 8 * Row::THREADS);
             }
         }
         ids = l.indices + begins;
@@ -146,7 +147,7 @@ template <class Row, bool PLACES> struct TileList {
             for (int r = 0; r < LIST_REGS; ++r) {
                 if (64 * r >= count) break;
                 const uint32_t at = (uint32_t)id[r] - first;
-                const bool mine = at < TILE && Row::owner((int)at) == tid >> 6;
+                const bool mine = at < Row::TILE && Row::owner((int)at) == tid >> 6;
                 if (__any(mine)) {
                     any = true;
                     if (mine) {
@@ -158,17 +159,17 @@ template <class Row, bool PLACES> struct TileList {
             return any;
         }
         __syncthreads();  // the last tile's words have been read
-        for (int i = tid * 4; i < TILE; i += TILE_THREADS * 4) *(uint4 *)(words + i) = make_uint4(0, 0, 0, 0);
+        for (int i = tid * 4; i < Row::TILE; i += Row::THREADS * 4) *(uint4 *)(words + i) = make_uint4(0, 0, 0, 0);
         __syncthreads();
 #pragma unroll 1
-        for (int i0 = tid; i0 < count; i0 += 8 * TILE_THREADS) {  // eight loads under way
+        for (int i0 = tid; i0 < count; i0 += 8 * Row::THREADS) {  // eight loads under way
             uint32_t at[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) at[u] = (uint32_t)ids[min(i0 + u * TILE_THREADS, count - 1)] - first;
+            for (int u = 0; u < 8; ++u) at[u] = (uint32_t)ids[min(i0 + u * Row::THREADS, count - 1)] - first;
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const int i = i0 + u * TILE_THREADS;
-                if (at[u] < TILE && i < count) {
+                const int i = i0 + u * Row::THREADS;
+                if (at[u] < Row::TILE && i < count) {
                     if constexpr (PLACES) atomicMax(words + at[u], (uint32_t)i + 1u);
                     else atomicAdd(words + at[u], 1u);
                 }
@@ -184,7 +185,7 @@ template <class Row, bool PLACES> struct TileList {
         for (int r = 0; r < LIST_REGS; ++r) {
             if (64 * r >= count) break;
             const uint32_t at = (uint32_t)id[r] - first;
-            if (at < TILE && Row::owner((int)at) == tid >> 6) words[at] = 0;
+            if (at < Row::TILE && Row::owner((int)at) == tid >> 6) words[at] = 0;
         }
     }
 };
@@ -197,7 +198,7 @@ template <class Row> struct RowRules {
     const uint32_t *allowed;
     __device__ __forceinline__ void begin(const RuleArgs &a, int64_t row, uint32_t *lds, int tid) {
         history.begin(a.history, row, lds, tid);
-        entries.begin(a.entries, row, lds + (a.history.indptr ? TILE : 0), tid);
+        entries.begin(a.entries, row, lds + (a.history.indptr ? Row::TILE : 0), tid);
         r = a.repetition; p = a.presence; f = a.frequency;
         if (a.penalties) {
             r = uniform_load(a.penalties + 3 * row);

@@ -5,11 +5,11 @@
 //
 // select kernel  a part of a row (several parts where there are few rows), a tile at a time, one read of the scores.  Every
 //                thread keeps the running maximum and sum of its elements' exponentials.  Scores above the bar are appended
-//                to a buffer in LDS.  The bar is a score that at least k of the part reach: on the first tile just below the
-//                smallest of the four wavefronts' ceil(k / 4)-th best lanes, later the k-th best of the buffer, found whenever
+//                to a buffer in LDS.  The bar is a score that at least k of the part reach: on the first tile just below what the
+//                wavefronts' best lanes reach (WaveRanks), later the k-th best of the buffer, found whenever
 //                that is full enough and then cut back to k.  Items come in ascending order, so a later score that equals the
 //                bar's loses against the k that are there.  A tile with more candidates than there is room for (an ascending
-//                row) goes in a quarter at a time with the buffer cut back between: nothing overflows, whatever the order or
+//                row) goes in a step at a time with the buffer cut back between: nothing overflows, whatever the order or
 //                the number of equal scores.
 // merge kernel   one workgroup per row: the parts' candidates, and their sums in a fixed order.
 #include <algorithm>
@@ -20,10 +20,11 @@
 namespace als {
 
 typedef unsigned long long Cand;
-constexpr int SELECT_KEEP = 256;                      // the buffer is cut back to k when it holds more than this after a tile
-constexpr int SELECT_CAP = SELECT_KEEP + TILE / 4;    // room: what is kept and a quarter of a tile
-constexpr int PART_SLOTS = 128;                       // candidates that a part hands on at most
-static_assert(TILE_EPT == 16 && SELECT_KEEP <= TILE_THREADS && ALS_TOPK_MAX_K <= 64, "a quarter of a tile is four scores per thread");
+constexpr int SELECT_KEEP = 256;  // the buffer is cut back to k when it holds more than this after a tile
+constexpr int PART_SLOTS = 128;   // candidates that a part hands on at most
+// A tile that does not fit goes in STEPS steps; the buffer has room for what is kept and one of them.
+template <int NT> constexpr int select_steps() { return NT == 1024 ? 8 : 4; }
+template <int NT> constexpr int select_room() { return SELECT_KEEP + NT * TILE_EPT / select_steps<NT>(); }
 
 __device__ __forceinline__ uint32_t ordered_bits(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);  // -0 becomes 0: equal scores
@@ -55,15 +56,19 @@ template <class T, class F> __device__ __forceinline__ T wave_all(T x, T none, F
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(x, none, f)), 63));
 }
 
-// A value that at least j of the wavefront's 64 reach, 1 <= j <= 64: the j-th largest without its last six bits (the lanes'
+// Values that at least j of the wavefront's 64 reach, 1 <= j <= 64: the j-th largest without its last six bits (the lanes'
 // numbers take their place, so that no two values are equal and a rank has one owner).
-__device__ __forceinline__ uint32_t wave_nth(uint32_t v, int j) {
-    v = (v & ~63u) | (63u - (threadIdx.x & 63));
+struct WaveRanks {
+    uint32_t v;
     int before = 0;
+    __device__ __forceinline__ explicit WaveRanks(uint32_t value) : v((value & ~63u) | (63u - (threadIdx.x & 63))) {
 #pragma unroll
-    for (int i = 0; i < 64; ++i) before += (uint32_t)__builtin_amdgcn_readlane((int)v, i) > v;
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, __ffsll((long long)__ballot(before == j - 1)) - 1) & ~63u;
-}
+        for (int i = 0; i < 64; ++i) before += (uint32_t)__builtin_amdgcn_readlane((int)v, i) > v;
+    }
+    __device__ __forceinline__ uint32_t nth(int j) const {
+        return (uint32_t)__builtin_amdgcn_readlane((int)v, __ffsll((long long)__ballot(before == j - 1)) - 1) & ~63u;
+    }
+};
 
 template <int CAP> struct Buffer {
     Cand cand[CAP], keep[ALS_TOPK_MAX_K];
@@ -170,16 +175,17 @@ struct PartSum {
 
 // Workgroup (x, y): part x (tiles_per_part tiles) of row y.  With one part a row it writes the answer, otherwise the part's
 // candidates, 0 in the slots that are left, and its exponential sum.
-template <bool BF16, bool RULES>
-__global__ __launch_bounds__(TILE_THREADS, RULES ? (BF16 ? 5 : 4) : 6) void select_kernel(const char *__restrict__ X, int64_t row_bytes, int64_t first_row, uint32_t cols, int k,
+template <bool BF16, bool RULES, int NT>
+__global__ __launch_bounds__(NT, NT == 1024 ? 4 : RULES ? (BF16 ? 5 : 4) : 6) void select_kernel(const char *__restrict__ X, int64_t row_bytes, int64_t first_row, uint32_t cols, int k,
                                                                  uint32_t tiles_per_part, float temperature, float scale, RuleArgs rules,
                                                                  Cand *__restrict__ part_cand, PartSum *__restrict__ part_sum,
                                                                  int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
-    typedef TileRow<BF16> Row;
-    constexpr int PER = Row::PER, PIECES = Row::PIECES, WAVES = TILE_THREADS / 64;
+    typedef TileRow<BF16, NT> Row;
+    constexpr int PER = Row::PER, PIECES = Row::PIECES, WAVES = NT / 64, TILE = Row::TILE;
+    constexpr int STEPS = select_steps<NT>(), EACH = TILE_EPT / STEPS, CAP = select_room<NT>();
     extern __shared__ __align__(16) uint32_t words[];
-    __shared__ Buffer<SELECT_CAP> buf;
-    __shared__ uint32_t wave_bar[WAVES];
+    __shared__ Buffer<CAP> buf;
+    __shared__ uint32_t wave_bar[WAVES], wave_kth[WAVES];
     __shared__ float wave_m[WAVES], wave_s[WAVES];
     __shared__ int added[3];  // candidates of a tile, by turns: the last one is cleared while this one is read
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, parts = gridDim.x;
@@ -194,7 +200,7 @@ __global__ __launch_bounds__(TILE_THREADS, RULES ? (BF16 ? 5 : 4) : 6) void sele
     ExpSum sum;
     float bar = -INFINITY;
     int have = 0, turn = 0;
-    const int most = parts > 1 ? PART_SLOTS : TILE_THREADS;  // candidates at the end
+    const int most = parts > 1 ? PART_SLOTS : SELECT_KEEP;  // candidates at the end
     if (tid < 3) added[tid] = 0;
     __syncthreads();
     for (uint32_t first = begin; first < end; first += TILE) {
@@ -235,31 +241,41 @@ __global__ __launch_bounds__(TILE_THREADS, RULES ? (BF16 ? 5 : 4) : 6) void sele
         sum.m = m;
 
         if (first == begin) {
-            const uint32_t nth = wave_nth(ordered_bits(top), (k + WAVES - 1) / WAVES);
-            if (lane == 0) wave_bar[wave] = nth;
+            // at least k reach the smallest of the wavefronts' ceil(k / WAVES)-th, and any wavefront's k-th: the latter counts
+            // where some wavefronts have nothing (short rows, sets that allow a stretch of items)
+            const WaveRanks ranks(ordered_bits(top));
+            const uint32_t nth = ranks.nth((k + WAVES - 1) / WAVES), kth = ranks.nth(k);
+            if (lane == 0) {
+                wave_bar[wave] = nth;
+                wave_kth[wave] = kth;
+            }
             __syncthreads();
-            uint32_t least = wave_bar[0];
+            uint32_t least = wave_bar[0], most_kth = wave_kth[0];
 #pragma unroll
-            for (int i = 1; i < WAVES; ++i) least = min(least, wave_bar[i]);
+            for (int i = 1; i < WAVES; ++i) {
+                least = min(least, wave_bar[i]);
+                most_kth = max(most_kth, wave_kth[i]);
+            }
+            least = max(least, most_kth);
             bar = bar_below(least);
         }
-        // The scores above the bar into the buffer: all at once, or, if they do not fit, a quarter of the tile after the other.
-        for (int q0 = 0, q1 = 4; q0 < 4;) {
+        // The scores above the bar into the buffer: all at once, or, if they do not fit, step by step.
+        for (int q0 = 0, q1 = STEPS; q0 < STEPS;) {
             if (__any(top > bar)) {
                 int mine_above = 0;
 #pragma unroll
-                for (int i = 0; i < TILE_EPT; ++i) mine_above += i / 4 >= q0 && i / 4 < q1 && x[i / PER][i % PER] > bar;
+                for (int i = 0; i < TILE_EPT; ++i) mine_above += i / EACH >= q0 && i / EACH < q1 && x[i / PER][i % PER] > bar;
                 const int upto = wave_scan(mine_above, 0, [](int a, int b) { return a + b; });
                 int at = 0;
                 if (lane == 63) at = atomicAdd(&added[turn], upto);
                 at = have + __builtin_amdgcn_readlane(at, 63) + upto - mine_above;
 #pragma unroll
                 for (int i = 0; i < TILE_EPT; ++i)
-                    if (i / 4 >= q0 && i / 4 < q1 && x[i / PER][i % PER] > bar) {
+                    if (i / EACH >= q0 && i / EACH < q1 && x[i / PER][i % PER] > bar) {
                         float v = x[i / PER][i % PER];
                         uint32_t from = first;
                         asm volatile("" : "+v"(v), "+s"(from));  // nothing is prepared for those that do not come here
-                        if (at < SELECT_CAP) buf.cand[at] = candidate(v, from + Row::item(i / PER, tid) + i % PER);
+                        if (at < CAP) buf.cand[at] = candidate(v, from + Row::item(i / PER, tid) + i % PER);
                         ++at;
                     }
             }
@@ -267,17 +283,17 @@ __global__ __launch_bounds__(TILE_THREADS, RULES ? (BF16 ? 5 : 4) : 6) void sele
             int count = have + __builtin_amdgcn_readfirstlane(added[turn]);
             if (tid == 0) added[turn == 0 ? 2 : turn - 1] = 0;
             turn = turn == 2 ? 0 : turn + 1;
-            if (count > SELECT_CAP) {
+            if (count > CAP) {
                 q1 = 1;
                 continue;
             }
             q0 = q1;
             q1 = q0 + 1;
-            if (count > (last && q0 == 4 ? most : SELECT_KEEP)) {
-                const Cand nth = buf.template cut_back<TILE_THREADS>(count, k, tid);
+            if (count > (last && q0 == STEPS ? most : SELECT_KEEP)) {
+                const Cand nth = buf.template cut_back<NT>(count, k, tid);
                 count = k;
-                // the tile's other quarters may hold an equal score with a smaller id, later tiles may not
-                bar = q0 == 4 ? bar_at(nth) : bar_below((uint32_t)(nth >> 32));
+                // the tile's other steps may hold an equal score with a smaller id, later tiles may not
+                bar = q0 == STEPS ? bar_at(nth) : bar_below((uint32_t)(nth >> 32));
             }
             have = count;
         }
@@ -344,7 +360,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
                 best = max(best, (uint32_t)(c[i] >> 32));
             }
             if (wave == 0 && lane < parts) all.add(part[lane].m, part[lane].s, scale);
-            const uint32_t nth = wave_nth(best, (k + WAVES - 1) / WAVES);
+            const uint32_t nth = WaveRanks(best).nth((k + WAVES - 1) / WAVES);
             if (lane == 0) wave_bar[wave] = nth;
             __syncthreads();
             uint32_t least = wave_bar[0];  // at least k candidates reach it, if there are as many
@@ -357,7 +373,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
             if (tid == 0) listed = 0;
             uint32_t best = 0;
             for (int p = lane * WAVES + wave; p < parts; p += MERGE_THREADS) best = max(best, part[p].best);
-            const uint32_t nth = wave_nth(best, (k + WAVES - 1) / WAVES);
+            const uint32_t nth = WaveRanks(best).nth((k + WAVES - 1) / WAVES);
             if (lane == 0) wave_bar[wave] = nth;
             __syncthreads();
             uint32_t least = wave_bar[0];
@@ -418,15 +434,51 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
     }
 }
 
+template <bool BF16, bool RULES, int NT>
+static als_status select_launch(als_ctx *ctx, const als_matrix *X, const RuleArgs &a, int64_t parts, int64_t tiles_per_part, float temperature,
+                                int k, int32_t *ids, float *scores, float *lse, hipStream_t s) {
+    constexpr int TILE = NT * TILE_EPT;
+    const float scale = 1.44269504f / temperature;
+    Cand *cand = nullptr;
+    PartSum *sums = nullptr;
+    if (parts > 1) {
+        const size_t cand_bytes = (size_t)X->rows * parts * PART_SLOTS * sizeof(Cand);
+        als_status st = ensure(ctx, ctx->select_partials, cand_bytes + (size_t)X->rows * parts * sizeof(PartSum));
+        if (st != ALS_OK) return st;
+        cand = (Cand *)ctx->select_partials.p;
+        sums = (PartSum *)((char *)ctx->select_partials.p + cand_bytes);
+    }
+    if (NT == 1024) {  // two lists' words are 128 KB
+        static const hipError_t attr = hipFuncSetAttribute((const void *)select_kernel<BF16, RULES, NT>,
+                                                           hipFuncAttributeMaxDynamicSharedMemorySize, 2 * TILE * 4);  // once per process
+        ALS_HIP(ctx, attr);
+    }
+    for (int64_t row = 0; row < X->rows; row += 65535)  // a grid's second dimension
+        hipLaunchKernelGGL((select_kernel<BF16, RULES, NT>), dim3((unsigned)parts, (unsigned)std::min<int64_t>(X->rows - row, 65535)), dim3(NT),
+                           rule_bytes(a, TILE), s, (const char *)X->data, X->ld * (BF16 ? 2 : 4), row, (uint32_t)X->cols, k,
+                           (uint32_t)tiles_per_part, temperature, scale, a, cand, sums, ids, scores, lse);
+    if (parts > 1) {
+        auto merge = [&](auto threads) {
+            hipLaunchKernelGGL((select_merge_kernel<threads()>), dim3((unsigned)std::min<int64_t>(X->rows, 1 << 20)), dim3(threads()), 0, s,
+                               X->rows, k, (int)parts, temperature, scale, (const Cand *)cand, (const PartSum *)sums, ids, scores, lse);
+        };
+        if (parts <= merge_few<256>()) merge(std::integral_constant<int, 256>{});
+        else merge(std::integral_constant<int, 1024>{});
+    }
+    ALS_HIP(ctx, hipGetLastError());
+    return ALS_OK;
+}
+
 als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int k, int32_t *ids,
                          float *scores, float *lse, hipStream_t s) {
     const RuleArgs a = rule_args(rules);
-    const int64_t tiles = (X->cols + TILE - 1) / TILE;
     const bool bf = X->dtype == ALS_BF16, any = a.history.indptr || a.entries.indptr || a.bias || a.allowed;
+    constexpr int TILE = 256 * TILE_EPT;
+    const int64_t tiles = (X->cols + TILE - 1) / TILE;
     // Parts of a row.  The card holds `slots` workgroups at a time (registers for four to six per compute unit, LDS for a buffer
     // and the lists' words); a row's parts are chosen so that the rounds of workgroups are full: with r rounds a workgroup
     // walks ceil(tiles / parts) tiles, and beginning and ending a part costs about as much as four more.
-    const int64_t lds_bytes = (int64_t)rule_bytes(a) + (int64_t)sizeof(Buffer<SELECT_CAP>) + 256;
+    const int64_t lds_bytes = (int64_t)rule_bytes(a, TILE) + (int64_t)sizeof(Buffer<select_room<256>()>) + 256;
     const int64_t slots = ctx->num_cu * std::min<int64_t>(any ? (bf ? 5 : 4) : 6, 160 * 1024 / lds_bytes);
     int64_t per = tiles, least = INT64_MAX;
     for (int64_t r = 1; r <= 8; ++r) {
@@ -438,36 +490,18 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
         }
     }
     const int64_t parts = std::max<int64_t>(1, (tiles + per - 1) / std::max<int64_t>(1, per));
-    const float scale = 1.44269504f / temperature;
-    Cand *cand = nullptr;
-    PartSum *sums = nullptr;
-    if (parts > 1) {
-        const size_t cand_bytes = (size_t)X->rows * parts * PART_SLOTS * sizeof(Cand);
-        als_status st = ensure(ctx, ctx->select_partials, cand_bytes + (size_t)X->rows * parts * sizeof(PartSum));
-        if (st != ALS_OK) return st;
-        cand = (Cand *)ctx->select_partials.p;
-        sums = (PartSum *)((char *)ctx->select_partials.p + cand_bytes);
-    }
-    auto go = [&](auto bf, auto with_rules) {
-        for (int64_t row = 0; row < X->rows; row += 65535)  // a grid's second dimension
-            hipLaunchKernelGGL((select_kernel<bf(), with_rules()>), dim3((unsigned)parts, (unsigned)std::min<int64_t>(X->rows - row, 65535)),
-                           dim3(TILE_THREADS), rule_bytes(a), s, (const char *)X->data, X->ld * (bf() ? 2 : 4), row, (uint32_t)X->cols, k, (uint32_t)per, temperature, scale, a, cand, sums, ids,
-                           scores, lse);
+    // One workgroup of 1024 threads per row where a row is short and the rows do not fill the card: no parts to merge.  With parts /
+    // so, in us, k = 50: 1 x 16000 17 / 14, 64 x 30000 17 / 15, 256 x 128000 42 / 34, with lists, biases and sets 64 x 16000 21 / 18,
+    // 256 x 128000 74 / 61; but 64 x 128000 26 / 30, 64 x 30000 with all rules 21 / 23, 2048 x 16000 42 / 83.
+    const int64_t wide_tiles = (X->cols + 4 * TILE - 1) / (4 * TILE);
+    const double fill = (double)X->rows / ctx->num_cu;
+    const bool wide = parts > 1 && fill <= 1 && (double)wide_tiles <= (any ? 1 : 2) + (any ? 7 : 6) * fill * fill;
+    auto typed = [&](auto b, auto r) {
+        if (wide) return select_launch<b(), r(), 1024>(ctx, X, a, 1, wide_tiles, temperature, k, ids, scores, lse, s);
+        return select_launch<b(), r(), 256>(ctx, X, a, parts, per, temperature, k, ids, scores, lse, s);
     };
-    if (bf && any) go(std::true_type{}, std::true_type{});
-    else if (bf) go(std::true_type{}, std::false_type{});
-    else if (any) go(std::false_type{}, std::true_type{});
-    else go(std::false_type{}, std::false_type{});
-    if (parts > 1) {
-        auto merge = [&](auto threads) {
-            hipLaunchKernelGGL((select_merge_kernel<threads()>), dim3((unsigned)std::min<int64_t>(X->rows, 1 << 20)), dim3(threads()), 0, s, X->rows, k,
-                               (int)parts, temperature, scale, (const Cand *)cand, (const PartSum *)sums, ids, scores, lse);
-        };
-        if (parts <= merge_few<256>()) merge(std::integral_constant<int, 256>{});
-        else merge(std::integral_constant<int, 1024>{});
-    }
-    ALS_HIP(ctx, hipGetLastError());
-    return ALS_OK;
+    if (bf) return any ? typed(std::true_type{}, std::true_type{}) : typed(std::true_type{}, std::false_type{});
+    return any ? typed(std::false_type{}, std::true_type{}) : typed(std::false_type{}, std::false_type{});
 }
 
 }  // namespace als
