@@ -21,7 +21,7 @@ __global__ __launch_bounds__(ADJUST_THREADS) void adjust_kernel(const void *X, i
         Row in;
         in.load((const char *)X + row * ldx * (BF_IN ? 2 : 4), first, cols, tid);
         RowRules<Row> mine;
-        mine.begin(rules, row, words, tid);
+        mine.begin(rules, row, first, words, tid);
         float x[Row::PIECES][Row::PER];
         in.floats(x);
         mine.apply(rules, first, cols, tid, x);

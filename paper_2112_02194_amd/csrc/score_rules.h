@@ -58,6 +58,25 @@ template <class T> __device__ __forceinline__ T uniform_load(const T *p) {
     return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
 }
 
+// One value from lanes of the wavefront by lane moves (v_add_f32_dpp and the like): rows of 16 lanes first, then across them.
+// F is associative and commutative; the result is in lane 63.
+template <class T, class F> __device__ __forceinline__ T wave_scan(T x, T none, F &&f) {
+    auto step = [&](auto ctrl, auto rows) {
+        const int moved = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, x), ctrl(), rows(), 0xf, false);
+        x = f(x, __builtin_bit_cast(T, moved));
+    };
+    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});  // from 1, 2, 4, 8 lanes below in the row
+    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // the row's end to the next row: rows 1 and 3
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // lane 31 to rows 2 and 3
+    return x;  // of the lanes up to this one
+}
+template <class T, class F> __device__ __forceinline__ T wave_all(T x, T none, F &&f) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(x, none, f)), 63));
+}
+
 // A thread's elements of a tile: PIECES times PER consecutive ones, 16 bytes.  Rows need not be aligned beyond their elements.
 template <bool BF16, int NT> struct TileRow {
     static constexpr int THREADS = NT, TILE = NT * TILE_EPT;
@@ -112,11 +131,18 @@ template <class Row, bool PLACES> struct TileList {
     const int32_t *ids;
     int64_t begins = 0;  // the row's part of the list; none without a list
     int count = 0;
-    int32_t id[LIST_REGS];          // short lists: entry 64 r + lane, -1 beyond
-    uint32_t *words;                // a tile's words in LDS
+    uint32_t next = ~0u;    // short lists: the least item of the list that no tile has had yet
+    int32_t id[LIST_REGS];  // short lists: entry 64 r + lane, -1 beyond
+    uint32_t *words;        // a tile's words in LDS
 
     __device__ __forceinline__ bool in_regs() const { return count <= 64 * LIST_REGS; }
-    __device__ __forceinline__ void begin(const RowList &l, int64_t row, uint32_t *lds, int tid) {
+    __device__ __forceinline__ void find_next(uint32_t from) {
+        uint32_t least = ~0u;  // ids below 0 are beyond all items as unsigned numbers
+#pragma unroll
+        for (int r = 0; r < LIST_REGS; ++r) least = min(least, (uint32_t)id[r] >= from ? (uint32_t)id[r] : ~0u);
+        next = wave_all(least, ~0u, [](uint32_t a, uint32_t b) { return min(a, b); });
+    }
+    __device__ __forceinline__ void begin(const RowList &l, int64_t row, uint32_t first, uint32_t *lds, int tid) {
         words = lds;
         begins = count = 0;
         if (l.indptr) {
@@ -137,26 +163,21 @@ template <class Row, bool PLACES> struct TileList {
         for (int j = 0; j < Row::PIECES; ++j)
 #pragma unroll
             for (int c = 0; c < Row::PER; c += 4) *(uint4 *)(words + Row::item(j, tid) + c) = make_uint4(0, 0, 0, 0);
+        find_next(first);
     }
     // Enters the tile's items; true where the wavefront's words may be other than 0.  Long lists: all threads come here, with barriers.
     __device__ __forceinline__ bool enter(uint32_t first, int tid) {
-        if (count == 0) return false;
         if (in_regs()) {
-            bool any = false;
+            if (next - first >= Row::TILE) return false;
 #pragma unroll
             for (int r = 0; r < LIST_REGS; ++r) {
-                if (64 * r >= count) break;
                 const uint32_t at = (uint32_t)id[r] - first;
-                const bool mine = at < Row::TILE && Row::owner((int)at) == tid >> 6;
-                if (__any(mine)) {
-                    any = true;
-                    if (mine) {
-                        if constexpr (PLACES) atomicMax(words + at, (uint32_t)(64 * r + (tid & 63)) + 1u);
-                        else atomicAdd(words + at, 1u);
-                    }
+                if (at < Row::TILE && Row::owner((int)at) == tid >> 6) {
+                    if constexpr (PLACES) atomicMax(words + at, (uint32_t)(64 * r + (tid & 63)) + 1u);
+                    else atomicAdd(words + at, 1u);
                 }
             }
-            return any;
+            return true;
         }
         __syncthreads();  // the last tile's words have been read
         for (int i = tid * 4; i < Row::TILE; i += Row::THREADS * 4) *(uint4 *)(words + i) = make_uint4(0, 0, 0, 0);
@@ -183,10 +204,10 @@ template <class Row, bool PLACES> struct TileList {
         if (!in_regs()) return;
 #pragma unroll
         for (int r = 0; r < LIST_REGS; ++r) {
-            if (64 * r >= count) break;
             const uint32_t at = (uint32_t)id[r] - first;
             if (at < Row::TILE && Row::owner((int)at) == tid >> 6) words[at] = 0;
         }
+        find_next(first + Row::TILE);
     }
 };
 
@@ -196,9 +217,10 @@ template <class Row> struct RowRules {
     TileList<Row, true> entries;
     float r, p, f;
     const uint32_t *allowed;
-    __device__ __forceinline__ void begin(const RuleArgs &a, int64_t row, uint32_t *lds, int tid) {
-        history.begin(a.history, row, lds, tid);
-        entries.begin(a.entries, row, lds + (a.history.indptr ? Row::TILE : 0), tid);
+    // `first`: the first item that the workgroup works on
+    __device__ __forceinline__ void begin(const RuleArgs &a, int64_t row, uint32_t first, uint32_t *lds, int tid) {
+        history.begin(a.history, row, first, lds, tid);
+        entries.begin(a.entries, row, first, lds + (a.history.indptr ? Row::TILE : 0), tid);
         r = a.repetition; p = a.presence; f = a.frequency;
         if (a.penalties) {
             r = uniform_load(a.penalties + 3 * row);

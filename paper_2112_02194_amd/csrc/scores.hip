@@ -1,12 +1,10 @@
 // Scores of queries against a table in 4 bits an entry (als_scores): S[q][i] = sum_g scale(i, g) sum_{j in g} Q[q][j] code(i, j).
 //
-// Codes become fp16 numbers, exactly, two at a time: a code plus 8 put into the low bits of 1024's mantissa is the number
-// 1024 + code + 8, from which a packed subtraction takes 1032; nibbles four bits further up come out times 16 and take a
-// packed multiply-add instead.  About nine vector instructions for eight codes.  Both kernels form the group's sum first and
-// multiply it by the group's scale once.
+// Both kernels form a group's sum of products first and multiply it by the group's scale once.
 //
-// few queries    (one or two) the vector units: 32 codes of an item per lane, products with the query's fp32 entries by
-//                mixed-precision multiply-adds, sums over the lanes of an item by lane moves.
+// few queries    (up to four) the vector units: 32 or 16 codes of an item per lane.  Codes are put into the upper halves of
+//                signed bytes, 16 times their value, and converted to fp32 from there (11 instructions for eight); the queries are
+//                held in fp32, a sixteenth of their value.  Sums over the lanes of an item by lane moves.
 // more           the matrix cores, 32 queries x 32 items x 16 entries an instruction.  Query rows become two fp16 parts,
 //                hi + lo, after a shift by a power of two that brings their largest entry to 2^13 .. 2^14: 22 bits and more of
 //                every entry within 2^-16 of the largest, an absolute error of 2^-39 of the largest below (bf16 queries need
@@ -23,8 +21,10 @@ typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// The eight codes of a word as fp16 numbers: element e of the word is c[e % 4][e / 4].  (w & mask) ^ bits in one instruction:
-// the exclusive or turns two's complement into code + 8 beside filling in the exponent.
+// The eight codes of a word as fp16 numbers, exactly: element e of the word is c[e % 4][e / 4].  A code plus 8 put into the low
+// bits of 1024's mantissa is the number 1024 + code + 8, from which a packed subtraction takes 1032; nibbles four bits further
+// up come out times 16 and take a packed multiply-add instead: nine instructions.  (w & mask) ^ bits is one of them: the exclusive
+// or turns two's complement into code + 8 beside filling in the exponent.
 __device__ __forceinline__ void unpack8(uint32_t w, halfx2 (&c)[4]) {
     const halfx2 k1 = {(_Float16)1032.f, (_Float16)1032.f}, k2 = {(_Float16)0.0625f, (_Float16)0.0625f}, k3 = {(_Float16)72.f, (_Float16)72.f};
     const uint32_t v = w >> 8;
@@ -38,12 +38,15 @@ __device__ __forceinline__ void unpack8(uint32_t w, halfx2 (&c)[4]) {
 }
 
 // ------------------------------------------------------------------------------------------------ few queries
+// What bounds it: the read of the codes (1 x 20M, d = 128, groups of 32: 300 us, 5.1 TB/s, as fast as a copy), with more queries the
+// vector units.
 template <bool BF_Q, bool BF_S, int D, int G, int NQ>
-__global__ __launch_bounds__(256, 4) void scores_few_kernel(const void *__restrict__ Q, int64_t ldq, const uint8_t *__restrict__ codes,
+__global__ __launch_bounds__(256, NQ > 2 ? 3 : 4) void scores_few_kernel(const void *__restrict__ Q, int64_t ldq, const uint8_t *__restrict__ codes,
                                                             const uint16_t *__restrict__ scales, int64_t n, void *__restrict__ S,
                                                             int64_t lds) {
-    constexpr int CPL = D < 32 ? D : 32, LPI = D / CPL, IPS = 64 / LPI, U = 4;  // codes per lane, lanes per item, items per step, steps
-    constexpr int W = CPL / 8, NG = CPL > G ? CPL / G : 1, WPG = W / NG;         // words and groups per lane, words per group
+    // codes per lane, lanes per item, items per step, steps
+    constexpr int CPL = D < 32 || NQ > 2 ? 16 : 32, LPI = D / CPL, IPS = 64 / LPI, U = LPI > 4 ? LPI : 4;
+    constexpr int W = CPL / 8, NG = CPL > G ? CPL / G : 1, WPG = W / NG;  // words and groups per lane, words per group
     const int lane = threadIdx.x & 63, chunk = lane % LPI;
     const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), waves = (int64_t)gridDim.x * 4;
     float q[NQ][CPL];
@@ -54,7 +57,7 @@ __global__ __launch_bounds__(256, 4) void scores_few_kernel(const void *__restri
             float x[8];
             piece_floats<BF_Q>(piece_load<BF_Q>(Q, r * ldq + chunk * CPL + 8 * p), x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[r][8 * p + e] = x[e];
+            for (int e = 0; e < 8; ++e) q[r][8 * p + e] = x[e] * 0.0625f;
         }
     uint32_t next_w[U][W];
     uint32_t next_s[U];
@@ -101,12 +104,13 @@ __global__ __launch_bounds__(256, 4) void scores_few_kernel(const void *__restri
                 for (int r = 0; r < NQ; ++r) part[r] = 0.f;
 #pragma unroll
                 for (int p = g * WPG; p < (g + 1) * WPG; ++p) {
-                    halfx2 c[4];
-                    unpack8(w[u][p], c);
+                    const uint32_t half[2] = {w[u][p] << 4 & 0xf0f0f0f0u, w[u][p] & 0xf0f0f0f0u};  // even and odd entries
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
+                    for (int e = 0; e < 8; ++e) {
+                        const float c = (float)(int8_t)(half[e & 1] >> (8 * (e / 2)));
 #pragma unroll
-                        for (int r = 0; r < NQ; ++r) part[r] = fmaf((float)c[e % 4][e / 4], q[r][8 * p + e], part[r]);
+                        for (int r = 0; r < NQ; ++r) part[r] = fmaf(c, q[r][8 * p + e], part[r]);
+                    }
                 }
 #pragma unroll
                 for (int r = 0; r < NQ; ++r) sum[r][u] = fmaf(part[r], s[u][g], sum[r][u]);
@@ -170,6 +174,29 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
     const int64_t step = 4 * (int64_t)stretch, begin = block * (step * rounds);
     const int64_t first = begin + 4 * (in_block % stretch) + wave, last = std::min(spans, begin + step * rounds);
 
+    uint32_t w[2][T::PARTS][T::STEPS], raw[2][(NS + 1) / 2];
+    auto fetch = [&](int64_t span) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int64_t item = std::min<int64_t>(span * 64 + 2 * a + c, n - 1);
+#pragma unroll
+            for (int t = 0; t < T::PARTS; ++t) {
+                const uint32_t *at = codes + item * (D / 8) + T::word(t, 0, h);
+                if constexpr (T::STEPS == 2) {
+                    const u32x2 v = *(const u32x2 *)at;
+                    w[c][t][0] = v[0];
+                    w[c][t][1] = v[1];
+                } else {
+                    w[c][t][0] = *at;
+                }
+            }
+            const uint16_t *ps = scales + item * NS;
+            if constexpr (NS == 1) raw[c][0] = *ps;
+            else __builtin_memcpy(raw[c], __builtin_assume_aligned(ps, NS < 8 ? 2 * NS : 16), 2 * NS);
+        }
+    };
+    if (first < last) fetch(first);  // on its way while the queries are prepared
+
     // The queries as operands, in LDS for the four wavefronts (registers for them would halve the wavefronts), shifted so that
     // the largest finite entry of a row lies in [2^13, 2^14).  Each wavefront makes every fourth step's.
     constexpr int NSTEP = D / 16, MINE = (NSTEP + 3) / 4;
@@ -221,27 +248,6 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
     const bool q_wide = __any(shift > 60 || shift < -60);
     if (first >= last) return;
 
-    uint32_t w[2][T::PARTS][T::STEPS], raw[2][(NS + 1) / 2];
-    auto fetch = [&](int64_t span) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const int64_t item = std::min<int64_t>(span * 64 + 2 * a + c, n - 1);
-#pragma unroll
-            for (int t = 0; t < T::PARTS; ++t) {
-                const uint32_t *at = codes + item * (D / 8) + T::word(t, 0, h);
-                if constexpr (T::STEPS == 2) {
-                    const u32x2 v = *(const u32x2 *)at;
-                    w[c][t][0] = v[0];
-                    w[c][t][1] = v[1];
-                } else {
-                    w[c][t][0] = *at;
-                }
-            }
-            const uint16_t *ps = scales + item * NS;
-            if constexpr (NS == 1) raw[c][0] = *ps;
-            else __builtin_memcpy(raw[c], __builtin_assume_aligned(ps, NS < 8 ? 2 * NS : 16), 2 * NS);
-        }
-    };
     // Waits for fetch's loads: at the end of a round the compiler knows how many stores came after them and lets those be.
     auto arrived = [&] {
 #pragma unroll
@@ -352,7 +358,6 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
     const int rows = (int)std::min<int64_t>(32, nq - q0);
     int64_t span = first;
     const int64_t whole = std::min(last, n / 64);
-    fetch(first);
     arrived();
     if (as == StoreAs::BUFFER) {
         const uint32_t half = (uint32_t)(4 * lds * ES);  // bytes from a row to that of the upper half's lanes
@@ -409,20 +414,27 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
     }
 }
 
-constexpr int SCORES_FEW = 2;  // queries up to which the vector units work
+// Queries up to which the vector units work; 3 and 4 on them / on the matrix cores: 1M, d = 128, fp32 26 and 32 / 34 us, 3M, d = 64,
+// groups of 16 37 and 43 / 68 us, 1M, d = 16, bf16 8 / 14 us, but 10M, d = 128, bf16 (one part of a query on the matrix cores) 227 and
+// 263 / 229 us.
+template <bool BF_Q, int D> constexpr int scores_few() { return BF_Q && D == 128 ? 2 : 4; }
 
 template <bool BF_Q, bool BF_S, int D, int G>
 static void scores_typed(const als_ctx *ctx, const als_table *Q, const als_qtable *T, const als_matrix *S, hipStream_t s) {
     const int64_t n = T->rows, nq = Q->rows;
-    if (nq <= SCORES_FEW) {
-        constexpr int ITEMS = 4 * 4 * 64 / (D / (D < 32 ? D : 32));  // of a workgroup's round
-        const dim3 grid((unsigned)std::min<int64_t>((n + ITEMS - 1) / ITEMS, (int64_t)ctx->num_cu * 8));
+    if (nq <= scores_few<BF_Q, D>()) {
         auto go = [&](auto count) {
+            constexpr int LPI = D / (D < 32 || count() > 2 ? 16 : 32), ITEMS = 4 * (64 / LPI) * (LPI > 4 ? LPI : 4);  // of a workgroup's round
+            const dim3 grid((unsigned)std::min<int64_t>((n + ITEMS - 1) / ITEMS, (int64_t)ctx->num_cu * 8));
             hipLaunchKernelGGL((scores_few_kernel<BF_Q, BF_S, D, G, count()>), grid, dim3(256), 0, s, Q->data, Q->ld,
                                (const uint8_t *)T->codes, (const uint16_t *)T->scales, n, S->data, S->ld);
         };
         if (nq == 1) go(std::integral_constant<int, 1>{});
-        else go(std::integral_constant<int, 2>{});
+        else if (nq == 2) go(std::integral_constant<int, 2>{});
+        else if constexpr (scores_few<BF_Q, D>() == 4) {
+            if (nq == 3) go(std::integral_constant<int, 3>{});
+            else go(std::integral_constant<int, 4>{});
+        }
         return;
     }
     const int64_t qgroups = (nq + 31) / 32, spans = (n + 63) / 64;

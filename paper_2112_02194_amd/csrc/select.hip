@@ -37,25 +37,6 @@ constexpr uint32_t ORDERED_LOWEST = 0x007fffffu, ORDERED_ZERO = 0x80000000u;  //
 __device__ __forceinline__ float bar_below(uint32_t o) { return from_ordered(max(o == ORDERED_ZERO ? o - 1 : o, ORDERED_LOWEST + 1) - 1); }
 __device__ __forceinline__ float bar_at(Cand c) { return from_ordered(max((uint32_t)(c >> 32), ORDERED_LOWEST)); }
 
-// One value from lanes of the wavefront by lane moves (v_add_f32_dpp and the like): rows of 16 lanes first, then across them.
-// F is associative and commutative; the result is in lane 63.
-template <class T, class F> __device__ __forceinline__ T wave_scan(T x, T none, F &&f) {
-    auto step = [&](auto ctrl, auto rows) {
-        const int moved = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, x), ctrl(), rows(), 0xf, false);
-        x = f(x, __builtin_bit_cast(T, moved));
-    };
-    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});  // from 1, 2, 4, 8 lanes below in the row
-    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
-    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
-    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
-    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // the row's end to the next row: rows 1 and 3
-    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // lane 31 to rows 2 and 3
-    return x;  // of the lanes up to this one
-}
-template <class T, class F> __device__ __forceinline__ T wave_all(T x, T none, F &&f) {
-    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(x, none, f)), 63));
-}
-
 // Values that at least j of the wavefront's 64 reach, 1 <= j <= 64: the j-th largest without its last six bits (the lanes'
 // numbers take their place, so that no two values are equal and a rank has one owner).
 struct WaveRanks {
@@ -196,7 +177,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : RULES ? (BF16 ? 5 : 4) : 6) vo
     Row in;
     if (begin < end) in.load(scores_row, begin, cols, tid);
     RowRules<Row> mine;
-    if constexpr (RULES) mine.begin(rules, row, words, tid);
+    if constexpr (RULES) mine.begin(rules, row, begin, words, tid);
     ExpSum sum;
     float bar = -INFINITY;
     int have = 0, turn = 0;
