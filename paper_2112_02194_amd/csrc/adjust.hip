@@ -20,7 +20,7 @@ __global__ __launch_bounds__(ADJUST_THREADS) void adjust_kernel(const void *X, i
         for (uint32_t first = blockIdx.y * TILE; first < cols; first += gridDim.y * TILE) {
         Row in;
         in.load((const char *)X + row * ldx * (BF_IN ? 2 : 4), first, cols, tid);
-        RowRules<Row> mine;
+        RowRules<Row, RULES_ALL> mine;
         mine.begin(rules, row, first, words, tid);
         float x[Row::PIECES][Row::PER];
         in.floats(x);

@@ -211,8 +211,14 @@ template <class Row, bool PLACES> struct TileList {
     }
 };
 
+// Which rules a kernel has the code for: what a call has not given costs registers and a look per tile.
+enum RuleSet { RULES_NONE, RULES_HISTORY, RULES_ALL };
+inline RuleSet rule_set(const RuleArgs &a) {
+    return a.entries.indptr || a.bias || a.allowed ? RULES_ALL : a.history.indptr ? RULES_HISTORY : RULES_NONE;
+}
+
 // The rules of one row over the tiles that a workgroup works on.
-template <class Row> struct RowRules {
+template <class Row, RuleSet SET> struct RowRules {
     TileList<Row, false> history;
     TileList<Row, true> entries;
     float r, p, f;
@@ -220,20 +226,21 @@ template <class Row> struct RowRules {
     // `first`: the first item that the workgroup works on
     __device__ __forceinline__ void begin(const RuleArgs &a, int64_t row, uint32_t first, uint32_t *lds, int tid) {
         history.begin(a.history, row, first, lds, tid);
-        entries.begin(a.entries, row, first, lds + (a.history.indptr ? Row::TILE : 0), tid);
+        if constexpr (SET == RULES_ALL) entries.begin(a.entries, row, first, lds + (a.history.indptr ? Row::TILE : 0), tid);
         r = a.repetition; p = a.presence; f = a.frequency;
         if (a.penalties) {
             r = uniform_load(a.penalties + 3 * row);
             p = uniform_load(a.penalties + 3 * row + 1);
             f = uniform_load(a.penalties + 3 * row + 2);
         }
-        allowed = a.allowed ? a.allowed + row * a.allowed_ld : nullptr;
+        if constexpr (SET == RULES_ALL) allowed = a.allowed ? a.allowed + row * a.allowed_ld : nullptr;
     }
     // x changed by the rules.  All threads of the workgroup come here.  Every operation rounds by itself, as it is defined.
     __device__ __forceinline__ void apply(const RuleArgs &a, uint32_t first, uint32_t cols, int tid, float (&x)[Row::PIECES][Row::PER]) {
 #pragma clang fp contract(off)
-        const bool had = history.enter(first, tid), added = entries.enter(first, tid);
-        const uint32_t left = cols - first;
+        const bool had = history.enter(first, tid);
+        bool added = false;
+        if constexpr (SET == RULES_ALL) added = entries.enter(first, tid);
         if (had) {
 #pragma unroll
             for (int j = 0; j < Row::PIECES; ++j)
@@ -253,6 +260,8 @@ template <class Row> struct RowRules {
                 }
             history.leave(first, tid);
         }
+        if constexpr (SET != RULES_ALL) return;
+        const uint32_t left = cols - first;
         __builtin_amdgcn_sched_barrier(0);  // one rule after the other: their loads together take more registers than there are
         if (a.bias) {
             const float *bias = a.bias + first;

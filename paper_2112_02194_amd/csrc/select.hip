@@ -20,11 +20,11 @@
 namespace als {
 
 typedef unsigned long long Cand;
-constexpr int SELECT_KEEP = 256;  // the buffer is cut back to k when it holds more than this after a tile
-constexpr int PART_SLOTS = 128;   // candidates that a part hands on at most
+constexpr int PART_SLOTS = 128;  // the buffer is cut back to k when it holds more after a tile; what a part hands on at most
+static_assert(ALS_TOPK_MAX_K <= PART_SLOTS && PART_SLOTS <= 256, "k fits in a part's slots, and one slot a thread is handed on");
 // A tile that does not fit goes in STEPS steps; the buffer has room for what is kept and one of them.
 template <int NT> constexpr int select_steps() { return NT == 1024 ? 8 : 4; }
-template <int NT> constexpr int select_room() { return SELECT_KEEP + NT * TILE_EPT / select_steps<NT>(); }
+template <int NT> constexpr int select_room() { return PART_SLOTS + NT * TILE_EPT / select_steps<NT>(); }
 
 __device__ __forceinline__ uint32_t ordered_bits(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);  // -0 becomes 0: equal scores
@@ -154,13 +154,21 @@ struct PartSum {
     uint32_t best, unused;  // the best candidate's score, ordered; 0: none
 };
 
+// Wavefronts per SIMD that the registers are bounded for: as many as spill no more than two.  A workgroup of 256 threads has one on
+// each SIMD.
+constexpr int select_waves(bool bf16, RuleSet rules, int threads) {
+    return threads == 1024 ? 4 : rules == RULES_ALL ? (bf16 ? 5 : 4) : rules == RULES_HISTORY && !bf16 ? 5 : 6;
+}
+
 // Workgroup (x, y): part x (tiles_per_part tiles) of row y.  With one part a row it writes the answer, otherwise the part's
 // candidates, 0 in the slots that are left, and its exponential sum.
-template <bool BF16, bool RULES, int NT>
-__global__ __launch_bounds__(NT, NT == 1024 ? 4 : RULES ? (BF16 ? 5 : 4) : 6) void select_kernel(const char *__restrict__ X, int64_t row_bytes, int64_t first_row, uint32_t cols, int k,
-                                                                 uint32_t tiles_per_part, float temperature, float scale, RuleArgs rules,
-                                                                 Cand *__restrict__ part_cand, PartSum *__restrict__ part_sum,
-                                                                 int32_t *__restrict__ ids, float *__restrict__ scores, float *__restrict__ lse) {
+template <bool BF16, RuleSet RULES, int NT>
+__global__ __launch_bounds__(NT, select_waves(BF16, RULES, NT)) void select_kernel(const char *__restrict__ X, int64_t row_bytes,
+                                                                                   int64_t first_row, uint32_t cols, int k,
+                                                                                   uint32_t tiles_per_part, float temperature, float scale,
+                                                                                   RuleArgs rules, Cand *__restrict__ part_cand,
+                                                                                   PartSum *__restrict__ part_sum, int32_t *__restrict__ ids,
+                                                                                   float *__restrict__ scores, float *__restrict__ lse) {
     typedef TileRow<BF16, NT> Row;
     constexpr int PER = Row::PER, PIECES = Row::PIECES, WAVES = NT / 64, TILE = Row::TILE;
     constexpr int STEPS = select_steps<NT>(), EACH = TILE_EPT / STEPS, CAP = select_room<NT>();
@@ -176,20 +184,18 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : RULES ? (BF16 ? 5 : 4) : 6) vo
     const char *scores_row = X + row * row_bytes;
     Row in;
     if (begin < end) in.load(scores_row, begin, cols, tid);
-    RowRules<Row> mine;
-    if constexpr (RULES) mine.begin(rules, row, begin, words, tid);
+    RowRules<Row, RULES> mine;
+    if constexpr (RULES != RULES_NONE) mine.begin(rules, row, begin, words, tid);
     ExpSum sum;
     float bar = -INFINITY;
     int have = 0, turn = 0;
-    const int most = parts > 1 ? PART_SLOTS : SELECT_KEEP;  // candidates at the end
     if (tid < 3) added[tid] = 0;
     __syncthreads();
     for (uint32_t first = begin; first < end; first += TILE) {
         float x[PIECES][PER];
         in.floats(x);
-        const bool last = first + TILE >= end;
-        if (!last) in.load(scores_row, first + TILE, cols, tid);
-        if constexpr (RULES) mine.apply(rules, first, cols, tid, x);
+        if (first + TILE < end) in.load(scores_row, first + TILE, cols, tid);
+        if constexpr (RULES != RULES_NONE) mine.apply(rules, first, cols, tid, x);
         if (first + TILE > cols) {
             const uint32_t left = cols - first;
 #pragma unroll
@@ -243,22 +249,27 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : RULES ? (BF16 ? 5 : 4) : 6) vo
         // The scores above the bar into the buffer: all at once, or, if they do not fit, step by step.
         for (int q0 = 0, q1 = STEPS; q0 < STEPS;) {
             if (__any(top > bar)) {
-                int mine_above = 0;
+                float step_bar[STEPS];
 #pragma unroll
-                for (int i = 0; i < TILE_EPT; ++i) mine_above += i / EACH >= q0 && i / EACH < q1 && x[i / PER][i % PER] > bar;
-                const int upto = wave_scan(mine_above, 0, [](int a, int b) { return a + b; });
+                for (int q = 0; q < STEPS; ++q) step_bar[q] = q >= q0 && q < q1 ? bar : INFINITY;
+                int above = 0;
+#pragma unroll
+                for (int i = 0; i < TILE_EPT; ++i) above += __popcll(__ballot(x[i / PER][i % PER] > step_bar[i / EACH]));
                 int at = 0;
-                if (lane == 63) at = atomicAdd(&added[turn], upto);
-                at = have + __builtin_amdgcn_readlane(at, 63) + upto - mine_above;
+                if (lane == 0) at = atomicAdd(&added[turn], above);
+                at = have + __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-                for (int i = 0; i < TILE_EPT; ++i)
-                    if (i / EACH >= q0 && i / EACH < q1 && x[i / PER][i % PER] > bar) {
+                for (int i = 0; i < TILE_EPT; ++i) {
+                    const unsigned long long who = __ballot(x[i / PER][i % PER] > step_bar[i / EACH]);
+                    if (who) {
                         float v = x[i / PER][i % PER];
                         uint32_t from = first;
                         asm volatile("" : "+v"(v), "+s"(from));  // nothing is prepared for those that do not come here
-                        if (at < CAP) buf.cand[at] = candidate(v, from + Row::item(i / PER, tid) + i % PER);
-                        ++at;
+                        const int place = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                        if (v > step_bar[i / EACH] && place < CAP) buf.cand[place] = candidate(v, from + Row::item(i / PER, tid) + i % PER);
+                        at += __popcll(who);
                     }
+                }
             }
             __syncthreads();
             int count = have + __builtin_amdgcn_readfirstlane(added[turn]);
@@ -270,7 +281,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : RULES ? (BF16 ? 5 : 4) : 6) vo
             }
             q0 = q1;
             q1 = q0 + 1;
-            if (count > (last && q0 == STEPS ? most : SELECT_KEEP)) {
+            if (count > PART_SLOTS) {
                 const Cand nth = buf.template cut_back<NT>(count, k, tid);
                 count = k;
                 // the tile's other steps may hold an equal score with a smaller id, later tiles may not
@@ -415,7 +426,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void select_merge_kernel(int64_t row
     }
 }
 
-template <bool BF16, bool RULES, int NT>
+template <bool BF16, RuleSet RULES, int NT>
 static als_status select_launch(als_ctx *ctx, const als_matrix *X, const RuleArgs &a, int64_t parts, int64_t tiles_per_part, float temperature,
                                 int k, int32_t *ids, float *scores, float *lse, hipStream_t s) {
     constexpr int TILE = NT * TILE_EPT;
@@ -453,14 +464,15 @@ static als_status select_launch(als_ctx *ctx, const als_matrix *X, const RuleArg
 als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int k, int32_t *ids,
                          float *scores, float *lse, hipStream_t s) {
     const RuleArgs a = rule_args(rules);
-    const bool bf = X->dtype == ALS_BF16, any = a.history.indptr || a.entries.indptr || a.bias || a.allowed;
+    const RuleSet set = rule_set(a);
+    const bool bf = X->dtype == ALS_BF16, all = set == RULES_ALL;
     constexpr int TILE = 256 * TILE_EPT;
     const int64_t tiles = (X->cols + TILE - 1) / TILE;
     // Parts of a row.  The card holds `slots` workgroups at a time (registers for four to six per compute unit, LDS for a buffer
     // and the lists' words); a row's parts are chosen so that the rounds of workgroups are full: with r rounds a workgroup
     // walks ceil(tiles / parts) tiles, and beginning and ending a part costs about as much as four more.
     const int64_t lds_bytes = (int64_t)rule_bytes(a, TILE) + (int64_t)sizeof(Buffer<select_room<256>()>) + 256;
-    const int64_t slots = ctx->num_cu * std::min<int64_t>(any ? (bf ? 5 : 4) : 6, 160 * 1024 / lds_bytes);
+    const int64_t slots = ctx->num_cu * std::min<int64_t>(select_waves(bf, set, 256), 160 * 1024 / lds_bytes);
     int64_t per = tiles, least = INT64_MAX;
     for (int64_t r = 1; r <= 8; ++r) {
         const int64_t p = std::max<int64_t>(1, std::min<int64_t>(tiles, slots * r / X->rows)), each = std::max<int64_t>(1, (tiles + p - 1) / p);
@@ -476,13 +488,15 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
     // 256 x 128000 74 / 61; but 64 x 128000 26 / 30, 64 x 30000 with all rules 21 / 23, 2048 x 16000 42 / 83.
     const int64_t wide_tiles = (X->cols + 4 * TILE - 1) / (4 * TILE);
     const double fill = (double)X->rows / ctx->num_cu;
-    const bool wide = parts > 1 && fill <= 1 && (double)wide_tiles <= (any ? 1 : 2) + (any ? 7 : 6) * fill * fill;
+    const bool wide = parts > 1 && fill <= 1 && (double)wide_tiles <= (all ? 1 : 2) + (all ? 7 : 6) * fill * fill;
     auto typed = [&](auto b, auto r) {
         if (wide) return select_launch<b(), r(), 1024>(ctx, X, a, 1, wide_tiles, temperature, k, ids, scores, lse, s);
         return select_launch<b(), r(), 256>(ctx, X, a, parts, per, temperature, k, ids, scores, lse, s);
     };
-    if (bf) return any ? typed(std::true_type{}, std::true_type{}) : typed(std::true_type{}, std::false_type{});
-    return any ? typed(std::false_type{}, std::true_type{}) : typed(std::false_type{}, std::false_type{});
+    auto with = [&](auto r) { return bf ? typed(std::true_type{}, r) : typed(std::false_type{}, r); };
+    if (all) return with(std::integral_constant<RuleSet, RULES_ALL>{});
+    if (set == RULES_HISTORY) return with(std::integral_constant<RuleSet, RULES_HISTORY>{});
+    return with(std::integral_constant<RuleSet, RULES_NONE>{});
 }
 
 }  // namespace als
