@@ -4,12 +4,13 @@
 //
 // few queries    (up to four) the vector units: 32 or 16 codes of an item per lane.  Codes are put into the upper halves of
 //                signed bytes, 16 times their value, and converted to fp32 from there (11 instructions for eight); the queries are
-//                held in fp32, a sixteenth of their value.  Sums over the lanes of an item by lane moves.
+//                held in fp32, a sixteenth of their value (rows with entries beyond 2^64 another 2^-64, which their scores
+//                take back).  Sums over the lanes of an item by lane moves.
 // more           the matrix cores, 32 queries x 32 items x 16 entries an instruction.  Query rows become two fp16 parts,
 //                hi + lo, after a shift by a power of two that brings their largest entry to 2^13 .. 2^14: 22 bits and more of
 //                every entry within 2^-16 of the largest, an absolute error of 2^-39 of the largest below (bf16 queries need
-//                no lo: their 8 bits fit one part down to 2^-31 of the largest).  A wavefront keeps 32 queries' operands in
-//                registers and walks item tiles, so that the codes are the only thing read.
+//                no lo: their 8 bits fit one part down to 2^-31 of the largest).  A workgroup keeps 32 queries' operands in
+//                LDS, its wavefronts walk item tiles with the next tile's codes under way.
 #include <algorithm>
 
 #include "row_piece.h"
@@ -49,16 +50,6 @@ __global__ __launch_bounds__(256, NQ > 2 ? 3 : 4) void scores_few_kernel(const v
     constexpr int W = CPL / 8, NG = CPL > G ? CPL / G : 1, WPG = W / NG;  // words and groups per lane, words per group
     const int lane = threadIdx.x & 63, chunk = lane % LPI;
     const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), waves = (int64_t)gridDim.x * 4;
-    float q[NQ][CPL];
-#pragma unroll
-    for (int r = 0; r < NQ; ++r)
-#pragma unroll
-        for (int p = 0; p < W; ++p) {
-            float x[8];
-            piece_floats<BF_Q>(piece_load<BF_Q>(Q, r * ldq + chunk * CPL + 8 * p), x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) q[r][8 * p + e] = x[e] * 0.0625f;
-        }
     uint32_t next_w[U][W];
     uint32_t next_s[U];
     auto fetch = [&](int64_t i0) {
@@ -80,7 +71,28 @@ __global__ __launch_bounds__(256, NQ > 2 ? 3 : 4) void scores_few_kernel(const v
         }
     };
     int64_t i0 = wave * (IPS * U);
-    if (i0 < n) fetch(i0);
+    if (i0 < n) fetch(i0);  // on its way while the queries are prepared
+    float q[NQ][CPL], back[NQ];
+#pragma unroll
+    for (int r = 0; r < NQ; ++r)
+#pragma unroll
+        for (int p = 0; p < W; ++p) {
+            float x[8];
+            piece_floats<BF_Q>(piece_load<BF_Q>(Q, r * ldq + chunk * CPL + 8 * p), x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[r][8 * p + e] = x[e];
+        }
+#pragma unroll
+    for (int r = 0; r < NQ; ++r) {
+        float top = 0.f;
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) top = fmaxf(top, fabsf(q[r][e]));
+        // a group's sum of such a query could pass fp32's range where its product with the scale does not
+        const bool far = __any(top > 0x1p64f);
+        back[r] = far ? 0x1p64f : 1.f;
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) q[r][e] *= far ? 0x1p-68f : 0x1p-4f;
+    }
     for (; i0 < n; i0 += waves * (IPS * U)) {
         uint32_t w[U][W];
         float s[U][NG];
@@ -128,7 +140,7 @@ __global__ __launch_bounds__(256, NQ > 2 ? 3 : 4) void scores_few_kernel(const v
                 float v = sum[r][t * LPI];
 #pragma unroll
                 for (int c = 1; c < LPI; ++c) v = chunk == c ? sum[r][t * LPI + c] : v;
-                if (item < n) store_elem<BF_S>(S, r * lds + item, v);
+                if (item < n) store_elem<BF_S>(S, r * lds + item, v * back[r]);
             }
         }
     }
@@ -414,8 +426,8 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
     }
 }
 
-// Queries up to which the vector units work; 3 and 4 on them / on the matrix cores: 1M, d = 128, fp32 26 and 32 / 34 us, 3M, d = 64,
-// groups of 16 37 and 43 / 68 us, 1M, d = 16, bf16 8 / 14 us, but 10M, d = 128, bf16 (one part of a query on the matrix cores) 227 and
+// Queries up to which the vector units work; 3 and 4 on them / on the matrix cores: 1M, d = 128, fp32 28 and 34 / 34 us, 3M, d = 64,
+// groups of 16 39 and 46 / 68 us, 1M, d = 16, bf16 8 / 14 us, but 10M, d = 128, bf16 (one part of a query on the matrix cores) 227 and
 // 263 / 229 us.
 template <bool BF_Q, int D> constexpr int scores_few() { return BF_Q && D == 128 ? 2 : 4; }
 

@@ -129,6 +129,21 @@ def test_scores_of_values_that_are_not_finite(ctx, gpu_device, nq):
     assert np.all(np.isfinite(S[1:, ok]))  # the other queries do not see it
 
 
+@pytest.mark.parametrize("nq", [1, 2, 4, 40])
+@pytest.mark.parametrize("dq", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("big,small", [(127, -20), (-100, 100), (60, -60)])
+def test_scores_in_range_of_factors_that_are_not(ctx, gpu_device, nq, dq, big, small):
+    say(f"als_scores: queries times 2^{big}, tables times 2^{small}, nq={nq} {dq}")
+    for d, group in ((16, 16), (64, 32), (128, 128)):
+        T = als.als_quantize(ctx, (init_table(300, d, seed=4, stream=1).clamp(-3, 3) * 2.0 ** small).to(gpu_device), group)
+        Q = (init_table(nq, d, seed=6, stream=2).clamp(-1, 1) * 2.0 ** big).to(dq)
+        assert torch.all(torch.isfinite(Q))
+        S = f64(als.als_scores(ctx, Q.to(gpu_device), T))
+        V, Qh = f64(als.als_dequantize(ctx, T)), f64(Q)
+        bound = (2 * d + 16) * 2.0 ** -24 * (np.abs(Qh) @ np.abs(V).T)
+        assert np.all(np.abs(S - Qh @ V.T) <= bound)
+
+
 def test_parts_of_a_table_are_tables(ctx, gpu_device):
     say("als_scores: ranges of rows, d=16, 128")
     for d, group in ((16, 16), (128, 32), (64, 16)):
