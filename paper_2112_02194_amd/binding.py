@@ -297,6 +297,13 @@ class Rules:
     entries: Optional[Csr] = None
     allowed: Optional[torch.Tensor] = None
 
+    def tensors(self):
+        out = [self.penalties, self.bias, self.allowed]
+        for y in (self.history, self.entries):
+            if y is not None:
+                out += (y.indptr, y.indices, y.values)
+        return out
+
     def c(self, rows: int, cols: int) -> c_als_rules:
         out = c_als_rules()
         out.repetition, out.presence, out.frequency = self.repetition, self.presence, self.frequency
@@ -348,6 +355,13 @@ def _matrix(t: torch.Tensor) -> c_als_matrix:
     return c_als_matrix(t.data_ptr() or None, rows, cols, ld if rows > 1 else max(ld, cols), dt)
 
 
+def _here(ctx: Context, *tensors) -> None:
+    device = ctx.device.index
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("every tensor must be on the context's GPU")
+
+
 def als_quantize(ctx: Context, X: torch.Tensor, group: int = 32, out: Optional[QTable] = None) -> QTable:
     """X in 4 bits an entry, one bf16 scale per ``group`` entries of a row (at most d, so 16 for d = 16)."""
     tx = _table(X)
@@ -358,6 +372,7 @@ def als_quantize(ctx: Context, X: torch.Tensor, group: int = 32, out: Optional[Q
         out = QTable(torch.empty((rows, d // 2), dtype=torch.uint8, device=X.device),
                      torch.empty((rows, d // group), dtype=torch.bfloat16, device=X.device))
     ct = out.c()
+    _here(ctx, X, out.codes, out.scales)
     ctx._check(ctx.lib.als_quantize(ctx.handle, ctypes.byref(tx), ctypes.byref(ct), _stream()))
     return out
 
@@ -366,6 +381,7 @@ def als_dequantize(ctx: Context, T: QTable, out: Optional[torch.Tensor] = None, 
     """The values of T as an ordinary table."""
     X = out if out is not None else torch.empty(T.shape, dtype=dtype, device=T.codes.device)
     ct, tx = T.c(), _table(X)
+    _here(ctx, X, T.codes, T.scales)
     ctx._check(ctx.lib.als_dequantize(ctx.handle, ctypes.byref(ct), ctypes.byref(tx), _stream()))
     return X
 
@@ -375,6 +391,7 @@ def als_scores(ctx: Context, Q: torch.Tensor, T: QTable, out: Optional[torch.Ten
     """Inner products of every row of Q with every row of T -> [Q rows, T rows], fp32 or bf16."""
     S = out if out is not None else torch.empty((Q.shape[0], T.codes.shape[0]), dtype=dtype, device=Q.device)
     tq, ct, cs = _table(Q), T.c(), _matrix(S)
+    _here(ctx, Q, T.codes, T.scales, S)
     ctx._check(ctx.lib.als_scores(ctx.handle, ctypes.byref(tq), ctypes.byref(ct), ctypes.byref(cs), _stream()))
     return S
 
@@ -383,6 +400,7 @@ def als_adjust(ctx: Context, S: torch.Tensor, rules: Rules, out: Optional[torch.
     """S changed by the rules, in place unless ``out`` (of S's shape, fp32 or bf16) is given."""
     Y = out if out is not None else S
     cs, cy, cr = _matrix(S), _matrix(Y), rules.c(*S.shape)
+    _here(ctx, S, Y, *rules.tensors())
     ctx._check(ctx.lib.als_adjust(ctx.handle, ctypes.byref(cs), ctypes.byref(cr), ctypes.byref(cy), _stream()))
     return Y
 
@@ -392,7 +410,11 @@ def als_select(ctx: Context, S: torch.Tensor, k: int, rules: Optional[Rules] = N
 
     ``scores / temperature - lse[:, None]`` are the log-probabilities of the returned items among all of the row."""
     cs = _matrix(S)
-    cr = ctypes.byref(rules.c(*S.shape)) if rules is not None else None
+    cr = None
+    if rules is not None:
+        cr = ctypes.byref(rules.c(*S.shape))
+        _here(ctx, *rules.tensors())
+    _here(ctx, S)
     ids = torch.empty((S.shape[0], max(k, 0)), dtype=torch.int32, device=S.device)
     scores = torch.empty((S.shape[0], max(k, 0)), dtype=torch.float32, device=S.device)
     lse = torch.empty((S.shape[0],), dtype=torch.float32, device=S.device)

@@ -1,5 +1,6 @@
 // C-ABI entry points of libals: argument validation, context and workspace management, and the
 // epoch / loss glue.  All arithmetic of the method lives in the kernel translation units.
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -158,7 +159,7 @@ static als_status check_matrix(als_ctx *ctx, const als_matrix *m, const char *na
     if (m->rows < 0 || m->cols < 0) return fail(ctx, ALS_EINVAL, std::string(name) + ": negative size");
     if (m->cols > INT32_MAX) return fail(ctx, ALS_ESHAPE, std::string(name) + ": item ids must fit int32");
     if (m->ld < m->cols) return fail(ctx, ALS_ESHAPE, std::string(name) + ": ld < cols");
-    if (m->rows > 0 && m->ld > INT64_MAX / 4 / m->rows) return fail(ctx, ALS_ESHAPE, std::string(name) + ": rows * ld is too large");
+    if (m->rows > INT64_MAX / (4 * ALS_TOPK_MAX_K) / std::max<int64_t>(1, m->ld)) return fail(ctx, ALS_ESHAPE, std::string(name) + ": rows * ld is too large");
     if (m->rows > 0 && m->cols > 0 && !m->data) return fail(ctx, ALS_EINVAL, std::string(name) + ": data is null");
     if ((uintptr_t)m->data % elem_size(m->dtype)) return fail(ctx, ALS_ESHAPE, std::string(name) + ": data is not aligned to its elements");
     return ALS_OK;

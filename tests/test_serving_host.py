@@ -47,6 +47,23 @@ def test_scores_matrix_refusals():
         als.als_quantize(None, torch.zeros((4, 16)), 32)
 
 
+class NoCalls:
+    """Context of GPU 0 whose library must not be reached."""
+    device, handle = torch.device("cuda", 0), None
+
+
+def test_tensors_elsewhere_are_refused():
+    T = als.QTable(torch.zeros((5, 16), dtype=torch.uint8), torch.zeros((5, 1), dtype=torch.bfloat16))
+    X, S = torch.zeros((5, 32)), torch.zeros((2, 5))
+    lists = als.Csr(2, 5, torch.zeros(3, dtype=torch.int64), torch.zeros(0, dtype=torch.int32))
+    for call in (lambda c: als.als_quantize(c, X), lambda c: als.als_dequantize(c, T), lambda c: als.als_scores(c, X, T),
+                 lambda c: als.als_adjust(c, S, als.Rules()), lambda c: als.als_select(c, S, 1),
+                 lambda c: als.als_select(c, S, 1, als.Rules(history=lists, bias=torch.zeros(5)))):
+        with pytest.raises(ValueError, match="GPU"):
+            call(NoCalls())
+    assert len(als.Rules(history=lists, entries=lists).tensors()) == 9
+
+
 def test_null_context_is_refused():
     if not os.path.exists(als.LIB_PATH):
         pytest.skip("library not built")
