@@ -11,7 +11,13 @@
 //                bar's loses against the k that are there.  A tile with more candidates than there is room for (an ascending
 //                row) goes in a step at a time with the buffer cut back between: nothing overflows, whatever the order or
 //                the number of equal scores.
-// merge kernel   one workgroup per row: the parts' candidates, and their sums in a fixed order.
+//                Memory bound up to the vector units' share: 512 x 1M bf16 202 us with k = 1 (5.1 TB/s, a copy's rate), 230 with
+//                k = 50 (candidates found and cut back), 265 with every row's history (words cleared and counted a tile; the
+//                vector units at work about 70 % of the time).  Short calls are chains of steps: 1 x 1M 9 us, 64 x 30000 with
+//                all rules 11.
+// merge kernel   one workgroup per row: the parts' candidates, and their sums in a fixed order.  A chain of loads and barriers:
+//                10 us for the 245 parts of 1 x 1M, 12 for 512 rows.  As the last part's work in the select kernel (a count in
+//                device memory, fences) it cost more than the launch: 21 us became 23, 293 became 352.
 #include <algorithm>
 #include <cmath>
 
@@ -468,8 +474,8 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
     const bool bf = X->dtype == ALS_BF16, all = set == RULES_ALL;
     constexpr int TILE = 256 * TILE_EPT;
     const int64_t tiles = (X->cols + TILE - 1) / TILE;
-    // Parts of a row.  The card holds `slots` workgroups at a time (registers for four to six per compute unit, LDS for a buffer
-    // and the lists' words); a row's parts are chosen so that the rounds of workgroups are full: with r rounds a workgroup
+    // Parts of a row.  The card holds `slots` workgroups at a time (select_waves of them per compute unit; LDS for a buffer and
+    // the lists' words); a row's parts are chosen so that the rounds of workgroups are full: with r rounds a workgroup
     // walks ceil(tiles / parts) tiles, and beginning and ending a part costs about as much as four more.
     const int64_t lds_bytes = (int64_t)rule_bytes(a, TILE) + (int64_t)sizeof(Buffer<select_room<256>()>) + 256;
     const int64_t slots = ctx->num_cu * std::min<int64_t>(select_waves(bf, set, 256), 160 * 1024 / lds_bytes);
