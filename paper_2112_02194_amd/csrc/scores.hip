@@ -2,7 +2,7 @@
 //
 // Both kernels form a group's sum of products first and multiply it by the group's scale once.
 //
-// few queries    (up to four) the vector units: 32 or 16 codes of an item per lane.  Codes are put into the upper halves of
+// few queries    (up to two to four) the vector units: 32 or 16 codes of an item per lane.  Codes are put into the upper halves of
 //                signed bytes, 16 times their value, and converted to fp32 from there (11 instructions for eight); the queries are
 //                held in fp32, a sixteenth of their value (rows with entries beyond 2^64 another 2^-64, which their scores
 //                take back).  Sums over the lanes of an item by lane moves.
@@ -147,10 +147,10 @@ __global__ __launch_bounds__(256, NQ > 2 ? 3 : 4) void scores_few_kernel(const v
 }
 
 // ------------------------------------------------------------------------------------------------ matrix cores
-// What bounds it: the write of the scores (512 x 1M, d = 64, bf16: 240 us, 1.0 GB at 4.4 TB/s, all of it written once and the codes read
-// once; a wavefront waits for its stores to leave), for few items the launch and one chain of loads (64 x 30000: 6.5 us).
-// 32 items and queries an instruction: the products of a group are one accumulator of 16 registers, so two item tiles fit
-// beside their sums at three wavefronts per SIMD.
+// What bounds it: the write of the scores (512 x 1M, d = 64, bf16: 213 us, 1.0 GB at 4.8 TB/s, all of it written once and the codes read
+// once), for few items the launch and one chain of loads (64 x 30000: 6.5 us).  Before an item's row was read by one lane, in 16-byte
+// loads, the L1's tags did: loads of 8 bytes in the order of the products took 248 us, 554 instead of 474 with d = 128 in fp32, 193
+// instead of 136 for 100 x 1M, groups of 16.  One item tile after the other: four wavefronts per SIMD have registers.
 //
 // A wavefront's 32 queries (A operand: query = lane % 32) and 32 items a tile (B operand: item = lane % 32).  In step s of group
 // part t (32 entries, or 16 for groups of 16) half h = lane / 32 of the wavefront holds eight entries of the group; which ones
@@ -172,7 +172,7 @@ enum class StoreAs {
 };
 
 template <bool BF_Q, bool BF_S, int D, int G>
-__global__ __launch_bounds__(256, 3)
+__global__ __launch_bounds__(256, 4)
 void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, const uint32_t *__restrict__ codes,
                         const uint16_t *__restrict__ scales, int64_t n, void *__restrict__ S, int64_t lds, StoreAs as, unsigned qgroups,
                         unsigned stretch, unsigned rounds, unsigned units) {
@@ -191,26 +191,15 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
     const int64_t step = 4 * (int64_t)stretch, begin = block * (step * rounds);
     const int64_t first = begin + 4 * (in_block % stretch) + wave, last = std::min(spans, begin + step * rounds);
 
-    uint32_t w[2][T::PARTS][T::STEPS], raw[2][(NS + 1) / 2];
+    // An item's row and scales are read by one lane, 16 bytes at a time: lane <a, h> has item 2 a + h of the round.  compute
+    // exchanges them between the halves of the wavefront, as the products take them.
+    uint32_t w[D / 8], raw[(NS + 1) / 2];
     auto fetch = [&](int64_t span) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const int64_t item = std::min<int64_t>(span * 64 + 2 * a + c, n - 1);
-#pragma unroll
-            for (int t = 0; t < T::PARTS; ++t) {
-                const uint32_t *at = codes + item * (D / 8) + T::word(t, 0, h);
-                if constexpr (T::STEPS == 2) {
-                    const u32x2 v = *(const u32x2 *)at;
-                    w[c][t][0] = v[0];
-                    w[c][t][1] = v[1];
-                } else {
-                    w[c][t][0] = *at;
-                }
-            }
-            const uint16_t *ps = scales + item * NS;
-            if constexpr (NS == 1) raw[c][0] = *ps;
-            else __builtin_memcpy(raw[c], __builtin_assume_aligned(ps, NS < 8 ? 2 * NS : 16), 2 * NS);
-        }
+        const int64_t item = std::min<int64_t>(span * 64 + 2 * a + h, n - 1);
+        __builtin_memcpy(w, __builtin_assume_aligned(codes + item * (D / 8), D < 32 ? 8 : 16), D / 2);
+        const uint16_t *ps = scales + item * NS;
+        if constexpr (NS == 1) raw[0] = *ps;
+        else __builtin_memcpy(raw, __builtin_assume_aligned(ps, NS < 8 ? 2 * NS : 16), 2 * NS);
     };
     if (first < last) fetch(first);  // on its way while the queries are prepared
 
@@ -268,14 +257,9 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
     // Waits for fetch's loads: at the end of a round the compiler knows how many stores came after them and lets those be.
     auto arrived = [&] {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int i = 0; i < D / 8; ++i) asm volatile("" : "+v"(w[i]));
 #pragma unroll
-            for (int t = 0; t < T::PARTS; ++t)
-#pragma unroll
-                for (int s = 0; s < T::STEPS; ++s) asm volatile("" : "+v"(w[c][t][s]));
-#pragma unroll
-            for (int i = 0; i < (NS + 1) / 2; ++i) asm volatile("" : "+v"(raw[c][i]));
-        }
+        for (int i = 0; i < (NS + 1) / 2; ++i) asm volatile("" : "+v"(raw[i]));
     };
 
     float total[2][16];
@@ -288,14 +272,26 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
         // Elsewhere the scales of an item are shifted too, and the results back in one step.
         bool wide = q_wide;
 #pragma unroll
+        for (int t = 0; t < T::PARTS; ++t)
+#pragma unroll
+            for (int s = 0; s < T::STEPS; ++s) {
+                // the upper half's first word against the lower half's second
+                const auto both = __builtin_amdgcn_permlane32_swap(w[T::word(t, s, 0)], w[T::word(t, s, 1)], false, false);
+                cw[0][t][s] = both[0];
+                cw[1][t][s] = both[1];
+            }
+        uint32_t own[2][(NS + 1) / 2];
+#pragma unroll
+        for (int i = 0; i < (NS + 1) / 2; ++i) {
+            const auto both = __builtin_amdgcn_permlane32_swap(raw[i], raw[i], false, false);
+            own[0][i] = both[0];
+            own[1][i] = both[1];
+        }
+#pragma unroll
         for (int c = 0; c < 2; ++c) {
 #pragma unroll
-            for (int t = 0; t < T::PARTS; ++t)
-#pragma unroll
-                for (int s = 0; s < T::STEPS; ++s) cw[c][t][s] = w[c][t][s];
-#pragma unroll
             for (int g = 0; g < NS; ++g) {
-                const uint32_t bits = g & 1 ? raw[c][g / 2] & 0xffff0000u : raw[c][g / 2] << 16, m = bits & 0x7fffffffu;
+                const uint32_t bits = g & 1 ? own[c][g / 2] & 0xffff0000u : own[c][g / 2] << 16, m = bits & 0x7fffffffu;
                 cs[c][g] = __uint_as_float(bits);
                 top[c] = max(top[c], m < 0x7f800000u ? m : 0u);
             }
@@ -314,38 +310,32 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
             }
         }
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 2; ++c) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) total[c][v] = 0.f;
 #pragma unroll
-        for (int t = 0; t < T::PARTS; ++t) {
-            floatx16 acc[2];
+            for (int t = 0; t < T::PARTS; ++t) {
+                floatx16 acc;
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+                for (int v = 0; v < 16; ++v) acc[v] = 0.f;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[c][v] = 0.f;
-#pragma unroll
-            for (int s = 0; s < T::STEPS; ++s) {
-                halfx8 A[NP];
-#pragma unroll
-                for (int p = 0; p < NP; ++p) A[p] = __builtin_bit_cast(halfx8, operand[((t * T::STEPS + s) * NP + p) * 64 + lane]);
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                for (int s = 0; s < T::STEPS; ++s) {
                     halfx2 e[4];
                     unpack8(cw[c][t][s], e);
                     const u32x4 bits = {__builtin_bit_cast(uint32_t, e[0]), __builtin_bit_cast(uint32_t, e[1]),
                                         __builtin_bit_cast(uint32_t, e[2]), __builtin_bit_cast(uint32_t, e[3])};
                     const halfx8 B = __builtin_bit_cast(halfx8, bits);
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A[p], B, acc[c], 0, 0, 0);
+                    for (int p = 0; p < NP; ++p) {
+                        const halfx8 A = __builtin_bit_cast(halfx8, operand[((t * T::STEPS + s) * NP + p) * 64 + lane]);
+                        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, B, acc, 0, 0, 0);
+                    }
                 }
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
                 const float scale = cs[c][t * T::PART / G];
 #pragma unroll
-                for (int v = 0; v < 16; ++v) total[c][v] = fmaf(acc[c][v], scale, total[c][v]);
+                for (int v = 0; v < 16; ++v) total[c][v] = fmaf(acc[v], scale, total[c][v]);
             }
+            asm volatile("" ::: "memory");
         }
         // result v is <query 8 (v / 4) + 4 h + v % 4, item 2 a + c>
         if (wide) {
@@ -431,10 +421,10 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
     }
 }
 
-// Queries up to which the vector units work; 3 and 4 on them / on the matrix cores: 1M, d = 128, fp32 28 and 34 / 34 us, 3M, d = 64,
-// groups of 16 39 and 46 / 68 us, 1M, d = 16, bf16 8 / 14 us, but 10M, d = 128, bf16 (one part of a query on the matrix cores) 227 and
-// 263 / 229 us.
-template <bool BF_Q, int D> constexpr int scores_few() { return BF_Q && D == 128 ? 2 : 4; }
+// Queries up to which the vector units work; on them / on the matrix cores, in us: 3 and 4 x 1M, d = 128,
+// fp32 28 / 31 and 35 / 31; 2 and 3 x 10M, d = 128, bf16 (one part of a query on the matrix cores) 168 / 178 and 227 / 180; 4 x 3M, d = 64,
+// groups of 16 47 / 49; 4 x 1M, d = 16, bf16 8 / 14.
+template <bool BF_Q, int D> constexpr int scores_few() { return D < 128 ? 4 : BF_Q ? 2 : 3; }
 
 template <bool BF_Q, bool BF_S, int D, int G>
 static void scores_typed(const als_ctx *ctx, const als_table *Q, const als_qtable *T, const als_matrix *S, hipStream_t s) {
@@ -448,18 +438,21 @@ static void scores_typed(const als_ctx *ctx, const als_table *Q, const als_qtabl
         };
         if (nq == 1) go(std::integral_constant<int, 1>{});
         else if (nq == 2) go(std::integral_constant<int, 2>{});
-        else if constexpr (scores_few<BF_Q, D>() == 4) {
+        else if constexpr (scores_few<BF_Q, D>() > 2) {
             if (nq == 3) go(std::integral_constant<int, 3>{});
-            else go(std::integral_constant<int, 4>{});
+            else if constexpr (scores_few<BF_Q, D>() > 3) go(std::integral_constant<int, 4>{});
         }
         return;
     }
     const int64_t qgroups = (nq + 31) / 32, spans = (n + 63) / 64;
     // Rounds per wavefront and workgroups side by side, where the table is long enough for 16 wavefronts per compute unit.  What
-    // counts is how close together the writes under way are: 4 x 16, 16 x 16, 16 x 32: 246, 237, 267 us (512 queries x 1M items,
-    // d = 64, bf16), 562, 549, 656 us (d = 128, fp32), with rows at odd places, whose ends share lines, 270, 411, 412 us and 655,
-    // 786, 870 us.  Workgroups of one item stretch and all query groups at one time instead: 424, 898 us.
-    const int64_t rounds = std::max<int64_t>(1, std::min<int64_t>(4, spans * qgroups / ((int64_t)ctx->num_cu * 16)));
+    // counts is how close together the writes under way are, most of all where the rows' pieces of a round do not end with a 128-byte
+    // line, which two wavefronts then write a part of each.  2, 4, 6, 8 rounds of 16 workgroups: whole lines 293, 266, 252, 252 us (512
+    // queries x 1M items, d = 64, bf16) and 514, 484, 474, 479 us (d = 128, fp32), shared lines (1 000 001 items) 262, 322, 368, 386 us
+    // and 533, 645, 691, 717 us; 2 x 32 or 4 x 8 are no better.  Workgroups of one item stretch and all query groups at one time
+    // took 1.6 times as long.
+    const int64_t es = BF_S ? 2 : 4, most = S->ld * es % 128 == 0 && (uintptr_t)S->data % 128 == 0 ? 6 : 2;
+    const int64_t rounds = std::max<int64_t>(1, std::min<int64_t>(most, spans * qgroups / ((int64_t)ctx->num_cu * 16)));
     const int64_t stretch = std::max<int64_t>(1, std::min<int64_t>(16, spans / (32 * rounds)));
     // a buffer's offsets have 32 bits: five rows must fit
     const bool near = S->ld < (int64_t)1 << 27, words = !BF_S || (S->ld % 2 == 0 && (uintptr_t)S->data % 4 == 0);
