@@ -148,9 +148,10 @@ __global__ __launch_bounds__(256, NQ > 2 ? 3 : 4) void scores_few_kernel(const v
 
 // ------------------------------------------------------------------------------------------------ matrix cores
 // What bounds it: the write of the scores (512 x 1M, d = 64, bf16: 213 us, 1.0 GB at 4.8 TB/s, all of it written once, the codes read
-// from memory about twice for 16 groups of queries), for few items the launch and one chain of loads (64 x 30000: 6.5 us).  Before an item's row was read by one lane, in 16-byte
-// loads, the L1's tags did: loads of 8 bytes in the order of the products took 248 us, 554 instead of 474 with d = 128 in fp32, 193
-// instead of 136 for 100 x 1M, groups of 16.  One item tile after the other: four wavefronts per SIMD have registers.
+// from memory about twice for 16 groups of queries), for few items the launch and one chain of loads (64 x 30000: 6.5 us).
+// An item's row is read by one lane in 16-byte loads: with loads of 8 bytes in the order of the products, which touch every line
+// eight times, it took 248 us, 554 instead of 474 with d = 128 in fp32, 193 instead of 136 for 100 x 1M, groups of 16.  The two item
+// tiles of a round follow one another, so that four wavefronts per SIMD have registers.
 //
 // A wavefront's 32 queries (A operand: query = lane % 32) and 32 items a tile (B operand: item = lane % 32).  In step s of group
 // part t (32 entries, or 16 for groups of 16) half h = lane / 32 of the wavefront holds eight entries of the group; which ones

@@ -477,6 +477,40 @@ def test_same_bits_every_time(ctx, gpu_device):
             assert torch.equal(a, b)
 
 
+def test_a_recorded_request_is_answered_as_a_live_one(ctx, gpu_device):
+    say("als_scores, als_adjust, als_select: replayed from a graph")
+    gen = torch.Generator().manual_seed(8)
+    n, nq = 50_001, 6
+    T = als.als_quantize(ctx, torch.randn((n, 64), generator=gen).to(gpu_device))
+    Q = torch.randn((nq, 64), generator=gen).to(gpu_device)
+    rules = to_rules(rules_case(nq, n, 5, "hbem"), nq, n, gpu_device)
+    S, Y = torch.empty((nq, n), device=gpu_device), torch.empty((nq, n), device=gpu_device)
+
+    def request():
+        als.als_scores(ctx, Q, T, out=S)
+        als.als_adjust(ctx, S, rules, out=Y)
+        return als.als_select(ctx, S, 20, rules, 0.9) + als.als_select(ctx, Y, 20)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        request()  # the workspace has its size
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        recorded = request()
+    for _ in range(4):
+        Q.copy_(torch.randn((nq, 64), generator=gen))
+        live = [t.clone() for t in request()] + [Y.clone()]
+        S.zero_()
+        Y.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(list(recorded) + [Y], live):
+            assert torch.equal(a, b)
+        assert torch.equal(recorded[0], recorded[3]) and torch.equal(recorded[1], recorded[4])  # the same rules, before or within
+
+
 def test_the_example_answers_from_4_bits(gpu_device):
     say("examples/serve_4bit.py")
     import importlib.util
