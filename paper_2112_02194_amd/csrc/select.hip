@@ -130,13 +130,16 @@ template <int CAP> struct Buffer {
 
 // Sum of exp(x / temperature) over some x, relative to the largest of them, m (-inf: none).  With c = m * scale as it was rounded
 // (scale = log2(e) / temperature) the sum is s 2^c: an element costs one multiply-add and one exponential, and the rounding
-// of c does no harm, since the same c is added in the end.  Where that product is out of range (scores near the type's
-// limits, infinities) the sum is s exp(m / temperature), its terms are 2^((x - m) scale), 1 for x = m.
+// of c does no harm, since the same c is added in the end.  That holds while it is small: the largest element's own term is
+// 2^(m * scale - c), at most 2^(1/32) up to |c| = 2^20 but beyond fp32's range from 2^31 on.  Above, the sum is
+// s exp(m / temperature), its terms are 2^((x - m) scale), 1 for x = m.  No product is joined with a sum that uses c into one
+// operation: c has to be the same number everywhere.
 struct ExpSum {
     float m = -INFINITY, s = 0.f;
-    static __device__ __forceinline__ bool plain(float m, float scale) { return fabsf(m * scale) < 1e30f; }
+    static __device__ __forceinline__ bool plain(float m, float scale) { return fabsf(m * scale) < 0x1p20f; }
     // what a sum relative to m is multiplied by to be relative to top >= m
     static __device__ __forceinline__ float factor(float m, float top, float scale) {
+#pragma clang fp contract(off)
         return m == top ? 1.f : __builtin_amdgcn_exp2f(plain(m, scale) && plain(top, scale) ? m * scale - top * scale : (m - top) * scale);
     }
     __device__ __forceinline__ void add(float om, float os, float scale) {
@@ -150,6 +153,7 @@ struct ExpSum {
         m = top;
     }
     __device__ __forceinline__ float log(float temperature, float scale) const {
+#pragma clang fp contract(off)
         if (s != s || m == -INFINITY || m == INFINITY) return s != s ? s : m;
         return plain(m, scale) ? (m * scale + log2f(s)) * 0.693147181f : m / temperature + logf(s);
     }

@@ -1,0 +1,76 @@
+"""Answering from trained tables on the GPU where it is easy to go wrong: scores far from zero, shapes that reach the inner loops
+of every kernel, recordings beside live calls of another size.
+
+References are plain 64-bit computations (serving_ref on the CPU; for large shapes elementary torch operations in 64 bits on the
+GPU).  Bounds stand at each test, derived before any run.
+"""
+import numpy as np
+import pytest
+import torch
+
+import serving_ref as ref
+from gpu_util import f64, say
+from paper_2112_02194_amd import binding as als
+from test_gpu_serving import check_selected
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx(gpu_device):
+    c = als.Context(0)
+    yield c
+    c.close()
+
+
+# ------------------------------------------------------------------------------------------------ log-sum-exp
+
+def far_rows(n, kind, gen):
+    """Rows of finite scores, all or some of them far from zero."""
+    x = torch.randn((4, n), generator=gen)
+    if kind == "ordinary":
+        return x
+    if kind.startswith("stretch"):  # a finite number where others would put -inf, in whole stretches, in most places, in all but one
+        value = -float(kind.split()[1])
+        x[0, : n // 2] = value
+        x[1, n // 3:] = value
+        x[2, torch.rand(n, generator=gen) < 0.9] = value
+        x[3, 1:] = value
+        return x
+    size = float(kind)  # scores about that large, a few steps apart: the largest counts, or some of them
+    return torch.tensor(size) * (1 + 2.0 ** -20 * torch.randint(-3, 4, (4, n), generator=gen)) + x
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind,temperature", [
+    ("1e5", 1.0), ("3e6", 1.0), ("-3e6", 1.0), ("2e9", 1.0), ("1e10", 1.0), ("1.1e10", 1.0), ("-1e10", 1.0), ("1e12", 1.0), ("1e20", 1.0),
+    ("-1e20", 1.0), ("1e30", 3.0), ("ordinary", 1e-10), ("ordinary", 1e-6), ("ordinary", 1e30), ("stretch 1e6", 1.0), ("stretch 1e9", 0.1),
+    ("stretch 1e10", 1.0), ("stretch 1e20", 1.0), ("stretch 3e38", 1.0), ("1e7", 1e7)])
+def test_lse_of_scores_far_from_zero(ctx, gpu_device, kind, temperature, dtype):
+    """Bounds: check_selected's, whose terms grow with the scores."""
+    t = float(np.float32(temperature))
+    for n in (1, 3, 700, 5000, 70_001):
+        say(f"als_select 4 x {n}, scores {kind}, temperature {temperature} {dtype}")
+        x = far_rows(n, kind, torch.Generator().manual_seed(n)).to(dtype)
+        got = als.als_select(ctx, x.to(gpu_device), 3, temperature=temperature)
+        torch.cuda.synchronize()
+        check_selected(got, f64(x), 3, t, n)
+
+
+def test_lse_of_biases_and_histories_far_from_zero(ctx, gpu_device):
+    say("als_select 3 x 9000, half the items by a bias of -1e10, penalties of 1e12")
+    gen = torch.Generator().manual_seed(1)
+    n = 9000
+    x = (torch.randn((3, n), generator=gen) * 8).round() / 8
+    bias = torch.where(torch.rand(n, generator=gen) < 0.5, -1e10, 0.0)
+    bias[: n // 3] = -1e10
+    indptr = torch.tensor([0, 300, 300, 320])
+    ids = torch.randint(0, n, (320,), generator=gen).to(torch.int32)
+    history = als.Csr(3, n, indptr.to(gpu_device), ids.to(gpu_device))
+    got = als.als_select(ctx, x.to(gpu_device), 5, als.Rules(history=history, presence=1e12, bias=bias.to(gpu_device)))
+    torch.cuda.synchronize()
+    want, _ = ref.adjust(f64(x), history=(indptr.numpy(), ids.numpy()), presence=float(np.float32(1e12)), bias=bias.numpy())
+    _, _, lse = ref.select(want, 5)
+    top = np.abs(want.max(1))
+    bound = (np.log2(n + 1) + 4) * 2.0 ** -22 + 2.0 ** -22 * (np.abs(lse) + 2 * top)
+    assert np.all(np.abs(f64(got[2]) - lse) <= bound)
