@@ -152,10 +152,13 @@ struct ExpSum {
         s = wave_all(s * factor(m, top, scale), 0.f, [](float a, float b) { return a + b; });
         m = top;
     }
+    // The largest score's part is m / temperature, with one rounding: c has that of scale too, which a score of 5 at a temperature
+    // of 0.01 shows in the fifth decimal of a log-probability (1.3e-4 by c ln 2, 0.5e-4 so).
     __device__ __forceinline__ float log(float temperature, float scale) const {
 #pragma clang fp contract(off)
         if (s != s || m == -INFINITY || m == INFINITY) return s != s ? s : m;
-        return plain(m, scale) ? (m * scale + log2f(s)) * 0.693147181f : m / temperature + logf(s);
+        const float c = m * scale, more = fmaf(m, scale, -c);  // the sum is s 2^c, or (s 2^-more) 2^(m scale)
+        return m / temperature + (plain(m, scale) ? logf(s) - more * 0.693147181f : logf(s));
     }
 };
 

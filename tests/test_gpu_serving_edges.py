@@ -74,3 +74,23 @@ def test_lse_of_biases_and_histories_far_from_zero(ctx, gpu_device):
     top = np.abs(want.max(1))
     bound = (np.log2(n + 1) + 4) * 2.0 ** -22 + 2.0 ** -22 * (np.abs(lse) + 2 * top)
     assert np.all(np.abs(f64(got[2]) - lse) <= bound)
+
+
+@pytest.mark.parametrize("temperature", [3.0, 0.3, 0.037, 0.01, 0.0013, 0.0001])
+def test_lse_is_as_exact_as_its_largest_part(ctx, gpu_device, temperature):
+    """lse = m / t + log(sum): one rounding each of the quotient and of the last sum, halves of a unit of |m / t| and |lse|, and the
+    sum's relative error in units of 2^-24: exponents of the terms, from three roundings of numbers whose mean, weighted by the terms,
+    is at most log2(n), in the terms and again where sums of lanes are joined (3.5 log2(n)); exponentials and their joining of
+    two units (8); at most 20 additions one after the other; the logarithm itself (2 |log sum|)."""
+    n, rows = 1000, 64
+    say(f"als_select {rows} x {n}, temperature {temperature}: distance of lse")
+    t = float(np.float32(temperature))
+    x = torch.randn((rows, n), generator=torch.Generator().manual_seed(7)) * 1.5
+    for scale in (1.0, 1.07, 1.23, 1.37, 1.71, 1.93):
+        y = x * scale
+        _, _, lse = als.als_select(ctx, y.to(gpu_device), 1, temperature=temperature)
+        torch.cuda.synchronize()
+        _, _, want = ref.select(f64(y), 1, t)
+        m = f64(y).max(1) / t
+        bound = 2.0 ** -24 * (np.abs(m) + np.abs(want) + 2 * np.abs(want - m) + 3.5 * np.log2(n) + 28)
+        assert np.all(np.abs(f64(lse) - want) <= bound)
