@@ -246,7 +246,10 @@ als_status als_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rules,
  * ids: device int32 [rows*k], scores: device fp32 [rows*k] (unrounded), row q at q*k; 1 <= k <= ALS_TOPK_MAX_K.
  * lse: device fp32 [rows] or NULL: log(sum_i exp(x_i / temperature)) over all items of the row, with which
  * scores / temperature - lse are the log-probabilities of the returned ones; -inf for a row without a score above
- * -inf, NaN for a row with a NaN that is not masked.  temperature > 0 and finite.  The order of all sums is fixed. */
+ * -inf, NaN for a row with a NaN that is not masked.  temperature > 0 and finite.  The order of all sums is fixed.
+ * The workspace (13 MB) is there from als_create on: the call never allocates, and neither do the four above.  They may
+ * be recorded into a HIP graph from the first call on, and a recording stays valid whatever is called between its replays
+ * (a replay is a call: it must not overlap others on the context). */
 als_status als_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int32_t k,
                       int32_t *ids, float *scores, float *lse, void *stream);
 

@@ -231,6 +231,7 @@ als_status als_create(als_ctx **out, int device) {
     hipDeviceProp_t prop;
     if (st == ALS_OK && hipGetDeviceProperties(&prop, device) == hipSuccess && prop.multiProcessorCount > 0)
         ctx->num_cu = prop.multiProcessorCount;
+    if (st == ALS_OK) st = select_setup(ctx);
     if (st != ALS_OK) {
         als_destroy(ctx);
         return st;

@@ -157,7 +157,7 @@ struct als_ctx {
     als::DevBuf small;          // counters, flags, factor matrices, scalars
     als::DevBuf loss_partials;  // fp64 per-workgroup sums
     als::DevBuf topk_partials;  // top-k: chunk norms, queries left to the scan, chunk maxima per query (or the scan's lists)
-    als::DevBuf select_partials;  // als_select: candidates and exponential sums of every part of a row
+    als::DevBuf select_partials;  // als_select: candidates and exponential sums of every part of a row; one size from als_create on
     als::DevBuf gram_w, gram_h; // fp32 [d*d] Gramians used by als_epoch / als_loss
     int32_t *host_counters = nullptr;  // pinned, 16 ints
     double *host_scalar = nullptr;     // pinned, 2 doubles
@@ -221,6 +221,7 @@ als_status launch_quantize(als_ctx *ctx, const als_table *X, const als_qtable *T
 als_status launch_dequantize(als_ctx *ctx, const als_qtable *T, const als_table *X, hipStream_t s);
 als_status launch_scores(als_ctx *ctx, const als_table *Q, const als_qtable *T, const als_matrix *S, hipStream_t s);
 als_status launch_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rules, const als_matrix *Y, hipStream_t s);
+als_status select_setup(als_ctx *ctx);  // als_select's workspace, once num_cu is known
 als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int k, int32_t *ids,
                          float *scores, float *lse, hipStream_t s);
 als_status launch_copy_probe(als_ctx *ctx, const void *src, void *dst, int64_t bytes, hipStream_t s);

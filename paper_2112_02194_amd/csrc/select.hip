@@ -169,9 +169,14 @@ struct PartSum {
 
 // Wavefronts per SIMD that the registers are bounded for: as many as spill no more than two.  A workgroup of 256 threads has one on
 // each SIMD.
+constexpr int SELECT_MAX_WAVES = 6;
 constexpr int select_waves(bool bf16, RuleSet rules, int threads) {
-    return threads == 1024 ? 4 : rules == RULES_ALL ? (bf16 ? 5 : 4) : rules == RULES_HISTORY && !bf16 ? 5 : 6;
+    return threads == 1024 ? 4 : rules == RULES_ALL ? (bf16 ? 5 : 4) : rules == RULES_HISTORY && !bf16 ? 5 : SELECT_MAX_WAVES;
 }
+// Rounds of workgroups that the parts of all rows may take, and the parts that there can be: the context holds room for as many from
+// its creation on (13 MB), so that no call allocates and a recorded one keeps its address.
+constexpr int SELECT_MAX_ROUNDS = 8;
+static int64_t select_max_parts(const als_ctx *ctx) { return (int64_t)ctx->num_cu * SELECT_MAX_WAVES * SELECT_MAX_ROUNDS; }
 
 // Workgroup (x, y): part x (tiles_per_part tiles) of row y.  With one part a row it writes the answer, otherwise the part's
 // candidates, 0 in the slots that are left, and its exponential sum.
@@ -447,11 +452,8 @@ static als_status select_launch(als_ctx *ctx, const als_matrix *X, const RuleArg
     Cand *cand = nullptr;
     PartSum *sums = nullptr;
     if (parts > 1) {
-        const size_t cand_bytes = (size_t)X->rows * parts * PART_SLOTS * sizeof(Cand);
-        als_status st = ensure(ctx, ctx->select_partials, cand_bytes + (size_t)X->rows * parts * sizeof(PartSum));
-        if (st != ALS_OK) return st;
         cand = (Cand *)ctx->select_partials.p;
-        sums = (PartSum *)((char *)ctx->select_partials.p + cand_bytes);
+        sums = (PartSum *)(cand + select_max_parts(ctx) * PART_SLOTS);
     }
     if (NT == 1024) {  // two lists' words are 128 KB
         static const hipError_t attr = hipFuncSetAttribute((const void *)select_kernel<BF16, RULES, NT>,
@@ -474,6 +476,10 @@ static als_status select_launch(als_ctx *ctx, const als_matrix *X, const RuleArg
     return ALS_OK;
 }
 
+als_status select_setup(als_ctx *ctx) {
+    return ensure(ctx, ctx->select_partials, (size_t)select_max_parts(ctx) * (PART_SLOTS * sizeof(Cand) + sizeof(PartSum)));
+}
+
 als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int k, int32_t *ids,
                          float *scores, float *lse, hipStream_t s) {
     const RuleArgs a = rule_args(rules);
@@ -487,7 +493,7 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
     const int64_t lds_bytes = (int64_t)rule_bytes(a, TILE) + (int64_t)sizeof(Buffer<select_room<256>()>) + 256;
     const int64_t slots = ctx->num_cu * std::min<int64_t>(select_waves(bf, set, 256), 160 * 1024 / lds_bytes);
     int64_t per = tiles, least = INT64_MAX;
-    for (int64_t r = 1; r <= 8; ++r) {
+    for (int64_t r = 1; r <= SELECT_MAX_ROUNDS; ++r) {
         const int64_t p = std::max<int64_t>(1, std::min<int64_t>(tiles, slots * r / X->rows)), each = std::max<int64_t>(1, (tiles + p - 1) / p);
         const int64_t cost = (X->rows * ((tiles + each - 1) / each) + slots - 1) / slots * (each + 4);
         if (cost < least) {

@@ -94,3 +94,48 @@ def test_lse_is_as_exact_as_its_largest_part(ctx, gpu_device, temperature):
         m = f64(y).max(1) / t
         bound = 2.0 ** -24 * (np.abs(m) + np.abs(want) + 2 * np.abs(want - m) + 3.5 * np.log2(n) + 28)
         assert np.all(np.abs(f64(lse) - want) <= bound)
+
+
+# ------------------------------------------------------------------------------------------------ recordings
+
+def test_a_recorded_selection_beside_larger_live_ones(gpu_device):
+    """The workspace of a recording must be the one it was recorded with, whatever is called on the context between its replays: calls
+    with many more parts of rows, of another kernel, for other rows.  The recorded call is the context's first."""
+    say("als_select: recorded as a context's first call, replayed between larger live calls")
+    gen = torch.Generator().manual_seed(11)
+    X = torch.randn((2, 50_001), generator=gen).to(gpu_device)
+    large = [torch.randn(shape, generator=gen).to(gpu_device) for shape in ((1, 3_000_001), (64, 300_000), (300, 30_000), (1500, 9000))]
+    ctx, other = als.Context(0), als.Context(0)
+    want = [als.als_select(other, t, 20, temperature=0.8) for t in large]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        recorded = als.als_select(ctx, X, 20, temperature=0.8)
+    for t, w in zip(large, want):
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(als.als_select(ctx, t, 20, temperature=0.8), w):
+            assert torch.equal(a, b)
+        X.copy_(torch.randn(X.shape, generator=gen))
+        for a in recorded:
+            a.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(recorded, als.als_select(other, X, 20, temperature=0.8)):
+            assert torch.equal(a, b)
+    ctx.close()
+    other.close()
+
+
+def test_selection_allocates_nothing(gpu_device):
+    say("als_select: free memory of the card before and after calls of growing size")
+    ctx = als.Context(0)
+    X = torch.randn((512, 200_000), generator=torch.Generator().manual_seed(1)).to(gpu_device)
+    als.als_select(ctx, X[:1, :100], 5)
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    for rows, cols in ((1, 5000), (1, 200_000), (8, 200_000), (64, 200_000), (512, 200_000)):
+        als.als_select(ctx, X[:rows, :cols], 5)
+        torch.cuda.synchronize()
+    assert free - torch.cuda.mem_get_info()[0] < 1 << 20  # torch's own results fit a block that it has; the old workspace was 10 MB
+    ctx.close()
