@@ -101,7 +101,9 @@ typedef struct als_ctx als_ctx;
 
 /* Create / destroy a context bound to one GPU.  als_create sets that device
  * current for the calling thread.  Workspace grows on demand and is released
- * by als_destroy.  Calls on one context must not overlap. */
+ * by als_destroy; once a call has been recorded into a HIP graph, buffers that later
+ * calls outgrow are kept until then too, so that the recording stays valid.  Calls on
+ * one context, replays of recorded ones among them, must not overlap. */
 als_status als_create(als_ctx **ctx, int device);
 als_status als_destroy(als_ctx *ctx);
 
@@ -248,8 +250,7 @@ als_status als_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rules,
  * scores / temperature - lse are the log-probabilities of the returned ones; -inf for a row without a score above
  * -inf, NaN for a row with a NaN that is not masked.  temperature > 0 and finite.  The order of all sums is fixed.
  * The workspace (13 MB) is there from als_create on: the call never allocates, and neither do the four above.  They may
- * be recorded into a HIP graph from the first call on, and a recording stays valid whatever is called between its replays
- * (a replay is a call: it must not overlap others on the context). */
+ * be recorded into a HIP graph from the first call on. */
 als_status als_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int32_t k,
                       int32_t *ids, float *scores, float *lse, void *stream);
 

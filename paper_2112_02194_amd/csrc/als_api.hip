@@ -22,7 +22,14 @@ als_status fail(als_ctx *ctx, als_status st, const std::string &msg) {
 als_status ensure(als_ctx *ctx, DevBuf &b, size_t bytes) {
     if (bytes <= b.bytes) return ALS_OK;
     if (b.p) {
-        ALS_HIP(ctx, hipFree(b.p));  // hipFree waits for work that may still use the old buffer
+        if (ctx->recorded) {  // a recording may hold its address
+            DevBuf *old = new (std::nothrow) DevBuf(b);
+            if (!old) return fail(ctx, ALS_ENOMEM, "no host memory left");
+            old->next = ctx->outgrown;
+            ctx->outgrown = old;
+        } else {
+            ALS_HIP(ctx, hipFree(b.p));  // hipFree waits for work that may still use the old buffer
+        }
         b.p = nullptr;
         b.bytes = 0;
     }
@@ -35,6 +42,14 @@ als_status ensure(als_ctx *ctx, DevBuf &b, size_t bytes) {
     }
     b.bytes = want;
     return ALS_OK;
+}
+
+// Called by the entry points whose workspace grows: from the first call that is recorded into a graph on, outgrown buffers stay
+// until als_destroy, since a replay writes where the recorded call would have.
+static void note_recording(als_ctx *ctx, void *stream) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing((hipStream_t)stream, &status) != hipSuccess) (void)hipGetLastError();
+    else if (status == hipStreamCaptureStatusActive) ctx->recorded = true;
 }
 
 void timer_begin(als_ctx *ctx, int slot, hipStream_t s) {
@@ -248,6 +263,11 @@ als_status als_destroy(als_ctx *ctx) {
                       &ctx->loss_partials, &ctx->topk_partials, &ctx->select_partials, &ctx->gram_w, &ctx->gram_h};
     for (DevBuf *b : bufs)
         if (b->p) (void)hipFree(b->p);
+    while (DevBuf *b = ctx->outgrown) {
+        ctx->outgrown = b->next;
+        (void)hipFree(b->p);
+        delete b;
+    }
     if (ctx->hint_counts) (void)hipHostFree(ctx->hint_counts);
     if (ctx->host_counters) (void)hipHostFree(ctx->host_counters);
     if (ctx->host_scalar) (void)hipHostFree(ctx->host_scalar);
@@ -263,6 +283,7 @@ als_status als_gramian(als_ctx *ctx, const als_table *V, float *G, void *stream)
     if (st != ALS_OK) return st;
     if (!G) return fail(ctx, ALS_EINVAL, "G is null");
     timers_reset(ctx);
+    note_recording(ctx, stream);
     return launch_gramian(ctx, V, G, (hipStream_t)stream);
 }
 
@@ -293,6 +314,7 @@ als_status als_solve_rows(als_ctx *ctx, const als_csr *Y, const als_table *V, co
     if (st != ALS_OK) return st;
     timers_reset(ctx);
     if (r1 == r0) return ALS_OK;
+    note_recording(ctx, stream);
     return launch_solve_rows(ctx, Y, V, G, prm, X, r0, r1, (hipStream_t)stream);
 }
 
@@ -309,6 +331,7 @@ als_status als_epoch(als_ctx *ctx, const als_csr *Y, const als_csr *Yt, als_tabl
         return fail(ctx, ALS_ESHAPE, "Yt is not shaped as the transpose of Y");
     timers_reset(ctx);
     hipStream_t s = (hipStream_t)stream;
+    note_recording(ctx, stream);
     if ((st = launch_gramian(ctx, H, GH, s)) != ALS_OK) return st;
     if (Y->rows > 0 && (st = launch_solve_rows(ctx, Y, H, GH, prm, W, 0, Y->rows, s)) != ALS_OK) return st;
     if ((st = launch_gramian(ctx, W, GW, s)) != ALS_OK) return st;
@@ -373,6 +396,7 @@ als_status als_topk(als_ctx *ctx, const als_table *Q, const als_table *H, const 
             return fail(ctx, ALS_ESHAPE, "exclude must have one row per query and one column per item");
     }
     if (Q->rows == 0) return ALS_OK;
+    note_recording(ctx, stream);
     return launch_topk(ctx, Q, H, exclude, k, ids, scores, (hipStream_t)stream);
 }
 

@@ -122,6 +122,7 @@ template <bool BF16> __device__ __forceinline__ float load_elem(const void *base
 struct DevBuf {
     void *p = nullptr;
     size_t bytes = 0;
+    DevBuf *next = nullptr;  // outgrown buffers: a list
 };
 
 // One slot per kernel (or pair of kernels timed together); T_DUAL_CLASS0 + c: dual row kernel of the class
@@ -159,6 +160,8 @@ struct als_ctx {
     als::DevBuf topk_partials;  // top-k: chunk norms, queries left to the scan, chunk maxima per query (or the scan's lists)
     als::DevBuf select_partials;  // als_select: candidates and exponential sums of every part of a row; one size from als_create on
     als::DevBuf gram_w, gram_h; // fp32 [d*d] Gramians used by als_epoch / als_loss
+    bool recorded = false;             // a call whose workspace grows was recorded into a graph
+    als::DevBuf *outgrown = nullptr;   // buffers that such a recording may still write to
     int32_t *host_counters = nullptr;  // pinned, 16 ints
     double *host_scalar = nullptr;     // pinned, 2 doubles
     int num_cu = 256;                  // compute units of the device (sizes the default grids)

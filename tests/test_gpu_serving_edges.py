@@ -9,8 +9,9 @@ import pytest
 import torch
 
 import serving_ref as ref
-from gpu_util import f64, say
+from gpu_util import f64, rel_fro, say
 from paper_2112_02194_amd import binding as als
+from synth import make_problem
 from test_gpu_serving import check_selected
 
 pytestmark = pytest.mark.gpu
@@ -139,3 +140,49 @@ def test_selection_allocates_nothing(gpu_device):
         torch.cuda.synchronize()
     assert free - torch.cuda.mem_get_info()[0] < 1 << 20  # torch's own results fit a block that it has; the old workspace was 10 MB
     ctx.close()
+
+
+def test_recordings_of_growing_calls_beside_larger_live_ones(gpu_device):
+    """als_gramian, als_solve_rows, als_topk and als_epoch grow their workspace on demand: a recording keeps the buffers that it holds."""
+    say("als_epoch, als_solve_rows, als_topk: replayed between larger live calls")
+    small, large = make_problem("c1", rows=700, cols=600), make_problem("c1", rows=40_000, cols=30_000)
+    dev, prm = gpu_device, als.make_params(small.alpha, small.lam)
+    ctx, other = als.Context(0), als.Context(0)
+
+    def held(p):
+        Y = als.Csr(p.rows, p.cols, p.indptr.to(dev), p.indices.to(dev))
+        Yt = als.Csr(p.cols, p.rows, p.t_indptr.to(dev), p.t_indices.to(dev))
+        return Y, Yt, p.W0.to(dev), p.H0.to(dev), torch.zeros_like(p.W0, device=dev)
+
+    def step(c, Y, Yt, W, H, X):
+        als.als_epoch(c, Y, Yt, W, H, prm)
+        als.als_solve_rows(c, Y, H, als.als_gramian(c, H), prm, X)
+        return als.als_topk(c, X, H, 10)
+
+    S, L, S2, L2 = held(small), held(large), held(small), held(large)
+    step(ctx, *S)  # the workspace takes this problem's size
+    als.als_status_sync(ctx)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ids, scores = step(ctx, *S)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = step(ctx, *L)  # outgrows it, the first time
+        want = step(other, *L2)
+        torch.cuda.synchronize()
+        assert rel_fro(f64(L[2]), f64(L2[2])) <= 1e-6 and torch.allclose(got[1], want[1], rtol=1e-4, atol=1e-6)
+        for t, p in ((S, small), (S2, small)):
+            t[2].copy_(p.W0)
+            t[3].copy_(p.H0)
+        ids.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        want = step(other, *S2)
+        torch.cuda.synchronize()
+        assert rel_fro(f64(S[2]), f64(S2[2])) <= 1e-6 and rel_fro(f64(S[3]), f64(S2[3])) <= 1e-6  # grids may differ from live calls
+        assert rel_fro(f64(S[4]), f64(S2[4])) <= 1e-6 and torch.allclose(scores, want[1], rtol=1e-4, atol=1e-6)
+        again = als.als_topk(other, S[4], S[3], 10)
+        torch.cuda.synchronize()
+        assert torch.equal(ids, again[0]) and torch.equal(scores, again[1])
+    ctx.close()
+    other.close()
