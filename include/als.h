@@ -215,9 +215,9 @@ als_status als_quantize(als_ctx *ctx, const als_table *X, const als_qtable *T, v
 /* The values of T as an ordinary table (rounded to nearest even where X is bf16); X is written. */
 als_status als_dequantize(als_ctx *ctx, const als_qtable *T, const als_table *X, void *stream);
 
-/* S[q][i] = <Q[q], T[i]> for every row of Q and of T: Q in fp32 or bf16, S in either.  An fp32 query keeps
- * at least 22 bits of every entry within 2^-16 of its row's largest, smaller ones an absolute error of 2^-39 of that;
- * products and sums are fp32, S is rounded once.  S must not overlap Q or T. */
+/* S[q][i] = <Q[q], T[i]> for every row of Q and of T: Q in fp32 or bf16, S in either.  An fp32 query's entries keep at
+ * least 22 bits within 2^-17 of its row's largest and 19 below, a bf16 query's all 8, down to 2^-113 of the largest; products and
+ * sums are fp32, S is rounded once.  S must not overlap Q or T. */
 als_status als_scores(als_ctx *ctx, const als_table *Q, const als_qtable *T, const als_matrix *S, void *stream);
 
 /* Rules that change a score x of row q and item i, in this order, in fp32:

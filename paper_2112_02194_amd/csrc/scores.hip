@@ -6,11 +6,15 @@
 //                signed bytes, 16 times their value, and converted to fp32 from there (11 instructions for eight); the queries are
 //                held in fp32, a sixteenth of their value (rows with entries beyond 2^64 another 2^-64, which their scores
 //                take back).  Sums over the lanes of an item by lane moves.
-// more           the matrix cores, 32 queries x 32 items x 16 entries an instruction.  Query rows become two fp16 parts,
-//                hi + lo, after a shift by a power of two that brings their largest entry to 2^13 .. 2^14: 22 bits and more of
-//                every entry within 2^-16 of the largest, an absolute error of 2^-39 of the largest below (bf16 queries need
-//                no lo: their 8 bits fit one part down to 2^-31 of the largest).  A workgroup keeps 32 queries' operands in
-//                LDS, its wavefronts walk item tiles with the next tile's codes under way.
+// more           the matrix cores, 32 queries x 32 items x 16 entries an instruction.  Query rows become two fp16 parts, hi + lo,
+//                after a shift by a power of two that brings their largest entry to 2^14 .. 2^15: 22 bits and more of every entry within
+//                2^-17 of the largest, 19 within 2^-20 (bf16 queries need no lo: their 8 bits fit one part down to 2^-31 of the
+//                largest).  Where a group of 32 queries has a row with entries below that (not 0), they become bf16 numbers, three
+//                of fp32 and one of bf16, which hold every bit down to 2^-113 of the largest: three products instead of two, six
+//                more instructions to unpack eight codes, and guarded stores.  Of 512 x 1M, d = 128, fp32, all groups so 665 us, none
+//                500; with the bf16 parts for all and the common stores 547, against 478 before there were two forms.  Ordinary
+//                rows of d = 128 have such an entry in one group in a hundred.  A workgroup keeps 32 queries' operands in LDS, its
+//                wavefronts walk item tiles with the next tile's codes under way.
 #include <algorithm>
 
 #include "row_piece.h"
@@ -19,6 +23,7 @@ namespace als {
 
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -36,6 +41,17 @@ __device__ __forceinline__ void unpack8(uint32_t w, halfx2 (&c)[4]) {
     c[1] = put(w, 0x00f000f0u, 0x64806480u) * k2 - k3;
     c[2] = put(v, 0x000f000fu, 0x64086408u) - k1;
     c[3] = put(v, 0x00f000f0u, 0x64806480u) * k2 - k3;
+}
+
+// The eight codes of a word as bf16 numbers times 16, in the order of the entries: signed bytes that hold the codes in their upper halves,
+// converted to fp32, whose upper halves are the bf16 numbers (five significant bits at most).
+__device__ __forceinline__ bf16x8 unpack8_wide(uint32_t w) {
+    const uint32_t even = w << 4 & 0xf0f0f0f0u, odd = w & 0xf0f0f0f0u;
+    u32x4 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        c[i] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(odd >> (8 * i))), __float_as_uint((float)(int8_t)(even >> (8 * i))), 0x07060302u);
+    return __builtin_bit_cast(bf16x8, c);
 }
 
 // ------------------------------------------------------------------------------------------------ few queries
@@ -172,100 +188,56 @@ enum class StoreAs {
     GUARDED  // a branch around every element: the rest
 };
 
-template <bool BF_Q, bool BF_S, int D, int G>
-__global__ __launch_bounds__(256, 4)
-void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, const uint32_t *__restrict__ codes,
-                        const uint16_t *__restrict__ scales, int64_t n, void *__restrict__ S, int64_t lds, StoreAs as, unsigned qgroups,
-                        unsigned stretch, unsigned rounds, unsigned units) {
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef const __attribute__((address_space(3))) u32x4 SharedParts;  // in LDS, also where a pointer to it is kept in a structure
+typedef const __attribute__((address_space(3))) float SharedFloat;
+typedef const __attribute__((address_space(3))) floatx4 SharedFloat4;
+
+// What a wavefront has to know for its rounds.
+struct TileWork {
+    const uint32_t *codes;
+    const uint16_t *scales;
+    int64_t n;
+    void *S;
+    int64_t lds, q0, nq, first, last, step;
+    StoreAs as;
+};
+
+// The rounds of a wavefront, with NP parts of a query entry in fp16, or (SPREAD) in bf16.  Two forms of the whole walk: a choice within a
+// round costs the common one its last registers (512 x 1M, d = 128, fp32 queries, bf16 scores 382 us, so 412), and so does a second
+// form with all ways to store.
+template <bool BF_S, int D, int G, int NP, bool SPREAD> struct TileWalk : TileWork {
     typedef ScoreSteps<D, G> T;
-    constexpr int NP = BF_Q ? 1 : 2, NS = D / G;  // parts of a query entry, scales of an item
-    const int lane = threadIdx.x & 63, a = lane & 31, h = lane >> 5;
-    // Units of work, a workgroup's each: a block of `stretch` x `rounds` x 4 x 64 items is walked by `stretch` workgroups side by side
-    // for one group of 32 queries, then for the next group.  So what is written at one time lies close together in few rows,
-    // and a block's codes are read from the L2 by all but the first group (consecutive workgroups go to different XCDs, which
-    // have an L2 each: every XCD has its own run of units).
-    const unsigned per_xcd = (units + 7) / 8, unit = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= per_xcd || unit >= units) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned block = unit / (qgroups * stretch), in_block = unit % (qgroups * stretch);
-    const int64_t q0 = (int64_t)(in_block / stretch) * 32, spans = (n + 63) / 64;
-    const int64_t step = 4 * (int64_t)stretch, begin = block * (step * rounds);
-    const int64_t first = begin + 4 * (in_block % stretch) + wave, last = std::min(spans, begin + step * rounds);
+    static constexpr int NS = D / G;  // scales of an item
+    SharedParts *operand;             // the queries' parts
+    SharedFloat *back;                // 2^-shift of every row
+    int shift;                        // of row lane % 32
+    bool q_wide;                      // some row's shift is far from 0
+    int lane, a, h;
+    uint32_t w[D / 8], raw[(NS + 1) / 2];
+    __device__ __forceinline__ TileWalk(const TileWork &work, SharedParts *operand, SharedFloat *back)
+        : TileWork(work), operand(operand), back(back), shift(0), q_wide(false), lane(threadIdx.x & 63), a(lane & 31), h(lane >> 5) {}
 
     // An item's row and scales are read by one lane, 16 bytes at a time: lane <a, h> has item 2 a + h of the round.  compute
     // exchanges them between the halves of the wavefront, as the products take them.
-    uint32_t w[D / 8], raw[(NS + 1) / 2];
-    auto fetch = [&](int64_t span) {
+    __device__ __forceinline__ void fetch(int64_t span) {
         const int64_t item = std::min<int64_t>(span * 64 + 2 * a + h, n - 1);
         __builtin_memcpy(w, __builtin_assume_aligned(codes + item * (D / 8), D < 32 ? 8 : 16), D / 2);
         const uint16_t *ps = scales + item * NS;
         if constexpr (NS == 1) raw[0] = *ps;
         else __builtin_memcpy(raw, __builtin_assume_aligned(ps, NS < 8 ? 2 * NS : 16), 2 * NS);
-    };
-    if (first < last) fetch(first);  // on its way while the queries are prepared
-
-    // The queries as operands, in LDS for the four wavefronts (registers for them would halve the wavefronts), shifted so that
-    // the largest finite entry of a row lies in [2^13, 2^14).  Each wavefront makes every fourth step's.
-    constexpr int NSTEP = D / 16, MINE = (NSTEP + 3) / 4;
-    __shared__ u32x4 operand[NSTEP * NP * 64];
-    __shared__ uint32_t row_top[4][32];
-    __shared__ __align__(16) float back[32];  // 2^-shift of every row
-    int shift;
-    {
-        float x[MINE][8];
-        uint32_t top = 0;  // the largest magnitude as bits, which order like the values
-#pragma unroll
-        for (int j = 0; j < MINE; ++j) {
-            const int i = 4 * j + wave;
-            Piece<BF_Q> p = piece_zero<BF_Q>();
-            if (i < NSTEP && q0 + a < nq) p = piece_load<BF_Q>(Q, (q0 + a) * ldq + 8 * T::word(i / T::STEPS, i % T::STEPS, h));
-            piece_floats<BF_Q>(p, x[j]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t m = __float_as_uint(x[j][e]) & 0x7fffffffu;
-                top = max(top, m < 0x7f800000u ? m : 0u);
-            }
-        }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        if (h == 0) row_top[wave][a] = top;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = max(top, row_top[i][a]);
-        shift = top ? 14 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) : 0;
-        if (threadIdx.x < 32) back[a] = ldexpf(1.f, -shift);
-#pragma unroll
-        for (int j = 0; j < MINE; ++j) {
-            const int i = 4 * j + wave;
-            halfx8 hi, lo;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int at = 2 * (e % 4) + e / 4;  // the order in which unpack8 leaves a word's codes
-                const float v = ldexpf(x[j][e], shift);
-                hi[at] = (_Float16)v;
-                const float rest = v - (float)hi[at];  // NaN where v is not finite
-                lo[at] = rest == rest ? (_Float16)rest : (_Float16)0.f;
-            }
-            if (i < NSTEP) {
-                operand[(i * NP) * 64 + lane] = __builtin_bit_cast(u32x4, hi);
-                if constexpr (NP == 2) operand[(i * NP + 1) * 64 + lane] = __builtin_bit_cast(u32x4, lo);
-            }
-        }
-        __syncthreads();
     }
-    const bool q_wide = __any(shift > 60 || shift < -60);
-    if (first >= last) return;
 
     // Waits for fetch's loads: at the end of a round the compiler knows how many stores came after them and lets those be.
-    auto arrived = [&] {
+    __device__ __forceinline__ void arrived() {
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) asm volatile("" : "+v"(w[i]));
 #pragma unroll
         for (int i = 0; i < (NS + 1) / 2; ++i) asm volatile("" : "+v"(raw[i]));
-    };
+    }
 
-    float total[2][16];
     // the round's sums, and the next round's codes on their way
-    auto compute = [&](int64_t next) {
+    __device__ __forceinline__ void compute(int64_t next, float (&total)[2][16]) {
         uint32_t cw[2][T::PARTS][T::STEPS];
         float cs[2][NS];
         uint32_t top[2] = {0, 0};
@@ -321,15 +293,24 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
                 for (int v = 0; v < 16; ++v) acc[v] = 0.f;
 #pragma unroll
                 for (int s = 0; s < T::STEPS; ++s) {
-                    halfx2 e[4];
-                    unpack8(cw[c][t][s], e);
-                    const u32x4 bits = {__builtin_bit_cast(uint32_t, e[0]), __builtin_bit_cast(uint32_t, e[1]),
-                                        __builtin_bit_cast(uint32_t, e[2]), __builtin_bit_cast(uint32_t, e[3])};
-                    const halfx8 B = __builtin_bit_cast(halfx8, bits);
+                    if constexpr (SPREAD) {
+                        const bf16x8 B = unpack8_wide(cw[c][t][s]);
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) {
-                        const halfx8 A = __builtin_bit_cast(halfx8, operand[((t * T::STEPS + s) * NP + p) * 64 + lane]);
-                        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, B, acc, 0, 0, 0);
+                        for (int p = 0; p < NP; ++p) {
+                            const bf16x8 A = __builtin_bit_cast(bf16x8, operand[((t * T::STEPS + s) * NP + p) * 64 + lane]);
+                            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, B, acc, 0, 0, 0);
+                        }
+                    } else {
+                        halfx2 e[4];
+                        unpack8(cw[c][t][s], e);
+                        const u32x4 bits = {__builtin_bit_cast(uint32_t, e[0]), __builtin_bit_cast(uint32_t, e[1]),
+                                            __builtin_bit_cast(uint32_t, e[2]), __builtin_bit_cast(uint32_t, e[3])};
+                        const halfx8 B = __builtin_bit_cast(halfx8, bits);
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) {
+                            const halfx8 A = __builtin_bit_cast(halfx8, operand[((t * T::STEPS + s) * NP + p) * 64 + lane]);
+                            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, B, acc, 0, 0, 0);
+                        }
                     }
                 }
                 const float scale = cs[c][t * T::PART / G];
@@ -349,77 +330,191 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float4 b4 = *(const float4 *)(back + 8 * j + 4 * h);
-                const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+                const floatx4 b4 = *(SharedFloat4 *)(back + 8 * j + 4 * h);
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    total[0][4 * j + v] *= b[v];
-                    total[1][4 * j + v] *= b[v];
+                    total[0][4 * j + v] *= b4[v];
+                    total[1][4 * j + v] *= b4[v];
                 }
             }
         }
-    };
+    }
 
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    typedef float floatx2 __attribute__((ext_vector_type(2)));
-    constexpr int ES = BF_S ? 2 : 4;
-    const int rows = (int)std::min<int64_t>(32, nq - q0);
-    int64_t span = first;
-    const int64_t whole = std::min(last, n / 64);
-    arrived();
-    if (as == StoreAs::BUFFER) {
-        const uint32_t half = (uint32_t)(4 * lds * ES);  // bytes from a row to that of the upper half's lanes
-        const uint32_t place = h * half + a * 2 * ES;
-        for (; span < whole; span += step) {
-            compute(std::min(span + step, last - 1));
-            char *at = (char *)S + (q0 * lds + span * 64) * ES;
+    __device__ __forceinline__ void run() {
+        float total[2][16];
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        typedef float floatx2 __attribute__((ext_vector_type(2)));
+        constexpr int ES = BF_S ? 2 : 4;
+        const int rows = (int)std::min<int64_t>(32, nq - q0);
+        int64_t span = first;
+        const int64_t whole = std::min(last, n / 64);
+        arrived();
+        if (!SPREAD && as == StoreAs::BUFFER) {
+            const uint32_t half = (uint32_t)(4 * lds * ES);  // bytes from a row to that of the upper half's lanes
+            const uint32_t place = h * half + a * 2 * ES;
+            for (; span < whole; span += step) {
+                compute(std::min(span + step, last - 1), total);
+                char *at = (char *)S + (q0 * lds + span * 64) * ES;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int row = 8 * (v >> 2) + (v & 3);  // and row + 4 in the upper half
-                // up to the end of the last of the two that exists
-                const uint32_t bytes = rows > row + 4 ? half + 64 * ES : rows > row ? 64 * ES : 0;
-                const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(at, 0, (int)bytes, 0x00020000);
-                const floatx2 f = {total[0][v], total[1][v]};
-                if constexpr (BF_S) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2)), rsrc, (int)place, 0, 0);
-                else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f), rsrc, (int)place, 0, 0);
-                at += lds * (ES * ((v & 3) == 3 ? 5 : 1));
+                for (int v = 0; v < 16; ++v) {
+                    const int row = 8 * (v >> 2) + (v & 3);  // and row + 4 in the upper half
+                    // up to the end of the last of the two that exists
+                    const uint32_t bytes = rows > row + 4 ? half + 64 * ES : rows > row ? 64 * ES : 0;
+                    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(at, 0, (int)bytes, 0x00020000);
+                    const floatx2 f = {total[0][v], total[1][v]};
+                    if constexpr (BF_S) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2)), rsrc, (int)place, 0, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f), rsrc, (int)place, 0, 0);
+                    at += lds * (ES * ((v & 3) == 3 ? 5 : 1));
+                }
+                arrived();
             }
-            arrived();
+        } else if (!SPREAD && BF_S && as == StoreAs::PLAIN && rows == 32) {
+            for (; span < whole; span += step) {
+                compute(std::min(span + step, last - 1), total);
+                char *at = (char *)S + ((q0 + 4 * h) * lds + span * 64 + 2 * a) * ES;
+                asm volatile("" : "+v"(at));  // sixteen addresses are not kept from round to round
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    typedef uint32_t u32_any __attribute__((aligned(2)));
+                    const floatx2 f = {total[0][v], total[1][v]};
+                    *(u32_any *)at = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+                    at += lds * (ES * ((v & 3) == 3 ? 5 : 1));
+                }
+                arrived();
+            }
         }
-    } else if (BF_S && as == StoreAs::PLAIN && rows == 32) {
-        for (; span < whole; span += step) {
-            compute(std::min(span + step, last - 1));
-            char *at = (char *)S + ((q0 + 4 * h) * lds + span * 64 + 2 * a) * ES;
-            asm volatile("" : "+v"(at));  // sixteen addresses are not kept from round to round
+        for (; span < last; span += step) {
+            compute(std::min(span + step, last - 1), total);
+            const int64_t item = span * 64 + 2 * a;
+            char *at = (char *)S + ((q0 + 4 * h) * lds + item) * ES;
+            asm volatile("" : "+v"(at));
+            const int left = rows - 4 * h;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                typedef uint32_t u32_any __attribute__((aligned(2)));
-                const floatx2 f = {total[0][v], total[1][v]};
-                *(u32_any *)at = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+                if (8 * (v >> 2) + (v & 3) < left) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        if (item + c < n) {
+                            if constexpr (BF_S) ((__bf16 *)at)[c] = (__bf16)total[c][v];
+                            else ((float *)at)[c] = total[c][v];
+                        }
+                }
                 at += lds * (ES * ((v & 3) == 3 ? 5 : 1));
             }
-            arrived();
         }
     }
-    for (; span < last; span += step) {
-        compute(std::min(span + step, last - 1));
-        const int64_t item = span * 64 + 2 * a;
-        char *at = (char *)S + ((q0 + 4 * h) * lds + item) * ES;
-        asm volatile("" : "+v"(at));
-        const int left = rows - 4 * h;
+};
+
+template <bool BF_Q, bool BF_S, int D, int G>
+__global__ __launch_bounds__(256, 4)
+void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, const uint32_t *__restrict__ codes,
+                        const uint16_t *__restrict__ scales, int64_t n, void *__restrict__ S, int64_t lds, StoreAs as, unsigned qgroups,
+                        unsigned stretch, unsigned rounds, unsigned units) {
+    typedef ScoreSteps<D, G> T;
+    constexpr int NP = BF_Q ? 1 : 2, NP_WIDE = BF_Q ? 1 : 3;  // parts of a query entry, in fp16 and in bf16
+    const int lane = threadIdx.x & 63, a = lane & 31, h = lane >> 5;
+    // Units of work, a workgroup's each: a block of `stretch` x `rounds` x 4 x 64 items is walked by `stretch` workgroups side by side
+    // for one group of 32 queries, then for the next group.  So what is written at one time lies close together in few rows,
+    // and a block's codes are read from the L2 by all but the first group (consecutive workgroups go to different XCDs, which
+    // have an L2 each: every XCD has its own run of units).
+    const unsigned per_xcd = (units + 7) / 8, unit = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per_xcd || unit >= units) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned block = unit / (qgroups * stretch), in_block = unit % (qgroups * stretch);
+    const int64_t q0 = (int64_t)(in_block / stretch) * 32, spans = (n + 63) / 64;
+    const int64_t step = 4 * (int64_t)stretch, begin = block * (step * rounds);
+    const int64_t first = begin + 4 * (in_block % stretch) + wave, last = std::min(spans, begin + step * rounds);
+
+    constexpr int NSTEP = D / 16, MINE = (NSTEP + 3) / 4;
+    __shared__ u32x4 operand[NSTEP * NP_WIDE * 64 > NSTEP * NP * 64 ? NSTEP * NP_WIDE * 64 : NSTEP * NP * 64];
+    __shared__ uint2 row_ends[4][32];
+    __shared__ __align__(16) float back[32];  // 2^-shift of every row
+    TileWalk<BF_S, D, G, NP, false> walk({codes, scales, n, S, lds, q0, nq, first, last, step, as}, (SharedParts *)operand, (SharedFloat *)back);
+    if (first < last) walk.fetch(first);  // on its way while the queries are prepared
+
+    // The queries as operands, in LDS for the four wavefronts (registers for them would halve the wavefronts), shifted so that
+    // the largest finite entry of a row lies in [2^14, 2^15).  Each wavefront makes every fourth step's.
+    int shift;
+    bool spread;  // entries of one row too far apart for the fp16 parts
+    {
+        float x[MINE][8];
+        uint32_t top = 0, low = ~0u;  // the largest magnitude and the smallest but 0 as bits, which order like the values; low is one less
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            if (8 * (v >> 2) + (v & 3) < left) {
+        for (int j = 0; j < MINE; ++j) {
+            const int i = 4 * j + wave;
+            Piece<BF_Q> p = piece_zero<BF_Q>();
+            if (i < NSTEP && q0 + a < nq) p = piece_load<BF_Q>(Q, (q0 + a) * ldq + 8 * T::word(i / T::STEPS, i % T::STEPS, h));
+            piece_floats<BF_Q>(p, x[j]);
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (item + c < n) {
-                        if constexpr (BF_S) ((__bf16 *)at)[c] = (__bf16)total[c][v];
-                        else ((float *)at)[c] = total[c][v];
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t m = __float_as_uint(x[j][e]) & 0x7fffffffu;
+                top = max(top, m < 0x7f800000u ? m : 0u);
+                low = min(low, m - 1);
+            }
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        low = min(low, (uint32_t)__shfl_xor((int)low, 32));
+        if (h == 0) row_ends[wave][a] = make_uint2(top, low);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint2 ends = row_ends[i][a];
+            top = max(top, ends.x);
+            low = min(low, ends.y);
+        }
+        shift = top ? 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) : 0;
+        const uint32_t least = __float_as_uint(ldexpf(__uint_as_float(top), BF_Q ? -31 : -20));
+        spread = __any(least > 0 && low < least - 1);
+        if (threadIdx.x < 32) back[a] = ldexpf(1.f, -shift);
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const int i = 4 * j + wave;
+            if (i < NSTEP && spread) {
+                uint32_t part[NP_WIDE][8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float v = ldexpf(x[j][e], shift - 4);  // the codes are times 16
+#pragma unroll
+                    for (int p = 0; p < NP_WIDE; ++p) {
+                        const __bf16 b = (__bf16)v;
+                        part[p][e] = __builtin_bit_cast(uint16_t, b);
+                        const float rest = v - (float)b;  // NaN where v is not finite
+                        v = rest == rest ? rest : 0.f;
                     }
+                }
+#pragma unroll
+                for (int p = 0; p < NP_WIDE; ++p)
+                    operand[(i * NP_WIDE + p) * 64 + lane] = u32x4{part[p][0] | part[p][1] << 16, part[p][2] | part[p][3] << 16,
+                                                                   part[p][4] | part[p][5] << 16, part[p][6] | part[p][7] << 16};
+            } else if (i < NSTEP) {
+                halfx8 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = 2 * (e % 4) + e / 4;  // the order in which unpack8 leaves a word's codes
+                    const float v = ldexpf(x[j][e], shift);
+                    hi[at] = (_Float16)v;
+                    const float rest = v - (float)hi[at];  // NaN where v is not finite
+                    lo[at] = rest == rest ? (_Float16)rest : (_Float16)0.f;
+                }
+                operand[(i * NP) * 64 + lane] = __builtin_bit_cast(u32x4, hi);
+                if constexpr (NP == 2) operand[(i * NP + 1) * 64 + lane] = __builtin_bit_cast(u32x4, lo);
             }
-            at += lds * (ES * ((v & 3) == 3 ? 5 : 1));
         }
+        __syncthreads();
     }
+    if (first >= last) return;
+    const bool q_wide = __any(shift > 60 || shift < -60);
+    if (spread) {
+        TileWalk<BF_S, D, G, NP_WIDE, true> other(walk, walk.operand, walk.back);
+        other.shift = shift;
+        other.q_wide = q_wide;
+        other.fetch(first);
+        other.run();
+        return;
+    }
+    walk.shift = shift;
+    walk.q_wide = q_wide;
+    walk.run();
 }
 
 // Queries up to which the vector units work; on them / on the matrix cores, in us: 3 and 4 x 1M, d = 128,

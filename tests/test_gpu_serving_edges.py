@@ -186,3 +186,66 @@ def test_recordings_of_growing_calls_beside_larger_live_ones(gpu_device):
         assert torch.equal(ids, again[0]) and torch.equal(scores, again[1])
     ctx.close()
     other.close()
+
+
+# ------------------------------------------------------------------------------------------------ scores
+
+def scores_bound(Q, V, d, want, ds):
+    """d fp32 products and their sum in any order, an entry rounded to at least 19 bits (2^-19 = 32 units of 2^-24 where entries are
+    far apart, 4 units elsewhere), a scale: (2 d + 16) 2^-24 sum_j |q_j v_ij| holds for both with d >= 16, since the sum's
+    d units are met by d - 1 additions at most; half an ulp of a bf16 result."""
+    bound = (2 * d + 16) * 2.0 ** -24 * (np.abs(Q) @ np.abs(V).T) + 1e-37
+    return bound if ds == torch.float32 else bound * (1 + 2.0 ** -7) + np.abs(want) * 2.0 ** -8
+
+
+PAIRS = [(16, 16), (32, 16), (32, 32), (64, 16), (64, 32), (64, 64), (128, 16), (128, 32), (128, 64), (128, 128)]
+
+
+@pytest.mark.parametrize("dq", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d,group", PAIRS)
+def test_scores_of_queries_with_entries_far_apart(ctx, gpu_device, d, group, dq):
+    """One large entry in a query's row, in an item whose code there is 0: the score is made of the small ones alone, and has their
+    bits, however many queries there are in the call."""
+    gen = torch.Generator().manual_seed(d + group)
+    n = 700
+    X = torch.randn((n, d), generator=gen)
+    X[: n // 2, d // 3] = 0.0
+    X[n // 2: n // 2 + 9, d // 3 + 1:] = 0.0  # others at the large entry alone, or mixed
+    T = als.als_quantize(ctx, X.to(gpu_device), group)
+    V = f64(als.als_dequantize(ctx, T))
+    for nq in (1, 2, 4, 5, 31, 40, 70):
+        for power in (-10, -16, -19, -20, -21, -30, -33, -40, -60, -100):
+            say(f"als_scores nq={nq} d={d} group={group} {dq}: entries 2^{power} of the largest")
+            Q = torch.randn((nq, d), generator=gen)
+            Q = torch.where(Q.abs() < 0.25, torch.full_like(Q, 0.25), Q) * 2.0 ** power
+            Q[::3, d // 3] = 5.0  # the other rows are ordinary ones
+            if nq > 31:
+                Q[3] *= 1e20  # and one is far from 1
+            Q = Q.to(dq)
+            for ds, pad in ((torch.float32, 0), (torch.bfloat16, 1)):
+                big = torch.full((nq + 1, n + pad), 9.0, dtype=ds, device=gpu_device)
+                als.als_scores(ctx, Q.to(gpu_device), T, out=big[:nq, :n])
+                torch.cuda.synchronize()
+                want = f64(Q) @ V.T
+                assert np.all(np.abs(f64(big[:nq, :n]) - want) <= scores_bound(f64(Q), V, d, want, ds))
+                assert torch.all(big[nq:] == 9.0) and torch.all(big[:, n:] == 9.0)
+
+
+@pytest.mark.parametrize("nq", [1, 5, 40])
+def test_scores_of_infinite_entries_beside_small_ones(ctx, gpu_device, nq):
+    say(f"als_scores: infinite and NaN entries in rows with entries far apart, nq={nq}")
+    d, n = 64, 300
+    gen = torch.Generator().manual_seed(3)
+    T = als.als_quantize(ctx, torch.randn((n, d), generator=gen).to(gpu_device), 32)
+    V = f64(als.als_dequantize(ctx, T))
+    Q = torch.randn((nq, d), generator=gen)
+    Q[:, 7] *= 2.0 ** -60
+    plain = f64(als.als_scores(ctx, Q.to(gpu_device), T))
+    Q[0, 5] = float("inf")
+    S = f64(als.als_scores(ctx, Q.to(gpu_device), T))
+    with np.errstate(all="ignore"):
+        assert np.array_equal(S[0], np.where(V[:, 5] == 0, np.nan, np.inf * V[:, 5]), equal_nan=True)
+    assert np.array_equal(S[1:], plain[1:])
+    Q[0, 5] = float("nan")
+    S = f64(als.als_scores(ctx, Q.to(gpu_device), T))
+    assert np.all(np.isnan(S[0])) and np.array_equal(S[1:], plain[1:])
