@@ -216,7 +216,7 @@ als_status als_quantize(als_ctx *ctx, const als_table *X, const als_qtable *T, v
 als_status als_dequantize(als_ctx *ctx, const als_qtable *T, const als_table *X, void *stream);
 
 /* S[q][i] = <Q[q], T[i]> for every row of Q and of T: Q in fp32 or bf16, S in either.  An fp32 query's entries keep at
- * least 22 bits within 2^-17 of its row's largest and 19 below, a bf16 query's all 8, down to 2^-113 of the largest; products and
+ * least 22 bits within 2^-17 of its row's largest and 19 below, a bf16 query's all 8, down to 2^-100 of the largest; products and
  * sums are fp32, S is rounded once.  S must not overlap Q or T. */
 als_status als_scores(als_ctx *ctx, const als_table *Q, const als_qtable *T, const als_matrix *S, void *stream);
 

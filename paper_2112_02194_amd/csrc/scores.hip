@@ -4,13 +4,13 @@
 //
 // few queries    (up to two to four) the vector units: 32 or 16 codes of an item per lane.  Codes are put into the upper halves of
 //                signed bytes, 16 times their value, and converted to fp32 from there (11 instructions for eight); the queries are
-//                held in fp32, a sixteenth of their value (rows with entries beyond 2^64 another 2^-64, which their scores
-//                take back).  Sums over the lanes of an item by lane moves.
+//                held in fp32, a sixteenth of their value (rows with entries beyond 2^64 another 2^-64, and rows without any beyond
+//                2^-16 their value, which their scores take back).  Sums over the lanes of an item by lane moves.
 // more           the matrix cores, 32 queries x 32 items x 16 entries an instruction.  Query rows become two fp16 parts, hi + lo,
 //                after a shift by a power of two that brings their largest entry to 2^14 .. 2^15: 22 bits and more of every entry within
 //                2^-17 of the largest, 19 within 2^-20 (bf16 queries need no lo: their 8 bits fit one part down to 2^-31 of the
 //                largest).  Where a group of 32 queries has a row with entries below that (not 0), they become bf16 numbers, three
-//                of fp32 and one of bf16, which hold every bit down to 2^-113 of the largest: three products instead of two, six
+//                of fp32 and one of bf16, which hold every bit down to 2^-100 of the largest: three products instead of two, six
 //                more instructions to unpack eight codes, and guarded stores.  Of 512 x 1M, d = 128, fp32, all groups so 665 us, none
 //                500; with the bf16 parts for all and the common stores 547, against 478 before there were two forms.  Ordinary
 //                rows of d = 128 have such an entry in one group in a hundred.  A workgroup keeps 32 queries' operands in LDS, its
@@ -103,11 +103,13 @@ __global__ __launch_bounds__(256, NQ > 2 ? 3 : 4) void scores_few_kernel(const v
         float top = 0.f;
 #pragma unroll
         for (int e = 0; e < CPL; ++e) top = fmaxf(top, fabsf(q[r][e]));
-        // a group's sum of such a query could pass fp32's range where its product with the scale does not
-        const bool far = __any(top > 0x1p64f);
-        back[r] = far ? 0x1p64f : 1.f;
+        // a group's sum of a query with large entries could pass fp32's range where its product with the scale does not; small entries
+        // would leave it, and need no room above: their sums times the largest scale stay 2^3 below its end
+        const bool far = __any(top > 0x1p64f), small = !__any(top > 0x1p-16f);
+        back[r] = far ? 0x1p64f : small ? 0x1p-4f : 1.f;
+        const float by = far ? 0x1p-68f : small ? 1.f : 0x1p-4f;
 #pragma unroll
-        for (int e = 0; e < CPL; ++e) q[r][e] *= far ? 0x1p-68f : 0x1p-4f;
+        for (int e = 0; e < CPL; ++e) q[r][e] *= by;
     }
     for (; i0 < n; i0 += waves * (IPS * U)) {
         uint32_t w[U][W];

@@ -11,7 +11,7 @@ import torch
 import serving_ref as ref
 from gpu_util import f64, rel_fro, say
 from paper_2112_02194_amd import binding as als
-from synth import make_problem
+from synth import init_table, make_problem
 from test_gpu_serving import check_selected
 
 pytestmark = pytest.mark.gpu
@@ -249,3 +249,19 @@ def test_scores_of_infinite_entries_beside_small_ones(ctx, gpu_device, nq):
     Q[0, 5] = float("nan")
     S = f64(als.als_scores(ctx, Q.to(gpu_device), T))
     assert np.all(np.isnan(S[0])) and np.array_equal(S[1:], plain[1:])
+
+
+@pytest.mark.parametrize("nq", [1, 2, 3, 4, 40])
+@pytest.mark.parametrize("dq", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("big,small", [(-124, 100), (-126, 124), (-132, 120), (-16, 120), (-15, 110), (-60, 124)])
+def test_scores_of_queries_near_the_end_of_the_range(ctx, gpu_device, nq, dq, big, small):
+    """Entries at and below the smallest normal number keep the bits that they have: what a query is scaled by may not take them."""
+    say(f"als_scores: queries times 2^{big}, tables times 2^{small}, nq={nq} {dq}")
+    for d, group in ((16, 16), (32, 32), (64, 32), (128, 128)):
+        T = als.als_quantize(ctx, (init_table(300, d, seed=4, stream=1).clamp(-3, 3) * 2.0 ** small).to(gpu_device), group)
+        Q = (init_table(nq, d, seed=6, stream=2).clamp(-1, 1) * 2.0 ** big).to(dq)
+        S = f64(als.als_scores(ctx, Q.to(gpu_device), T))
+        V, Qh = f64(als.als_dequantize(ctx, T)), f64(Q)
+        assert np.all(np.isfinite(V))
+        want = Qh @ V.T
+        assert np.all(np.abs(S - want) <= scores_bound(Qh, V, d, want, torch.float32))
