@@ -12,7 +12,7 @@ import serving_ref as ref
 from gpu_util import f64, rel_fro, say
 from paper_2112_02194_amd import binding as als
 from synth import init_table, make_problem
-from test_gpu_serving import check_selected
+from test_gpu_serving import check_selected, to_ref, to_rules
 
 pytestmark = pytest.mark.gpu
 
@@ -265,3 +265,156 @@ def test_scores_of_queries_near_the_end_of_the_range(ctx, gpu_device, nq, dq, bi
         assert np.all(np.isfinite(V))
         want = Qh @ V.T
         assert np.all(np.abs(S - want) <= scores_bound(Qh, V, d, want, torch.float32))
+
+
+# ------------------------------------------------------------------------------------------------ shapes that reach the inner loops
+
+def close_on_gpu(S, Q, T, ctx, ds):
+    """scores_bound on the GPU, a million items at a time."""
+    d, Qd = Q.shape[1], Q.double()
+    for i in range(0, S.shape[1], 1 << 20):
+        part = als.QTable(T.codes[i:i + (1 << 20)], T.scales[i:i + (1 << 20)])
+        Vt = als.als_dequantize(ctx, part).double().T.contiguous()
+        want = Qd @ Vt
+        bound = (2 * d + 16) * 2.0 ** -24 * (Qd.abs() @ Vt.abs()) + 1e-37
+        if ds == torch.bfloat16:
+            bound = bound * (1 + 2.0 ** -7) + want.abs() * 2.0 ** -8
+        if not bool(((S[:, i:i + (1 << 20)].double() - want).abs() <= bound).all()):
+            return False
+    return True
+
+
+def random_table(n, d, group, gen, dev):
+    codes = torch.randint(0, 256, (n, d // 2), dtype=torch.uint8, device=dev, generator=gen)
+    return als.QTable(codes, (0.02 * torch.rand((n, d // group), device=dev, generator=gen) + 0.001).to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("dq", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("ds", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d,group", PAIRS)
+def test_scores_over_several_rounds(ctx, gpu_device, d, group, dq, ds):
+    """500 queries against enough items that a wavefront walks six rounds (rows of whole 128-byte lines) or two (rows that share
+    lines; bf16 rows of odd length take the form without a bounds check), the last ones not whole."""
+    gen = torch.Generator(device=gpu_device).manual_seed(d + group)
+    for n, ld in ((98_560, 98_560), (98_501, 98_560), (98_501, 98_501), (98_502, 98_502)):
+        say(f"als_scores 500 x {n} (rows of {ld}) d={d} group={group} {dq} -> {ds}")
+        T = random_table(n, d, group, gen, gpu_device)
+        Q = torch.randn((500, d), device=gpu_device, generator=gen)
+        Q = torch.where(Q.abs() < 1e-4, torch.full_like(Q, 1e-4), Q).to(dq)
+        if n != 98_560:
+            Q[65, 3] = 1e-12  # one group of queries in the form for entries far apart
+        big = torch.full((501, ld), 9.0, dtype=ds, device=gpu_device)
+        als.als_scores(ctx, Q, T, out=big[:500, :n])
+        torch.cuda.synchronize()
+        assert close_on_gpu(big[:500, :n], Q, T, ctx, ds)
+        assert bool((big[500] == 9.0).all()) and bool((big[:500, n:] == 9.0).all())
+        del big
+
+
+@pytest.mark.parametrize("ds", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d,group,n", [(16, 16, 4_500_001), (32, 16, 4_500_001), (32, 32, 4_500_001), (64, 16, 2_300_003), (64, 64, 2_300_003),
+                                       (128, 16, 1_300_007), (128, 32, 1_300_007), (128, 128, 1_300_007)])
+def test_scores_of_few_queries_over_several_rounds(ctx, gpu_device, d, group, n, ds):
+    gen = torch.Generator(device=gpu_device).manual_seed(d + group)
+    T = random_table(n, d, group, gen, gpu_device)
+    for nq, dq in ((1, torch.float32), (2, torch.bfloat16), (3, torch.float32), (4, torch.float32), (4, torch.bfloat16)):
+        say(f"als_scores {nq} x {n} d={d} group={group} {dq} -> {ds}")
+        Q = torch.randn((nq, d), device=gpu_device, generator=gen).to(dq)
+        S = als.als_scores(ctx, Q, T, dtype=ds)
+        torch.cuda.synchronize()
+        assert close_on_gpu(S, Q, T, ctx, ds)
+
+
+@pytest.mark.parametrize("rows,d,group,dtype", [(600_001, 128, 32, torch.float32), (1_100_003, 128, 128, torch.bfloat16), (4_300_001, 16, 16, torch.float32)])
+def test_quantize_of_more_rows_than_a_grid_takes_at_once(ctx, gpu_device, rows, d, group, dtype):
+    """Parts of the table, each of one turn of the grid, have the same bits as the whole, and some rows at every turn's ends those of
+    the definition."""
+    say(f"als_quantize, als_dequantize {rows} x {d} groups of {group} {dtype}")
+    gen = torch.Generator(device=gpu_device).manual_seed(5)
+    X = (torch.randn((rows, d), device=gpu_device, generator=gen) * torch.exp(torch.randn((rows, 1), device=gpu_device, generator=gen))).to(dtype)
+    T = als.als_quantize(ctx, X, group)
+    back = als.als_dequantize(ctx, T)
+    half = als.als_dequantize(ctx, T, dtype=torch.bfloat16)
+    torch.cuda.synchronize()
+    turn = 16_384 * 1024 // (d // (4 if dtype == torch.float32 else 8))
+    step = turn // 2 + 3
+    for i in range(0, rows, step):
+        P = als.als_quantize(ctx, X[i:i + step], group)
+        assert torch.equal(P.codes, T.codes[i:i + step]) and torch.equal(P.scales, T.scales[i:i + step])
+        assert torch.equal(als.als_dequantize(ctx, P), back[i:i + step])
+        assert torch.equal(als.als_dequantize(ctx, P, dtype=torch.bfloat16), half[i:i + step])
+    for i in (0, turn - 700, rows - 700):
+        code, scale = ref.quantize(X[i:i + 700].float().cpu().numpy(), group)
+        assert np.array_equal(T.codes[i:i + 700].cpu().numpy(), ref.pack(code))
+        assert np.array_equal(f64(T.scales[i:i + 700]), scale.astype(np.float64))
+        assert np.array_equal(f64(back[i:i + 700]), ref.values(code, scale))
+
+
+def lists_of_lengths(rows, cols, lengths, gen, values):
+    n = torch.tensor([lengths[q % len(lengths)] for q in range(rows)])
+    indptr = torch.zeros(rows + 1, dtype=torch.int64)
+    indptr[1:] = torch.cumsum(n, 0)
+    total = int(indptr[-1])
+    ids = (torch.rand(total, generator=gen) ** 2 * cols).to(torch.int32)
+    return indptr, ids, (torch.randn(total, generator=gen) * 8).round() / 8 if values else None
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,k", [(128, 30_000, 20), (256, 60_000, 64), (200, 33_001, 1)])
+def test_select_by_one_large_workgroup_per_row_with_every_rule(ctx, gpu_device, rows, cols, k, dtype):
+    """Rows that take several tiles of the kernel with 1024 threads, lists that a wavefront holds and lists that are walked, of both
+    kinds in every combination; the rules' arithmetic is exact, so ids and scores have to be equal."""
+    say(f"als_select {rows} x {cols} every rule, k={k} {dtype}")
+    gen = torch.Generator().manual_seed(rows)
+    X = ((torch.randn((rows, cols), generator=gen) * 24).round() / 8).to(dtype)
+    kw = dict(history=lists_of_lengths(rows, cols, (0, 3, 255, 256, 257, 900, 5000), gen, False), penalties=torch.tensor([[2.0, 0.5, 0.25], [0.5, 0.0, 0.125]])[torch.arange(rows) % 2],
+              entries=lists_of_lengths(rows, cols, (700, 0, 257, 20, 256), gen, True), bias=(torch.randn(cols, generator=gen) * 8).round() / 8,
+              allowed=torch.randint(-2 ** 31, 2 ** 31, (rows, (cols + 31) // 32), generator=gen).to(torch.int32))
+    kw["allowed"][rows // 2] = 0
+    kw["allowed"][3, : cols // 32 - 3] = 0  # the last items alone
+    want, _ = ref.adjust(f64(X), **to_ref(kw))
+    got = als.als_select(ctx, X.to(gpu_device), k, to_rules(kw, rows, cols, gpu_device), 0.5)
+    torch.cuda.synchronize()
+    check_selected(got, want, k, 0.5, cols)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(4, 20_011), (256, 60_000), (600, 40_001)])
+def test_select_by_every_kernel_whatever_the_order(ctx, gpu_device, rows, cols, dtype):
+    """Ascending, descending and equal scores, one row of each kind after the other, with histories and without: more candidates than
+    a tile's buffer holds, cut back between its steps."""
+    gen = torch.Generator().manual_seed(cols)
+    base = torch.arange(cols, dtype=torch.float32)
+    kinds = [base / 8, -base, torch.full((cols,), 2.0), base % 97, -(base // 4096)]
+    X = torch.stack([kinds[q % 5] for q in range(rows)]).to(dtype)
+    history = lists_of_lengths(rows, cols, (0, 3, 255, 300), gen, False)
+    kw = dict(history=history, repetition=2.0, presence=0.25, frequency=0.125)
+    some = sorted({0, 1, 2, 3, 4, rows // 2, rows - 1} & set(range(rows)))  # rows that are checked one by one
+    cut = (torch.cat([torch.zeros(1, dtype=torch.int64), torch.cumsum(torch.tensor([int(history[0][q + 1] - history[0][q]) for q in some]), 0)]),
+           torch.cat([history[1][history[0][q]:history[0][q + 1]] for q in some]), None)
+    for k in (1, 64):
+        say(f"als_select {rows} x {cols} ordered and equal scores, k={k} {dtype}")
+        plain = als.als_select(ctx, X.to(gpu_device), k)
+        ruled = als.als_select(ctx, X.to(gpu_device), k, to_rules(kw, rows, cols, gpu_device))
+        torch.cuda.synchronize()
+        check_selected([t[some] for t in plain], f64(X[some]), k, 1.0, cols)
+        want, _ = ref.adjust(f64(X[some]), **to_ref({**kw, "history": cut}))
+        # bf16 scores with a quarter or an eighth taken off are exact in fp32, so are fp32 ones up to 60 000 / 8
+        check_selected([t[some] for t in ruled], want, k, 1.0, cols)
+        for kind in range(min(5, rows)):  # without rules all rows of a kind have one answer
+            for t in plain:
+                assert bool((t[kind::5] == t[kind]).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_select_of_one_long_row_with_equal_and_ordered_scores(ctx, gpu_device, dtype):
+    """Hundreds of parts that all reach the best score: more candidates than the merge holds at a time."""
+    n = 3_000_001
+    base = torch.arange(n, dtype=torch.float32)
+    for name, x in (("equal", torch.zeros(n)), ("ascending", base / 8), ("descending", -base), ("few values", base % 3)):
+        x = x.to(dtype)[None, :]
+        for k in (1, 64):
+            say(f"als_select 1 x {n}, {name}, k={k} {dtype}")
+            got = als.als_select(ctx, x.to(gpu_device), k, temperature=4.0)
+            torch.cuda.synchronize()
+            check_selected(got, f64(x), k, 4.0, n)
