@@ -440,7 +440,10 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
     bool spread;  // entries of one row too far apart for the fp16 parts
     {
         float x[MINE][8];
-        uint32_t top = 0, low = ~0u;  // the largest magnitude and the smallest but 0 as bits, which order like the values; low is one less
+        // The largest finite magnitude and the smallest but 0 as bits, which order like the values: top is NONE + 2 * magnitude, where
+        // infinities and NaN wrap around to less than NONE, low is 2 * magnitude - 1, where they and 0 come out above all others.
+        constexpr uint32_t NONE = 0x01000000u;
+        uint32_t top = NONE, low = ~0u;
 #pragma unroll
         for (int j = 0; j < MINE; ++j) {
             const int i = 4 * j + wave;
@@ -449,9 +452,9 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
             piece_floats<BF_Q>(p, x[j]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const uint32_t m = __float_as_uint(x[j][e]) & 0x7fffffffu;
-                top = max(top, m < 0x7f800000u ? m : 0u);
-                low = min(low, m - 1);
+                const uint32_t m = (__float_as_uint(x[j][e]) << 1) + NONE;
+                top = max(top, m);
+                low = min(low, m - (NONE + 1));
             }
         }
         top = max(top, (uint32_t)__shfl_xor((int)top, 32));
@@ -464,8 +467,9 @@ void scores_tile_kernel(const void *__restrict__ Q, int64_t ldq, int64_t nq, con
             top = max(top, ends.x);
             low = min(low, ends.y);
         }
-        shift = top ? 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) : 0;
-        const uint32_t least = __float_as_uint(ldexpf(__uint_as_float(top), BF_Q ? -31 : -20));
+        const float largest = __uint_as_float((top - NONE) >> 1);
+        shift = top > NONE ? 15 - __builtin_amdgcn_frexp_expf(largest) : 0;
+        const uint32_t least = 2 * __float_as_uint(ldexpf(largest, BF_Q ? -31 : -20));
         spread = __any(least > 0 && low < least - 1);
         if (threadIdx.x < 32) back[a] = ldexpf(1.f, -shift);
 #pragma unroll
