@@ -227,7 +227,8 @@ als_status als_scores(als_ctx *ctx, const als_table *Q, const als_qtable *T, con
  *   entries    x = x + the value that row q of `entries` stores for item i (the last one where there are several;
  *              1 without values)
  *   allowed    x = -inf where bit i % 32 of word i / 32 of row q is clear, whatever x is (NaN too)
- * Every pointer may be NULL: no such rule.  Item ids outside 0 .. cols-1 in `history` and `entries` are passed over. */
+ * Every pointer may be NULL: no such rule.  Item ids outside 0 .. cols-1 in `history` and `entries` are passed over, and so is what
+ * one row of them holds beyond 2^31 - 2^14 ids. */
 typedef struct {
     const als_csr *history; /* rows and cols as the scores' */
     const als_csr *entries; /* the same */

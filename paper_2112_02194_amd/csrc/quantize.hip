@@ -1,7 +1,10 @@
 // Tables in 4 bits an entry with one bf16 scale per group of entries (als_quantize, als_dequantize).
 //
-// Bound by memory: one read and one write of everything.  A lane owns 16 bytes of the table, four or eight consecutive entries,
-// so that a wavefront moves 1 KB in one piece; the lanes of a group share its largest magnitude by lane moves.
+// One read and one write of everything.  A lane owns 16 bytes of the table, four or eight consecutive entries, so that a wavefront
+// moves 1 KB in one piece; the lanes of a group share its largest magnitude by lane moves.  Reading back is bound by memory (10M x 128
+// to fp32 1.32 ms, 4.4 TB/s, to bf16 0.62 ms, 5.3 TB/s), quantizing by the vector units: 35 instructions an entry of
+// fp32, 26 of bf16, at work 96 and 85 % of the time (10M x 128 fp32 1.26 ms, 4.6 TB/s; 1M x 64 bf16 54 us, 3.0 TB/s, where memory would
+// need 33).
 #include <algorithm>
 
 #include "row_piece.h"

@@ -5,7 +5,8 @@
 // often it occurs (history) or tells where it is stored last (entries); integer atomics, so the order does not matter.
 //   short lists (up to LIST_REGS per lane): every wavefront holds the row's whole list in registers and enters the items that
 //                its own elements cover, so that a tile needs no barrier, and none of this where the list has no item in it
-//   long lists   the workgroup walks the list together, once per tile
+//   long lists   the workgroup walks the list together, once per tile: the list times the row's tiles (als_select of 64 x 128000 with
+//                250, 257 and 4000 ids a row: 28, 30 and 34 us)
 #pragma once
 
 #include <algorithm>

@@ -11,9 +11,9 @@
 //                2^-17 of the largest, 19 within 2^-20 (bf16 queries need no lo: their 8 bits fit one part down to 2^-31 of the
 //                largest).  Where a group of 32 queries has a row with entries below that (not 0), they become bf16 numbers, three
 //                of fp32 and one of bf16, which hold every bit down to 2^-100 of the largest: three products instead of two, six
-//                more instructions to unpack eight codes, and guarded stores.  Of 512 x 1M, d = 128, fp32, all groups so 665 us, none
-//                500; with the bf16 parts for all and the common stores 547, against 478 before there were two forms.  Ordinary
-//                rows of d = 128 have such an entry in one group in a hundred.  A workgroup keeps 32 queries' operands in LDS, its
+//                more instructions to unpack eight codes, and guarded stores.  512 x 1M, d = 128, fp32 scores of fp32 queries: 655 us
+//                with such a row in every group, 486 with none; bf16 of bf16 423 and 329; the bf16 parts and the common stores for
+//                all 547, where the fp16 parts for all took 478.  Ordinary rows of d = 128 make it one group in a hundred.  A workgroup keeps 32 queries' operands in LDS, its
 //                wavefronts walk item tiles with the next tile's codes under way.
 #include <algorithm>
 
@@ -27,7 +27,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// The eight codes of a word as fp16 numbers, exactly: element e of the word is c[e % 4][e / 4].  A code plus 8 put into the low
+// The eight codes of a word as fp16 numbers, exactly (the well-known conversion of small integers through the mantissa of a large
+// power of two): element e of the word is c[e % 4][e / 4].  A code plus 8 put into the low
 // bits of 1024's mantissa is the number 1024 + code + 8, from which a packed subtraction takes 1032; nibbles four bits further
 // up come out times 16 and take a packed multiply-add instead: nine instructions.  (w & mask) ^ bits is one of them: the exclusive
 // or turns two's complement into code + 8 beside filling in the exponent.
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(256, NQ > 2 ? 3 : 4) void scores_few_kernel(const v
 #pragma unroll
         for (int e = 0; e < CPL; ++e) top = fmaxf(top, fabsf(q[r][e]));
         // a group's sum of a query with large entries could pass fp32's range where its product with the scale does not; small entries
-        // would leave it, and need no room above: their sums times the largest scale stay 2^3 below its end
+        // would leave it, and need no room above: their sums times the largest scale stay within it
         const bool far = __any(top > 0x1p64f), small = !__any(top > 0x1p-16f);
         back[r] = far ? 0x1p64f : small ? 0x1p-4f : 1.f;
         const float by = far ? 0x1p-68f : small ? 1.f : 0x1p-4f;
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(256, NQ > 2 ? 3 : 4) void scores_few_kernel(const v
 }
 
 // ------------------------------------------------------------------------------------------------ matrix cores
-// What bounds it: the write of the scores (512 x 1M, d = 64, bf16: 213 us, 1.0 GB at 4.8 TB/s, all of it written once, the codes read
+// What bounds it: the write of the scores (512 x 1M, d = 64, bf16: 216 us, 1.0 GB at 4.7 TB/s, all of it written once, the codes read
 // from memory about twice for 16 groups of queries), for few items the launch and one chain of loads (64 x 30000: 6.5 us).
 // An item's row is read by one lane in 16-byte loads: with loads of 8 bytes in the order of the products, which touch every line
 // eight times, it took 248 us, 554 instead of 474 with d = 128 in fp32, 193 instead of 136 for 100 x 1M, groups of 16.  The two item

@@ -504,7 +504,8 @@ als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rul
     const int64_t parts = std::max<int64_t>(1, (tiles + per - 1) / std::max<int64_t>(1, per));
     // One workgroup of 1024 threads per row where a row is short and the rows do not fill the card: no parts to merge.  With parts /
     // so, in us, k = 50: 1 x 16000 17 / 14, 64 x 30000 17 / 15, 256 x 128000 42 / 34, with lists, biases and sets 64 x 16000 21 / 18,
-    // 256 x 128000 74 / 61; but 64 x 128000 26 / 30, 64 x 30000 with all rules 21 / 23, 2048 x 16000 42 / 83.
+    // 256 x 128000 74 / 61; but 64 x 128000 26 / 30, 64 x 30000 with all rules 21 / 23, 2048 x 16000 42 / 83.  The curve is laid through
+    // these; between a quarter of the card and all of it nothing was measured.
     const int64_t wide_tiles = (X->cols + 4 * TILE - 1) / (4 * TILE);
     const double fill = (double)X->rows / ctx->num_cu;
     const bool wide = parts > 1 && fill <= 1 && (double)wide_tiles <= (all ? 1 : 2) + (all ? 7 : 6) * fill * fill;
