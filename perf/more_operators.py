@@ -299,8 +299,7 @@ def _plain_back(state):
     first = torch.zeros((indptr.numel() - 1, x.shape[1]), device=DEV) if state["first"] is None else state["first"].float()
     before = state["h"].float().roll(1, 0)
     before[starts] = first[some]
-    b = state["d_states"].float()
-    b[ends] += state["d_last"].float()[some]
+    b = state["d_states"].float().index_add(0, ends, state["d_last"].float()[some])
     a = keep.roll(-1, 0)  # of the next entry
     a[ends] = 0.0
     delta = _plain_scan(a.flip(0), b.flip(0), state["longest"]).flip(0)
