@@ -255,6 +255,92 @@ als_status als_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rules,
 als_status als_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int32_t k,
                       int32_t *ids, float *scores, float *lse, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Ordered histories: queries from histories whose order counts, their gradients, answers of several items one after the
+ * other.  Everything below is asynchronous on `stream`, allocates nothing and may be recorded into a HIP graph from the
+ * first call on.  The order of all sums is fixed.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/* A gated linear recurrence over the entries of every row of Y, in their stored order and for each of the d columns:
+ *     h_t = s_t h_{t-1} + (1 - s_t) V[i_t],    s_t = 1 / (1 + exp(-F[i_t])),    i_t the column id of entry t,
+ * from h_0 = the row of H0, or zeros where H0 is NULL.  V (values) and F (gates) have Y->cols rows, the same d and type;
+ * Y's values are not read.  Y->indices may be NULL: entry p of Y then takes row p of V and F (Y->nnz <= Y->cols).
+ * An entry whose id is outside 0 .. cols-1 leaves the state as it is (padding, say).
+ *   states  NULL, or the state after each entry: Y->nnz rows in Y's order
+ *   last    NULL, or the state after the last entry: Y->rows rows, a row's h_0 where it has no entry
+ * H0, states and last are in fp32 or bf16 each; states are fp32 within the call and are rounded where they are written.
+ * Rows of states that belong to no row of Y (before indptr[0], behind indptr[rows]) are left as they are. */
+als_status als_recur(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
+                     const als_table *states, const als_table *last, void *stream);
+
+/* One more entry for each row of X:  X[r] = s H[p] + (1 - s) V[i],  s from F[i],  i = items[r],  p = parents[r], or r where
+ * parents is NULL (X and H then have the same rows, and X may be H itself: same data, ld and type; otherwise they must
+ * not overlap).  items, parents: device [X->rows].  An item outside 0 .. V->rows-1 leaves the state as it is; a parent outside
+ * 0 .. H->rows-1 stands for a state of zeros. */
+als_status als_recur_step(als_ctx *ctx, const int32_t *items, const int32_t *parents, const als_table *V, const als_table *F,
+                          const als_table *H, const als_table *X, void *stream);
+
+/* Gradients of als_recur from those of its outputs.  With g_t = d_states[t] + s_{t+1} g_{t+1} (of a row's last entry
+ * d_states[t] + d_last[row]):
+ *     dV[t] = (1 - s_t) g_t,    dF[t] = g_t (h_{t-1} - V[i_t]) s_t (1 - s_t),    dH0[row] = s_1 g_1 (d_last[row] of a row without entries)
+ * states are those that als_recur gave, d_states and d_last NULL or theirs (one of them at least); H0 as it was given.
+ * dV and dF have a row per entry, zeros where its id is outside the tables; the tables' own gradients are sums of these over the
+ * entries with the same id (als_sum_rows).  dH0: NULL, or Y->rows rows.  states, d_states, dV and dF have one type; H0, d_last and
+ * dH0 may have either.  Rows of dV and dF that belong to no row of Y are left as they are. */
+als_status als_recur_backward(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
+                              const als_table *states, const als_table *d_states, const als_table *d_last,
+                              const als_table *dV, const als_table *dF, const als_table *dH0, void *stream);
+
+/* X[u] = sum over the entries of row u of Y:  y_ui E[i]  (y = 1 where Y has no values): the sum of a history's vectors, or, with
+ * Y the lists of the entries that store an item, an item table's gradient from those of the entries.  E has Y->cols rows, X
+ * Y->rows, in fp32 or bf16 each; sums are fp32, in a fixed order.  Entries with an id outside 0 .. cols-1 are passed over. */
+als_status als_sum_rows(als_ctx *ctx, const als_csr *Y, const als_table *E, const als_table *X, void *stream);
+
+/* norm = sqrt(sum of the squares of all elements of X[0 .. n-1]), squares and sums in fp64, to `norm` (device fp64 [1]);
+ * then Y[j] = X[j] * c, c = bound / norm where norm is above `bound` and finite, otherwise c = 1: tensors
+ * with an infinity or NaN are left as they are, and norm tells.  c is rounded to fp32 (below 2^-100 it is kept in fp64), each product to fp32 and then to its tensor's type.
+ * X, Y: host arrays of n matrices; Y may be NULL (in place), Y[j] may be X[j]; otherwise outputs overlap neither each other nor X
+ * (a matrix reaches from its first element to its last: two that lie between each other's rows do overlap).
+ * Y[j] has X[j]'s shape and type; cols may be any.  bound >= 0; +inf: the norm alone where Y is NULL.  n <= ALS_CLIP_MAX. */
+#define ALS_CLIP_MAX 65536
+als_status als_clip(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, int32_t n, double bound, double *norm, void *stream);
+
+/* Beam search: the best continuations of groups of beams from each beam's best items (als_select on the rows of all beams).
+ * Row r = g * beams + b is beam b of group g.  A candidate of row r and place j (0 .. k-1) is
+ *     total = totals[r] + (scores[r][j] / temperature - lse[r])      item = ids[r][j]
+ * in fp32, one rounding each; with totals NULL (the first step) 0 for the first beam of a group, and the others have no candidate.
+ * Where last is given and last[r] == end, the beam has ended: its only candidate is itself, with its total and the item `end`.
+ * An id below 0 and a total that is -inf or NaN are no candidates.  A group's candidates are ordered by total, or, with `factors`, by
+ * total * factors[length] (the last factor for longer ones; -inf and NaN are no candidates), equal ones by row and place; length =
+ * lengths[r] + 1, lengths[r] of a beam that has ended.  The first `beams` of them become the group's beams, best first.
+ * parents: device int32, the row each beam continues; items, totals, lengths (may be NULL): device, of the new beams.
+ * Where a group has fewer candidates, the rest have parent -1, item -1, total -inf and length 0.
+ * The best continuations of all are among these if k >= beams. */
+typedef struct {
+    int64_t groups;
+    int32_t beams, k;      /* 1 .. ALS_TOPK_MAX_K each */
+    const int32_t *ids;    /* device [groups * beams][k] */
+    const float *scores;   /* device [groups * beams][k] */
+    const float *lse;      /* device [groups * beams], or NULL: zeros */
+    const float *totals;   /* device [groups * beams], or NULL */
+    const int32_t *last;   /* device [groups * beams], or NULL: no beam has ended */
+    const int32_t *lengths; /* device [groups * beams], or NULL: zeros */
+    const float *factors;  /* device [n_factors], or NULL */
+    int32_t n_factors;
+    int32_t end;
+    float temperature;     /* > 0 and finite */
+} als_beams;
+als_status als_beam(als_ctx *ctx, const als_beams *in, int32_t *parents, int32_t *items, float *totals, int32_t *lengths,
+                    void *stream);
+
+/* What goes with the beams in their new order: Y[j] row r = X[j] row parents[r], for n matrices of groups * beams rows each, whose
+ * elements are moved as they are.  A parent outside r's own group stands for a row of zeros.  X, Y: host arrays; Y may be
+ * NULL and Y[j] may be X[j] (in place); otherwise outputs overlap neither each other nor X, as for als_clip.  Y[j] has X[j]'s shape and
+ * type.  parents: device [groups * beams], in no output.  n <= ALS_REORDER_MAX. */
+#define ALS_REORDER_MAX 64
+als_status als_reorder(als_ctx *ctx, const int32_t *parents, int64_t groups, int32_t beams, const als_matrix *X,
+                       const als_matrix *Y, int32_t n, void *stream);
+
 /* Synchronise `stream` and report (then clear) the device-side error flag. */
 als_status als_status_sync(als_ctx *ctx, void *stream);
 

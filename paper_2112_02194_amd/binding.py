@@ -25,7 +25,8 @@ SOLVER_DIRECT, SOLVER_CG, SOLVER_CG_FREE = 0, 1, 2
 EXPORTS = ["als_create", "als_destroy", "als_gramian", "als_solve_rows", "als_epoch", "als_loss",
            "als_status_sync", "als_check_csr", "als_copy_probe", "als_set_timing", "als_get_timing",
            "als_strerror", "als_last_error", "als_gramian_static", "als_static_last_error", "als_topk",
-           "als_quantize", "als_dequantize", "als_scores", "als_adjust", "als_select"]
+           "als_quantize", "als_dequantize", "als_scores", "als_adjust", "als_select",
+           "als_recur", "als_recur_step", "als_recur_backward", "als_sum_rows", "als_clip", "als_beam", "als_reorder"]
 
 
 class c_als_csr(ctypes.Structure):
@@ -58,6 +59,13 @@ class c_als_rules(ctypes.Structure):
     _fields_ = [("history", ctypes.c_void_p), ("entries", ctypes.c_void_p), ("bias", ctypes.c_void_p),  # the lists: to c_als_csr
                 ("allowed", ctypes.c_void_p), ("allowed_ld", ctypes.c_int64), ("penalties", ctypes.c_void_p),
                 ("repetition", ctypes.c_float), ("presence", ctypes.c_float), ("frequency", ctypes.c_float)]
+
+
+class c_als_beams(ctypes.Structure):
+    _fields_ = [("groups", ctypes.c_int64), ("beams", ctypes.c_int32), ("k", ctypes.c_int32), ("ids", ctypes.c_void_p),
+                ("scores", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("totals", ctypes.c_void_p), ("last", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("factors", ctypes.c_void_p), ("n_factors", ctypes.c_int32), ("end", ctypes.c_int32),
+                ("temperature", ctypes.c_float)]
 
 
 class AlsError(RuntimeError):
@@ -105,7 +113,14 @@ def load_library(path: str = LIB_PATH):
     lib.als_scores.argtypes = [vp, P(c_als_table), P(c_als_qtable), P(c_als_matrix), vp]
     lib.als_adjust.argtypes = [vp, P(c_als_matrix), P(c_als_rules), P(c_als_matrix), vp]
     lib.als_select.argtypes = [vp, P(c_als_matrix), P(c_als_rules), ctypes.c_float, i32, vp, vp, vp, vp]
-    for name in ("als_quantize", "als_dequantize", "als_scores", "als_adjust", "als_select"):
+    lib.als_recur.argtypes = [vp, P(c_als_csr), P(c_als_table), P(c_als_table), P(c_als_table), P(c_als_table), P(c_als_table), vp]
+    lib.als_recur_step.argtypes = [vp, vp, vp, P(c_als_table), P(c_als_table), P(c_als_table), P(c_als_table), vp]
+    lib.als_recur_backward.argtypes = [vp, P(c_als_csr)] + [P(c_als_table)] * 9 + [vp]
+    lib.als_sum_rows.argtypes = [vp, P(c_als_csr), P(c_als_table), P(c_als_table), vp]
+    lib.als_clip.argtypes = [vp, vp, vp, i32, ctypes.c_double, vp, vp]
+    lib.als_beam.argtypes = [vp, P(c_als_beams), vp, vp, vp, vp, vp]
+    lib.als_reorder.argtypes = [vp, vp, i64, i32, P(c_als_matrix), P(c_als_matrix), i32, vp]
+    for name in EXPORTS[16:]:
         getattr(lib, name).restype = i32
     lib.als_static_last_error.argtypes = []
     lib.als_static_last_error.restype = ctypes.c_char_p
@@ -115,19 +130,23 @@ def load_library(path: str = LIB_PATH):
 
 @dataclass
 class Csr:
-    """CSR matrix on the GPU: int64 indptr [rows+1], int32 indices [nnz], optional fp32 values."""
+    """CSR matrix on the GPU: int64 indptr [rows+1], int32 indices [nnz], optional fp32 values.  ``indices`` may be None for
+    als_recur and als_recur_backward: an entry for each of the ``cols`` table rows, in their order."""
     rows: int
     cols: int
     indptr: torch.Tensor
-    indices: torch.Tensor
+    indices: Optional[torch.Tensor]
     values: Optional[torch.Tensor] = None
 
     @property
     def nnz(self) -> int:
-        return int(self.indices.numel())
+        return self.cols if self.indices is None else int(self.indices.numel())
 
     def c(self) -> c_als_csr:
         indptr, indices, values = self.indptr, self.indices, self.values
+        if indices is None:
+            assert indptr.dtype is torch.int64 and indptr.is_contiguous() and indptr.numel() == self.rows + 1 and values is None
+            return c_als_csr(self.rows, self.cols, self.cols, indptr.data_ptr(), None, None)
         nnz, vals = indices.numel(), None
         assert indptr.dtype is torch.int64 and indices.dtype is torch.int32
         assert indptr.is_contiguous() and indices.is_contiguous()
@@ -143,7 +162,7 @@ def _table(t: torch.Tensor) -> c_als_table:
     if t.dim() != 2:
         raise ValueError("table must be 2-D with unit column stride")
     rows, d = t.shape
-    ld, unit = t.stride()
+    ld, unit = t.stride() if rows else (d, 1)
     if unit != 1:
         raise ValueError("table must be 2-D with unit column stride")
     dtype = t.dtype
@@ -428,6 +447,194 @@ def als_select(ctx: Context, S: torch.Tensor, k: int, rules: Optional[Rules] = N
     ctx._check(ctx.lib.als_select(ctx.handle, ctypes.byref(cs), cr, temperature, k, ids.data_ptr(), scores.data_ptr(),
                                   lse.data_ptr(), _stream()))
     return ids, scores, lse
+
+
+def _opt(t: Optional[torch.Tensor]):
+    """A table that may be left out, as an argument."""
+    return None if t is None else ctypes.byref(_table(t))
+
+
+def _ids(t: Optional[torch.Tensor], rows: int, name: str):
+    """Address of int32 [rows], one after the other."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != rows or not t.is_contiguous():
+        raise ValueError(name + " must be contiguous int32, one per row")
+    return t.data_ptr() or None
+
+
+def als_recur(ctx: Context, Y: Csr, V: torch.Tensor, F: torch.Tensor, H0: Optional[torch.Tensor] = None, all_states: bool = False,
+              dtype: torch.dtype = torch.float32, last: Optional[torch.Tensor] = None, states: Optional[torch.Tensor] = None):
+    """h = s h + (1 - s) V[item], s = sigmoid(F[item]), over every row's entries in their order -> (last, states or None).
+
+    ``last`` [Y.rows, d]: each row's last state; ``states`` [Y.nnz, d]: the state after each entry, where ``all_states`` or a
+    tensor for them is given.  Tensors that are given are written, others are made in ``dtype``.  Y.indices None: entry p takes row p."""
+    d = V.shape[1]
+    if last is None:
+        last = torch.empty((Y.rows, d), dtype=dtype, device=V.device)
+    if states is None and all_states:
+        states = torch.empty((Y.nnz, d), dtype=dtype, device=V.device)
+    cy, tv, tf, tl = Y.c(), _table(V), _table(F), _table(last)
+    _here(ctx, V, F, H0, last, states, Y.indptr, Y.indices)
+    ctx._check(ctx.lib.als_recur(ctx.handle, ctypes.byref(cy), ctypes.byref(tv), ctypes.byref(tf), _opt(H0), _opt(states),
+                                 ctypes.byref(tl), _stream()))
+    return last, states
+
+
+def als_recur_step(ctx: Context, items: torch.Tensor, V: torch.Tensor, F: torch.Tensor, H: torch.Tensor,
+                   parents: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One more entry for each row: s H[parent] + (1 - s) V[item].  ``out`` may be H where there are no parents."""
+    rows = items.shape[0]
+    X = out if out is not None else torch.empty((rows, H.shape[1]), dtype=H.dtype, device=H.device)
+    if X.shape[0] != rows:
+        raise ValueError("out must have one row per item")
+    tv, tf, th, tx = _table(V), _table(F), _table(H), _table(X)
+    _here(ctx, items, V, F, H, parents, X)
+    ctx._check(ctx.lib.als_recur_step(ctx.handle, _ids(items, rows, "items"), _ids(parents, rows, "parents"), ctypes.byref(tv),
+                                      ctypes.byref(tf), ctypes.byref(th), ctypes.byref(tx), _stream()))
+    return X
+
+
+def als_recur_backward(ctx: Context, Y: Csr, V: torch.Tensor, F: torch.Tensor, states: torch.Tensor,
+                       d_states: Optional[torch.Tensor] = None, d_last: Optional[torch.Tensor] = None, H0: Optional[torch.Tensor] = None,
+                       dtype: Optional[torch.dtype] = None, out=None):
+    """Gradients of als_recur -> (dV [nnz, d], dF [nnz, d], dH0 [rows, d] or None without H0), the first two a row per entry,
+    of the states' type: als_sum_rows over the entries with the same item gives the tables'.  ``out``: the three to write."""
+    dtype = states.dtype if dtype is None else dtype
+    if out is not None:
+        dV, dF, dH0 = out
+    else:
+        dV, dF = (torch.empty(states.shape, dtype=dtype, device=V.device) for _ in range(2))
+        dH0 = None if H0 is None else torch.empty((Y.rows, V.shape[1]), dtype=dtype, device=V.device)
+    cy, tv, tf, ts, tdv, tdf = Y.c(), _table(V), _table(F), _table(states), _table(dV), _table(dF)
+    _here(ctx, V, F, states, d_states, d_last, H0, dV, dF, dH0, Y.indptr, Y.indices)
+    ctx._check(ctx.lib.als_recur_backward(ctx.handle, ctypes.byref(cy), ctypes.byref(tv), ctypes.byref(tf), _opt(H0), ctypes.byref(ts),
+                                          _opt(d_states), _opt(d_last), ctypes.byref(tdv), ctypes.byref(tdf), _opt(dH0), _stream()))
+    return dV, dF, dH0
+
+
+def als_sum_rows(ctx: Context, Y: Csr, E: torch.Tensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """Sum of the rows of E that each row of Y stores, times Y's values -> [Y.rows, d]."""
+    X = out if out is not None else torch.empty((Y.rows, E.shape[1]), dtype=dtype, device=E.device)
+    cy, te, tx = Y.c(), _table(E), _table(X)
+    _here(ctx, E, X, Y.indptr, Y.indices, Y.values)
+    ctx._check(ctx.lib.als_sum_rows(ctx.handle, ctypes.byref(cy), ctypes.byref(te), ctypes.byref(tx), _stream()))
+    return X
+
+
+_CODES = {torch.float32: ALS_F32, torch.bfloat16: ALS_BF16}
+
+
+def _values_of(device: int, tensors, flat: bool):
+    """Tensors as an array of c_als_matrix (five 64-bit words each): one row where ``flat``, otherwise 2-D with unit column stride."""
+    words = []
+    for t in tensors:
+        code = _CODES.get(t.dtype)
+        if code is None:
+            raise TypeError("tensors must be float32 or bfloat16")
+        if t.get_device() != device:
+            raise ValueError("every tensor must be on the context's GPU")
+        if flat:
+            n = t.numel()
+            words += (t.data_ptr(), 1, n, n, code)
+        else:
+            m = _matrix(t)
+            words += (m.data or 0, m.rows, m.cols, m.ld, code)
+    return (ctypes.c_int64 * len(words))(*words)
+
+
+def als_clip(ctx: Context, tensors, bound: float, out=None) -> torch.Tensor:
+    """The norm over all elements of all tensors (float64, on the GPU); the tensors are scaled by bound / norm where that is
+    below 1, in place or into ``out`` (a tensor for each).  Tensors of any shape whose elements lie one after the other, or 2-D
+    ones with unit column stride."""
+    n, device = len(tensors), ctx.device.index
+    flat = all([t.is_contiguous() for t in tensors])
+    Y = None
+    if out is not None:
+        if len(out) != n or any([x.shape != y.shape for x, y in zip(tensors, out)]):
+            raise ValueError("out must have a tensor of the same shape for each")
+        flat = flat and all([t.is_contiguous() for t in out])
+    if not flat:  # those whose elements lie one after the other as one row
+        lone = [x.is_contiguous() and (out is None or out[j].is_contiguous()) for j, x in enumerate(tensors)]
+        tensors = [x.view(1, -1) if f else x for x, f in zip(tensors, lone)]
+        out = out and [y.view(1, -1) if f else y for y, f in zip(out, lone)]
+    X = _values_of(device, tensors, flat)
+    if out is not None:
+        Y = _values_of(device, out, flat)
+    norm = torch.empty((), dtype=torch.float64, device=ctx.device)
+    ctx._check(ctx.lib.als_clip(ctx.handle, X, Y, n, bound, norm.data_ptr(), _stream()))
+    return norm
+
+
+def _per_row(t: Optional[torch.Tensor], rows: int, dtype: torch.dtype, name: str):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != rows or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype}, one per beam")
+    return t.data_ptr() or None
+
+
+def als_beam(ctx: Context, ids: torch.Tensor, scores: torch.Tensor, lse: Optional[torch.Tensor], totals: Optional[torch.Tensor], beams: int,
+             temperature: float = 1.0, last: Optional[torch.Tensor] = None, end: int = -1, lengths: Optional[torch.Tensor] = None,
+             factors: Optional[torch.Tensor] = None):
+    """The best ``beams`` continuations of each group of ``beams`` rows, from the rows' best items as als_select returns them ->
+    (parents int32, items int32, totals fp32, lengths int32), one per beam, a group's best first.
+
+    totals + scores / temperature - lse orders them (times ``factors``[length] where given; None for ``totals``: the first step, a
+    group's first row alone counts).  ``last``: each beam's last item; a beam whose last is ``end`` stays as it is."""
+    rows, k = ids.shape
+    if beams < 1 or rows % beams:
+        raise ValueError("rows must be a whole number of groups of beams")
+    if ids.dtype is not torch.int32 or scores.dtype is not torch.float32 or scores.shape != ids.shape:
+        raise ValueError("ids must be int32 [rows, k] and scores float32 of the same shape")
+    if not ids.is_contiguous() or not scores.is_contiguous():
+        raise ValueError("ids and scores must be contiguous")
+    if factors is not None and (factors.dtype is not torch.float32 or factors.dim() != 1 or not factors.is_contiguous() or not factors.numel()):
+        raise ValueError("factors must be contiguous float32, one at least")
+    c = c_als_beams(rows // beams, beams, k, ids.data_ptr() or None, scores.data_ptr() or None, _per_row(lse, rows, torch.float32, "lse"),
+                    _per_row(totals, rows, torch.float32, "totals"), _per_row(last, rows, torch.int32, "last"),
+                    _per_row(lengths, rows, torch.int32, "lengths"), None if factors is None else factors.data_ptr(),
+                    0 if factors is None else factors.numel(), end, temperature)
+    _here(ctx, ids, scores, lse, totals, last, lengths, factors)
+    parents, items, new_lengths = torch.empty((3, rows), dtype=torch.int32, device=ids.device).unbind()
+    new_totals = torch.empty(rows, dtype=torch.float32, device=ids.device)
+    ctx._check(ctx.lib.als_beam(ctx.handle, ctypes.byref(c), parents.data_ptr(), items.data_ptr(), new_totals.data_ptr(),
+                                new_lengths.data_ptr(), _stream()))
+    return parents, items, new_totals, new_lengths
+
+
+def _state(t: torch.Tensor, rows: int) -> c_als_matrix:
+    """What goes with the beams: a row each, its elements one after the other."""
+    if t.dim() < 1 or t.shape[0] != rows:
+        raise ValueError("a state must have one row per beam")
+    es, cols = t.element_size(), 1
+    for size, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size != 1 and step != cols:
+            raise ValueError("the elements of a state's row must lie one after the other")
+        cols *= size
+    ld = t.stride(0) if rows > 1 else cols
+    if es not in (2, 4, 8):
+        raise TypeError("elements of a state must have 2, 4 or 8 bytes")
+    more = 2 if es == 8 else 1
+    return c_als_matrix(t.data_ptr() or None, rows, cols * more, max(ld, cols) * more if rows <= 1 else ld * more, ALS_BF16 if es == 2 else ALS_F32)
+
+
+def als_reorder(ctx: Context, parents: torch.Tensor, beams: int, states, out=None):
+    """Row parents[r] of every state to row r, in place or into ``out`` (a tensor for each); elements of 2, 4 or 8 bytes of any kind.
+    Rows of parents outside r's own group of ``beams`` rows (-1, say) become zeros."""
+    rows, n = parents.shape[0], len(states)
+    if beams < 1 or rows % beams:
+        raise ValueError("rows must be a whole number of groups of beams")
+    X = (c_als_matrix * n)(*[_state(t, rows) for t in states])
+    Y = None
+    if out is not None:
+        if len(out) != n or any(x.shape != y.shape or x.dtype != y.dtype for x, y in zip(states, out)):
+            raise ValueError("out must have a tensor of the same shape and type for each")
+        Y = (c_als_matrix * n)(*[_state(t, rows) for t in out])
+        _here(ctx, *out)
+    _here(ctx, parents, *states)
+    ctx._check(ctx.lib.als_reorder(ctx.handle, _ids(parents, rows, "parents"), rows // beams, beams, X, Y, n, _stream()))
+    return states if out is None else out
 
 
 def als_status_sync(ctx: Context) -> None:

@@ -33,6 +33,10 @@ UNITS = [
     ("scores.hip", "scores", VGPR_FORM),
     ("adjust.hip", "adjust", []),
     ("select.hip", "select", []),
+    ("recur.hip", "recur", []),
+    ("sum_rows.hip", "sum_rows", []),
+    ("clip.hip", "clip", []),
+    ("beam.hip", "beam", []),
     ("cg_free.hip", "cg_free", []),
     ("dual_prepare.hip", "dual_prepare", []),
     ("dual_rows.hip", "dual_rows", VGPR_FORM),

@@ -168,11 +168,11 @@ static als_status check_qtable(als_ctx *ctx, const als_qtable *t) {
     return ALS_OK;
 }
 
-static als_status check_matrix(als_ctx *ctx, const als_matrix *m, const char *name) {
+static als_status check_matrix(als_ctx *ctx, const als_matrix *m, const char *name, bool items = true) {
     if (!m) return fail(ctx, ALS_EINVAL, std::string(name) + " is null");
     if (m->dtype != ALS_F32 && m->dtype != ALS_BF16) return fail(ctx, ALS_EDTYPE, std::string(name) + ": unknown dtype");
     if (m->rows < 0 || m->cols < 0) return fail(ctx, ALS_EINVAL, std::string(name) + ": negative size");
-    if (m->cols > INT32_MAX) return fail(ctx, ALS_ESHAPE, std::string(name) + ": item ids must fit int32");
+    if (items && m->cols > INT32_MAX) return fail(ctx, ALS_ESHAPE, std::string(name) + ": item ids must fit int32");
     if (m->ld < m->cols) return fail(ctx, ALS_ESHAPE, std::string(name) + ": ld < cols");
     if (m->rows > INT64_MAX / (4 * ALS_TOPK_MAX_K) / std::max<int64_t>(1, m->ld)) return fail(ctx, ALS_ESHAPE, std::string(name) + ": rows * ld is too large");
     if (m->rows > 0 && m->cols > 0 && !m->data) return fail(ctx, ALS_EINVAL, std::string(name) + ": data is null");
@@ -212,6 +212,83 @@ static bool rules_meet(const als_rules *r, const als_matrix *X, const Span &out)
            out.meets(Span(r->penalties, X->rows * 12));
 }
 
+static Span table_span(const als_table *t) { return t ? Span(t) : Span(nullptr, 0); }
+
+// A table of a recurrence or a sum: `rows` rows of d columns; NULL passes where `optional`.
+static als_status check_rows_of(als_ctx *ctx, const als_table *t, int64_t rows, int32_t d, bool optional, const char *name) {
+    if (!t && optional) return ALS_OK;
+    als_status st = check_table(ctx, t, name);
+    if (st != ALS_OK) return st;
+    if (t->rows != rows || t->d != d) return fail(ctx, ALS_ESHAPE, std::string(name) + ": rows or d do not fit");
+    return ALS_OK;
+}
+
+// The tables of a recurrence and the lists over them.
+static als_status check_recur(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F) {
+    als_status st;
+    if (!Y) return fail(ctx, ALS_EINVAL, "Y is null");
+    als_csr lists = *Y;
+    const int32_t none = 0;
+    if (!lists.indices) lists.indices = &none;  // an entry's own row: checked below
+    if ((st = check_csr_args(ctx, &lists, "Y")) != ALS_OK) return st;
+    if (!Y->indices && Y->nnz > Y->cols) return fail(ctx, ALS_ESHAPE, "Y without indices must have at most cols entries");
+    if ((st = check_table(ctx, V, "V")) != ALS_OK) return st;
+    if ((st = check_table(ctx, F, "F")) != ALS_OK) return st;
+    if (V->d != F->d || V->rows != F->rows) return fail(ctx, ALS_ESHAPE, "V and F differ in shape");
+    if (V->dtype != F->dtype) return fail(ctx, ALS_EDTYPE, "V and F differ in dtype");
+    if (Y->cols != V->rows) return fail(ctx, ALS_ESHAPE, "Y->cols != V->rows");
+    if (Y->rows > INT64_MAX / 1024 || Y->nnz > INT64_MAX / 1024) return fail(ctx, ALS_ESHAPE, "Y is too large");
+    return ALS_OK;
+}
+
+// Whether `out` meets the lists.
+static bool lists_meet(const als_csr *Y, const Span &out) {
+    return out.meets(Span(Y->indptr, (Y->rows + 1) * 8)) || out.meets(Span(Y->indices, Y->nnz * 4)) || out.meets(Span(Y->values, Y->nnz * 4));
+}
+
+// X and Y of als_clip and als_reorder: shapes, types and what overlaps.  `rows`: of every matrix, or -1: any.
+static als_status check_pairs(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, int n, int64_t rows) {
+    als_status st;
+    for (int j = 0; j < n; ++j) {
+        if ((st = check_matrix(ctx, X + j, "X", false)) != ALS_OK || (Y && (st = check_matrix(ctx, Y + j, "Y", false)) != ALS_OK)) return st;
+        if (X[j].cols > INT64_MAX / 1024) return fail(ctx, ALS_ESHAPE, "X: cols is too large");
+        if (rows >= 0 && X[j].rows != rows) return fail(ctx, ALS_ESHAPE, "X must have one row per beam");
+        if (Y && (X[j].rows != Y[j].rows || X[j].cols != Y[j].cols)) return fail(ctx, ALS_ESHAPE, "X and Y differ in shape");
+        if (Y && X[j].dtype != Y[j].dtype) return fail(ctx, ALS_EDTYPE, "X and Y differ in dtype");
+    }
+    return ALS_OK;
+}
+
+// Whether an output overlaps another one, or an input other than its own taken as a whole.  Spans in the order of their
+// addresses: an output may not begin before one that is open has ended, nor an input within an output that is not its own.
+static als_status check_pairs_apart(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, int n) {
+    struct Piece {
+        Span span;
+        int of;
+        bool out, in_place;
+    };
+    std::vector<Piece> all;
+    try {
+        all.reserve(2 * (size_t)n);
+    } catch (...) {
+        return fail(ctx, ALS_ENOMEM, "no host memory left");
+    }
+    for (int j = 0; j < n; ++j) {
+        const bool in_place = !Y || (X[j].data == Y[j].data && X[j].ld == Y[j].ld);
+        if (!in_place) all.push_back(Piece{Span(X + j), j, false, false});
+        all.push_back(Piece{Span(in_place ? X + j : Y + j), j, true, in_place});
+    }
+    std::sort(all.begin(), all.end(), [](const Piece &a, const Piece &b) { return a.span.first < b.span.first; });
+    uintptr_t any_end = 0, out_end = 0;  // of all that began before, and of the outputs among them
+    for (const Piece &p : all) {
+        if (p.span.first == p.span.last) continue;
+        if (p.span.first < (p.out ? any_end : out_end)) return fail(ctx, ALS_EALIAS, "an output overlaps another one or an input that is not its own");
+        any_end = std::max(any_end, p.span.last);
+        if (p.out) out_end = std::max(out_end, p.span.last);
+    }
+    return ALS_OK;
+}
+
 }  // namespace als
 
 using namespace als;
@@ -247,6 +324,7 @@ als_status als_create(als_ctx **out, int device) {
     if (st == ALS_OK && hipGetDeviceProperties(&prop, device) == hipSuccess && prop.multiProcessorCount > 0)
         ctx->num_cu = prop.multiProcessorCount;
     if (st == ALS_OK) st = select_setup(ctx);
+    if (st == ALS_OK) st = clip_setup(ctx);
     if (st != ALS_OK) {
         als_destroy(ctx);
         return st;
@@ -260,7 +338,7 @@ als_status als_destroy(als_ctx *ctx) {
     (void)hipSetDevice(ctx->device);
     (void)hipDeviceSynchronize();
     DevBuf *bufs[] = {&ctx->gram_partials, &ctx->lists, &ctx->seg_partials, &ctx->ztable, &ctx->entry_ids, &ctx->rtable, &ctx->small,
-                      &ctx->loss_partials, &ctx->topk_partials, &ctx->select_partials, &ctx->gram_w, &ctx->gram_h};
+                      &ctx->loss_partials, &ctx->topk_partials, &ctx->select_partials, &ctx->clip_partials, &ctx->gram_w, &ctx->gram_h};
     for (DevBuf *b : bufs)
         if (b->p) (void)hipFree(b->p);
     while (DevBuf *b = ctx->outgrown) {
@@ -467,6 +545,150 @@ als_status als_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules,
             return fail(ctx, ALS_EALIAS, "ids, scores and lse must not overlap X, the rules or each other");
     if (X->rows == 0) return ALS_OK;
     return launch_select(ctx, X, rules, temperature, k, ids, scores, lse, (hipStream_t)stream);
+}
+
+als_status als_recur(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
+                     const als_table *states, const als_table *last, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if ((st = check_recur(ctx, Y, V, F)) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, H0, Y->rows, V->d, true, "H0")) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, states, Y->nnz, V->d, true, "states")) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, last, Y->rows, V->d, true, "last")) != ALS_OK) return st;
+    if (!states && !last) return fail(ctx, ALS_EINVAL, "states and last are null");
+    const Span out[2] = {table_span(states), table_span(last)};
+    for (const Span &o : out)
+        if (o.meets(Span(V)) || o.meets(Span(F)) || o.meets(table_span(H0)) || lists_meet(Y, o)) return fail(ctx, ALS_EALIAS, "states or last overlaps an input");
+    if (out[0].meets(out[1])) return fail(ctx, ALS_EALIAS, "states overlaps last");
+    if (Y->rows == 0) return ALS_OK;
+    return launch_recur(ctx, Y, V, F, H0, states, last, (hipStream_t)stream);
+}
+
+als_status als_recur_step(als_ctx *ctx, const int32_t *items, const int32_t *parents, const als_table *V, const als_table *F,
+                          const als_table *H, const als_table *X, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if ((st = check_table(ctx, V, "V")) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, F, V->rows, V->d, false, "F")) != ALS_OK) return st;
+    if (V->dtype != F->dtype) return fail(ctx, ALS_EDTYPE, "V and F differ in dtype");
+    if (V->rows > INT32_MAX) return fail(ctx, ALS_ESHAPE, "V: item ids must fit int32");
+    if ((st = check_table(ctx, H, "H")) != ALS_OK) return st;
+    if ((st = check_table(ctx, X, "X")) != ALS_OK) return st;
+    if (H->d != V->d || X->d != V->d) return fail(ctx, ALS_ESHAPE, "H or X differs from V in d");
+    if (!parents && H->rows != X->rows) return fail(ctx, ALS_ESHAPE, "H and X differ in rows");
+    if (X->rows > 0 && !items) return fail(ctx, ALS_EINVAL, "items is null");
+    if ((uintptr_t)items % 4 || (uintptr_t)parents % 4) return fail(ctx, ALS_ESHAPE, "items and parents must be 4-byte aligned");
+    const Span out(X);
+    const bool in_place = !parents && X->data == H->data && X->ld == H->ld && X->dtype == H->dtype;
+    if ((!in_place && out.meets(Span(H))) || out.meets(Span(V)) || out.meets(Span(F)) || out.meets(Span(items, X->rows * 4)) ||
+        out.meets(Span(parents, X->rows * 4)))
+        return fail(ctx, ALS_EALIAS, "X overlaps an input");
+    if (X->rows == 0) return ALS_OK;
+    return launch_recur_step(ctx, items, parents, V, F, H, X, (hipStream_t)stream);
+}
+
+als_status als_recur_backward(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
+                              const als_table *states, const als_table *d_states, const als_table *d_last, const als_table *dV,
+                              const als_table *dF, const als_table *dH0, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if ((st = check_recur(ctx, Y, V, F)) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, H0, Y->rows, V->d, true, "H0")) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, states, Y->nnz, V->d, false, "states")) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, d_states, Y->nnz, V->d, true, "d_states")) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, d_last, Y->rows, V->d, true, "d_last")) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, dV, Y->nnz, V->d, false, "dV")) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, dF, Y->nnz, V->d, false, "dF")) != ALS_OK) return st;
+    if ((st = check_rows_of(ctx, dH0, Y->rows, V->d, true, "dH0")) != ALS_OK) return st;
+    if (!d_states && !d_last) return fail(ctx, ALS_EINVAL, "d_states and d_last are null");
+    if (dV->dtype != states->dtype || dF->dtype != states->dtype || (d_states && d_states->dtype != states->dtype))
+        return fail(ctx, ALS_EDTYPE, "states, d_states, dV and dF differ in dtype");
+    const Span out[3] = {Span(dV), Span(dF), table_span(dH0)};
+    const als_table *in[6] = {V, F, H0, states, d_states, d_last};
+    for (int i = 0; i < 3; ++i) {
+        for (const als_table *t : in)
+            if (out[i].meets(table_span(t))) return fail(ctx, ALS_EALIAS, "a gradient overlaps an input");
+        if (lists_meet(Y, out[i])) return fail(ctx, ALS_EALIAS, "a gradient overlaps Y");
+        if (out[i].meets(out[(i + 1) % 3])) return fail(ctx, ALS_EALIAS, "gradients overlap");
+    }
+    if (Y->rows == 0) return ALS_OK;
+    return launch_recur_backward(ctx, Y, V, F, H0, states, d_states, d_last, dV, dF, dH0, (hipStream_t)stream);
+}
+
+als_status als_sum_rows(als_ctx *ctx, const als_csr *Y, const als_table *E, const als_table *X, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if ((st = check_csr_args(ctx, Y, "Y")) != ALS_OK) return st;
+    if ((st = check_table(ctx, E, "E")) != ALS_OK) return st;
+    if (Y->cols != E->rows) return fail(ctx, ALS_ESHAPE, "Y->cols != E->rows");
+    if ((st = check_rows_of(ctx, X, Y->rows, E->d, false, "X")) != ALS_OK) return st;
+    if (Y->rows > INT64_MAX / 1024 || Y->nnz > INT64_MAX / 1024) return fail(ctx, ALS_ESHAPE, "Y is too large");
+    const Span out(X);
+    if (out.meets(Span(E)) || lists_meet(Y, out)) return fail(ctx, ALS_EALIAS, "X overlaps an input");
+    if (Y->rows == 0) return ALS_OK;
+    return launch_sum_rows(ctx, Y, E, X, (hipStream_t)stream);
+}
+
+als_status als_clip(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, int32_t n, double bound, double *norm, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if (n < 0 || n > ALS_CLIP_MAX) return fail(ctx, ALS_EINVAL, "n must be in [0, ALS_CLIP_MAX]");
+    if (n > 0 && !X) return fail(ctx, ALS_EINVAL, "X is null");
+    if (!(bound >= 0)) return fail(ctx, ALS_EINVAL, "bound must be >= 0");
+    if (!norm || (uintptr_t)norm % 8) return fail(ctx, ALS_EINVAL, "norm is null or not aligned");
+    if ((st = check_pairs(ctx, X, Y, n, -1)) != ALS_OK) return st;
+    if ((st = check_pairs_apart(ctx, X, Y, n)) != ALS_OK) return st;
+    const Span out(norm, 8);
+    for (int j = 0; j < n; ++j)
+        if (out.meets(Span(X + j)) || (Y && out.meets(Span(Y + j)))) return fail(ctx, ALS_EALIAS, "norm overlaps a tensor");
+    return launch_clip(ctx, X, Y, n, bound, norm, (hipStream_t)stream);
+}
+
+als_status als_beam(als_ctx *ctx, const als_beams *in, int32_t *parents, int32_t *items, float *totals, int32_t *lengths, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    if (!in) return fail(ctx, ALS_EINVAL, "in is null");
+    if (in->beams < 1 || in->beams > ALS_TOPK_MAX_K || in->k < 1 || in->k > ALS_TOPK_MAX_K)
+        return fail(ctx, ALS_EINVAL, "beams and k must be in [1, ALS_TOPK_MAX_K]");
+    if (in->groups < 0) return fail(ctx, ALS_EINVAL, "negative number of groups");
+    if (in->groups > INT32_MAX / in->beams) return fail(ctx, ALS_ESHAPE, "rows must fit int32");
+    if (!(in->temperature > 0.f) || !std::isfinite(in->temperature)) return fail(ctx, ALS_EINVAL, "temperature must be > 0 and finite");
+    if (in->factors && in->n_factors < 1) return fail(ctx, ALS_EINVAL, "n_factors must be at least 1");
+    if (in->groups == 0) return ALS_OK;
+    if (!in->ids || !in->scores || !parents || !items || !totals) return fail(ctx, ALS_EINVAL, "ids, scores, parents, items or totals is null");
+    const int64_t rows = in->groups * in->beams, each = rows * in->k;
+    const void *every[11] = {in->ids, in->scores, in->lse, in->totals, in->last, in->lengths, in->factors, parents, items, totals, lengths};
+    for (const void *p : every)
+        if ((uintptr_t)p % 4) return fail(ctx, ALS_ESHAPE, "every array must be 4-byte aligned");
+    const Span inputs[7] = {Span(in->ids, each * 4), Span(in->scores, each * 4), Span(in->lse, rows * 4), Span(in->totals, rows * 4),
+                            Span(in->last, rows * 4), Span(in->lengths, rows * 4), Span(in->factors, (int64_t)in->n_factors * 4)};
+    const Span out[4] = {Span(parents, rows * 4), Span(items, rows * 4), Span(totals, rows * 4), Span(lengths, rows * 4)};
+    for (int i = 0; i < 4; ++i) {
+        for (const Span &s : inputs)
+            if (out[i].meets(s)) return fail(ctx, ALS_EALIAS, "an output overlaps an input");
+        for (int j = 0; j < i; ++j)
+            if (out[i].meets(out[j])) return fail(ctx, ALS_EALIAS, "outputs overlap");
+    }
+    return launch_beam(ctx, in, parents, items, totals, lengths, (hipStream_t)stream);
+}
+
+als_status als_reorder(als_ctx *ctx, const int32_t *parents, int64_t groups, int32_t beams, const als_matrix *X, const als_matrix *Y,
+                       int32_t n, void *stream) {
+    if (!ctx) return ALS_EINVAL;
+    als_status st;
+    if (n < 0 || n > ALS_REORDER_MAX) return fail(ctx, ALS_EINVAL, "n must be in [0, ALS_REORDER_MAX]");
+    if (n > 0 && !X) return fail(ctx, ALS_EINVAL, "X is null");
+    if (beams < 1 || beams > ALS_TOPK_MAX_K) return fail(ctx, ALS_EINVAL, "beams must be in [1, ALS_TOPK_MAX_K]");
+    if (groups < 0) return fail(ctx, ALS_EINVAL, "negative number of groups");
+    if (groups > INT32_MAX / beams) return fail(ctx, ALS_ESHAPE, "rows must fit int32");
+    if (groups > 0 && !parents) return fail(ctx, ALS_EINVAL, "parents is null");
+    if ((uintptr_t)parents % 4) return fail(ctx, ALS_ESHAPE, "parents must be 4-byte aligned");
+    if ((st = check_pairs(ctx, X, Y, n, groups * beams)) != ALS_OK) return st;
+    if ((st = check_pairs_apart(ctx, X, Y, n)) != ALS_OK) return st;
+    const Span rows(parents, groups * beams * 4);
+    for (int j = 0; j < n; ++j)
+        if (rows.meets(Span(Y ? Y + j : X + j))) return fail(ctx, ALS_EALIAS, "an output overlaps parents");
+    if (groups == 0 || n == 0) return ALS_OK;
+    return launch_reorder(ctx, parents, groups, beams, X, Y, n, (hipStream_t)stream);
 }
 
 als_status als_check_csr(als_ctx *ctx, const als_csr *Y, void *stream) {

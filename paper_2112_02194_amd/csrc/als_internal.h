@@ -159,6 +159,7 @@ struct als_ctx {
     als::DevBuf loss_partials;  // fp64 per-workgroup sums
     als::DevBuf topk_partials;  // top-k: chunk norms, queries left to the scan, chunk maxima per query (or the scan's lists)
     als::DevBuf select_partials;  // als_select: candidates and exponential sums of every part of a row; one size from als_create on
+    als::DevBuf clip_partials;  // als_clip: fp64 sums of its workgroups; one size from als_create on
     als::DevBuf gram_w, gram_h; // fp32 [d*d] Gramians used by als_epoch / als_loss
     bool recorded = false;             // a call whose workspace grows was recorded into a graph
     als::DevBuf *outgrown = nullptr;   // buffers that such a recording may still write to
@@ -227,6 +228,19 @@ als_status launch_adjust(als_ctx *ctx, const als_matrix *X, const als_rules *rul
 als_status select_setup(als_ctx *ctx);  // als_select's workspace, once num_cu is known
 als_status launch_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules, float temperature, int k, int32_t *ids,
                          float *scores, float *lse, hipStream_t s);
+als_status launch_recur(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
+                        const als_table *states, const als_table *last, hipStream_t s);
+als_status launch_recur_step(als_ctx *ctx, const int32_t *items, const int32_t *parents, const als_table *V, const als_table *F,
+                             const als_table *H, const als_table *X, hipStream_t s);
+als_status launch_recur_backward(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
+                                 const als_table *states, const als_table *d_states, const als_table *d_last, const als_table *dV,
+                                 const als_table *dF, const als_table *dH0, hipStream_t s);
+als_status launch_sum_rows(als_ctx *ctx, const als_csr *Y, const als_table *E, const als_table *X, hipStream_t s);
+als_status clip_setup(als_ctx *ctx);  // als_clip's workspace
+als_status launch_clip(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, int n, double bound, double *norm, hipStream_t s);
+als_status launch_beam(als_ctx *ctx, const als_beams *in, int32_t *parents, int32_t *items, float *totals, int32_t *lengths, hipStream_t s);
+als_status launch_reorder(als_ctx *ctx, const int32_t *parents, int64_t groups, int beams, const als_matrix *X, const als_matrix *Y,
+                          int n, hipStream_t s);
 als_status launch_copy_probe(als_ctx *ctx, const void *src, void *dst, int64_t bytes, hipStream_t s);
 
 }  // namespace als

@@ -1,0 +1,82 @@
+// Pieces of table rows as the kernels over ordered entries read and write them: N consecutive columns a lane, fp32 in registers.
+#pragma once
+
+#include "als_internal.h"
+
+namespace als {
+
+// A table as a kernel sees it: rows `ld` bytes apart.
+struct RowsOf {
+    char *p;  // null: not given
+    int64_t ld;
+    int bf16;
+};
+inline RowsOf rows_of(const als_table *t) {
+    return t ? RowsOf{(char *)t->data, t->ld * (t->dtype == ALS_BF16 ? 2 : 4), t->dtype == ALS_BF16} : RowsOf{nullptr, 0, 0};
+}
+
+template <bool BF16, int N> __device__ __forceinline__ void load_piece(const char *row, int lane, float (&x)[N]) {
+    static_assert(N == 4 || N == 8, "16 bytes of one of the types");
+    if constexpr (!BF16) {
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) {
+            const float4 v = *(const float4 *)(row + (lane * N + 4 * j) * 4);
+            x[4 * j] = v.x; x[4 * j + 1] = v.y; x[4 * j + 2] = v.z; x[4 * j + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) {
+            const uint2 v = *(const uint2 *)(row + (lane * N + 4 * j) * 2);
+            x[4 * j] = __uint_as_float(v.x << 16);
+            x[4 * j + 1] = __uint_as_float(v.x & 0xffff0000u);
+            x[4 * j + 2] = __uint_as_float(v.y << 16);
+            x[4 * j + 3] = __uint_as_float(v.y & 0xffff0000u);
+        }
+    }
+}
+template <bool BF16, int N> __device__ __forceinline__ void store_piece(char *row, int lane, const float (&x)[N]) {
+    typedef float Full __attribute__((ext_vector_type(4)));
+    typedef __bf16 Half __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int j = 0; j < N / 4; ++j) {
+        const Full v = {x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+        if constexpr (BF16) *(Half *)(row + (lane * N + 4 * j) * 2) = __builtin_convertvector(v, Half);
+        else *(Full *)(row + (lane * N + 4 * j) * 4) = v;
+    }
+}
+// The same where only the call knows the type: pieces that are read or written once a row.
+template <int N> __device__ __forceinline__ void load_piece(const RowsOf &t, int64_t row, int lane, float (&x)[N]) {
+    if (t.bf16) load_piece<true, N>(t.p + row * t.ld, lane, x);
+    else load_piece<false, N>(t.p + row * t.ld, lane, x);
+}
+template <int N> __device__ __forceinline__ void store_piece(const RowsOf &t, int64_t row, int lane, const float (&x)[N]) {
+    if (t.bf16) store_piece<true, N>(t.p + row * t.ld, lane, x);
+    else store_piece<false, N>(t.p + row * t.ld, lane, x);
+}
+
+// s = 1 / (1 + exp(-g)) and 1 - s, each to its own size: with e = exp(-|g|) they are 1 / (1 + e) and e / (1 + e).
+__device__ __forceinline__ void gate(float g, float &keep, float &take) {
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(g)), large = __builtin_amdgcn_rcpf(1.f + e), small = e * large;
+    const bool up = g >= 0.f;  // NaN: e is NaN, and so are both
+    keep = up ? large : small;
+    take = up ? small : large;
+}
+
+// Entries of row u, whatever indptr holds.
+__device__ __forceinline__ void row_range(const int64_t *indptr, int64_t u, int64_t nnz, int64_t &b, int64_t &e) {
+    b = indptr[u];
+    e = indptr[u + 1];
+    if (b < 0) b = 0;
+    if (e > nnz) e = nnz;
+    if (e < b) e = b;
+}
+
+// Lists over a table: entry p takes row ids[p], or its own where ids is null.
+struct Lists {
+    const int64_t *indptr;
+    const int32_t *ids;
+    int64_t rows, nnz, cols;
+};
+inline Lists lists_of(const als_csr *y) { return Lists{y->indptr, y->indices, y->rows, y->nnz, y->cols}; }
+
+}  // namespace als
