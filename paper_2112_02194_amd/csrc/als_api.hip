@@ -237,7 +237,7 @@ static als_status check_recur(als_ctx *ctx, const als_csr *Y, const als_table *V
     if (V->d != F->d || V->rows != F->rows) return fail(ctx, ALS_ESHAPE, "V and F differ in shape");
     if (V->dtype != F->dtype) return fail(ctx, ALS_EDTYPE, "V and F differ in dtype");
     if (Y->cols != V->rows) return fail(ctx, ALS_ESHAPE, "Y->cols != V->rows");
-    if (Y->rows > INT64_MAX / 1024 || Y->nnz > INT64_MAX / 1024) return fail(ctx, ALS_ESHAPE, "Y is too large");
+    if (Y->rows > INT32_MAX || Y->nnz > INT64_MAX / 1024) return fail(ctx, ALS_ESHAPE, "Y: row numbers must fit int32");
     return ALS_OK;
 }
 
@@ -325,6 +325,7 @@ als_status als_create(als_ctx **out, int device) {
         ctx->num_cu = prop.multiProcessorCount;
     if (st == ALS_OK) st = select_setup(ctx);
     if (st == ALS_OK) st = clip_setup(ctx);
+    if (st == ALS_OK) st = walk_setup(ctx);
     if (st != ALS_OK) {
         als_destroy(ctx);
         return st;
@@ -338,7 +339,7 @@ als_status als_destroy(als_ctx *ctx) {
     (void)hipSetDevice(ctx->device);
     (void)hipDeviceSynchronize();
     DevBuf *bufs[] = {&ctx->gram_partials, &ctx->lists, &ctx->seg_partials, &ctx->ztable, &ctx->entry_ids, &ctx->rtable, &ctx->small,
-                      &ctx->loss_partials, &ctx->topk_partials, &ctx->select_partials, &ctx->clip_partials, &ctx->gram_w, &ctx->gram_h};
+                      &ctx->loss_partials, &ctx->topk_partials, &ctx->select_partials, &ctx->clip_partials, &ctx->walk_maps, &ctx->gram_w, &ctx->gram_h};
     for (DevBuf *b : bufs)
         if (b->p) (void)hipFree(b->p);
     while (DevBuf *b = ctx->outgrown) {
@@ -622,7 +623,7 @@ als_status als_sum_rows(als_ctx *ctx, const als_csr *Y, const als_table *E, cons
     if ((st = check_table(ctx, E, "E")) != ALS_OK) return st;
     if (Y->cols != E->rows) return fail(ctx, ALS_ESHAPE, "Y->cols != E->rows");
     if ((st = check_rows_of(ctx, X, Y->rows, E->d, false, "X")) != ALS_OK) return st;
-    if (Y->rows > INT64_MAX / 1024 || Y->nnz > INT64_MAX / 1024) return fail(ctx, ALS_ESHAPE, "Y is too large");
+    if (Y->rows > INT32_MAX || Y->nnz > INT64_MAX / 1024) return fail(ctx, ALS_ESHAPE, "Y: row numbers must fit int32");
     const Span out(X);
     if (out.meets(Span(E)) || lists_meet(Y, out)) return fail(ctx, ALS_EALIAS, "X overlaps an input");
     if (Y->rows == 0) return ALS_OK;

@@ -160,6 +160,7 @@ struct als_ctx {
     als::DevBuf topk_partials;  // top-k: chunk norms, queries left to the scan, chunk maxima per query (or the scan's lists)
     als::DevBuf select_partials;  // als_select: candidates and exponential sums of every part of a row; one size from als_create on
     als::DevBuf clip_partials;  // als_clip: fp64 sums of its workgroups; one size from als_create on
+    als::DevBuf walk_maps;      // recurrences and sums over long rows: the maps of their pieces; one size from als_create on
     als::DevBuf gram_w, gram_h; // fp32 [d*d] Gramians used by als_epoch / als_loss
     bool recorded = false;             // a call whose workspace grows was recorded into a graph
     als::DevBuf *outgrown = nullptr;   // buffers that such a recording may still write to
@@ -236,6 +237,7 @@ als_status launch_recur_backward(als_ctx *ctx, const als_csr *Y, const als_table
                                  const als_table *states, const als_table *d_states, const als_table *d_last, const als_table *dV,
                                  const als_table *dF, const als_table *dH0, hipStream_t s);
 als_status launch_sum_rows(als_ctx *ctx, const als_csr *Y, const als_table *E, const als_table *X, hipStream_t s);
+als_status walk_setup(als_ctx *ctx);  // the workspace of the four above
 als_status clip_setup(als_ctx *ctx);  // als_clip's workspace
 als_status launch_clip(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, int n, double bound, double *norm, hipStream_t s);
 als_status launch_beam(als_ctx *ctx, const als_beams *in, int32_t *parents, int32_t *items, float *totals, int32_t *lengths, hipStream_t s);

@@ -1,6 +1,8 @@
 // Pieces of table rows as the kernels over ordered entries read and write them: N consecutive columns a lane, fp32 in registers.
 #pragma once
 
+#include <type_traits>
+
 #include "als_internal.h"
 
 namespace als {
@@ -52,6 +54,16 @@ template <int N> __device__ __forceinline__ void load_piece(const RowsOf &t, int
 template <int N> __device__ __forceinline__ void store_piece(const RowsOf &t, int64_t row, int lane, const float (&x)[N]) {
     if (t.bf16) store_piece<true, N>(t.p + row * t.ld, lane, x);
     else store_piece<false, N>(t.p + row * t.ld, lane, x);
+}
+
+// The same pieces as they lie in memory: 16 bytes, or four columns.
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
+typedef uint32_t HalfWords __attribute__((ext_vector_type(2)));
+template <bool BF16> using Part = std::conditional_t<BF16, HalfWords, Words>;
+template <bool BF16, int N, class W> __device__ __forceinline__ void widen(const W &w, float (&x)[N]) {
+    static_assert(sizeof(W) == N * (BF16 ? 2 : 4), "");
+#pragma unroll
+    for (int c = 0; c < N; ++c) x[c] = !BF16 ? __uint_as_float(w[c]) : __uint_as_float(c & 1 ? w[c / 2] & 0xffff0000u : w[c / 2] << 16);
 }
 
 // s = 1 / (1 + exp(-g)) and 1 - s, each to its own size: with e = exp(-|g|) they are 1 / (1 + e) and e / (1 + e).

@@ -3,91 +3,123 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "entry_rows.h"
+#include "entry_walk.h"
 
 namespace als {
 
 constexpr int RECUR_THREADS = 256;
 
-// F(bool) for a value that only the call knows
-template <class F> static auto pick(bool v, F &&f) { return v ? f(std::true_type{}) : f(std::false_type{}); }
-template <class F> static auto pick_d(int d, F &&f) {
-    switch (d) {
-        case 16: return f(std::integral_constant<int, 16>{});
-        case 32: return f(std::integral_constant<int, 32>{});
-        case 64: return f(std::integral_constant<int, 64>{});
-        default: return f(std::integral_constant<int, 128>{});
+// h = s h + (1 - s) x along a row (als_recur).
+template <int D, bool BF, bool SBF, bool STATES> struct Forward {
+    static constexpr int N = BF ? 8 : 4, K = 32 / N, L = D / N, WAVES = 3;
+    static constexpr bool BACK = false, ONES = false, KEEP = true;
+    RowsOf V, F, H0, states, last;
+    struct Raw {
+        Words x, g;
+    };
+    __device__ __forceinline__ void load(Raw &r, int64_t, int64_t id, int lane) const {
+        r.x = *(const Words *)(V.p + id * V.ld + lane * 16);
+        r.g = *(const Words *)(F.p + id * F.ld + lane * 16);
     }
-}
-
-template <int D, bool BF, bool SBF>
-__global__ __launch_bounds__(RECUR_THREADS) void recur_kernel(Lists y, RowsOf V, RowsOf F, RowsOf H0, RowsOf states, RowsOf last) {
-    constexpr int N = BF ? 8 : 4, L = D / N;
-    const int lane = threadIdx.x % L;
-    for (int64_t u = (blockIdx.x * (int64_t)RECUR_THREADS + threadIdx.x) / L; u < y.rows; u += (int64_t)gridDim.x * RECUR_THREADS / L) {
-        int64_t b, e;
-        row_range(y.indptr, u, y.nnz, b, e);
-        float h[N] = {};
-        if (H0.p) load_piece(H0, u, lane, h);
-        for (int64_t p = b; p < e; ++p) {
-            const int64_t i = y.ids ? y.ids[p] : p;
-            if (i >= 0 && i < y.cols) {
-                float x[N], g[N];
-                load_piece<BF, N>(V.p + i * V.ld, lane, x);
-                load_piece<BF, N>(F.p + i * F.ld, lane, g);
+    __device__ __forceinline__ void load_map(Raw &r, int64_t p, int64_t id, int lane) const { load(r, p, id, lane); }
+    __device__ __forceinline__ void map(const Raw &r, bool some, float (&k)[N], float (&b)[N]) const {
+        float x[N], g[N];
+        widen<BF, N>(r.x, x);
+        widen<BF, N>(r.g, g);
 #pragma unroll
-                for (int c = 0; c < N; ++c) {
-                    float keep, take;
-                    gate(g[c], keep, take);
-                    h[c] = fmaf(keep, h[c], take * x[c]);
-                }
-            }
-            if (states.p) store_piece<SBF, N>(states.p + p * states.ld, lane, h);
+        for (int c = 0; c < N; ++c) {
+            float take;
+            gate(g[c], k[c], take);
+            b[c] = take * x[c];
         }
-        if (last.p) store_piece(last, u, lane, h);
+        if (__any(!some)) {
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                k[c] = some ? k[c] : 1.f;
+                b[c] = some ? b[c] : 0.f;
+            }
+        }
     }
-}
+    __device__ __forceinline__ void begin(int64_t row, int lane, float (&s)[N]) const {
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] = 0.f;
+        if (H0.p) load_piece(H0, row, lane, s);
+    }
+    __device__ __forceinline__ void output(int64_t p, bool valid, int lane, const float (&s)[N]) const {
+        if (STATES && valid) store_piece<SBF, N>(states.p + p * states.ld, lane, s);
+    }
+    __device__ __forceinline__ void finish(int64_t row, bool mine, int lane, const float (&s)[N]) const {
+        if (last.p && mine) store_piece(last, row, lane, s);
+    }
+};
 
-template <int D, bool BF, bool SBF>
-__global__ __launch_bounds__(RECUR_THREADS) void recur_backward_kernel(Lists y, RowsOf V, RowsOf F, RowsOf H0, RowsOf states,
-                                                                     RowsOf d_states, RowsOf d_last, RowsOf dV, RowsOf dF, RowsOf dH0) {
-    constexpr int N = BF ? 8 : 4, L = D / N;
-    const int lane = threadIdx.x % L;
-    for (int64_t u = (blockIdx.x * (int64_t)RECUR_THREADS + threadIdx.x) / L; u < y.rows; u += (int64_t)gridDim.x * RECUR_THREADS / L) {
-        int64_t b, e;
-        row_range(y.indptr, u, y.nnz, b, e);
-        float a[N] = {};  // s_{t+1} g_{t+1}
-        if (d_last.p) load_piece(d_last, u, lane, a);
-        for (int64_t p = e - 1; p >= b; --p) {
-            if (d_states.p) {
-                float d[N];
-                load_piece<SBF, N>(d_states.p + p * d_states.ld, lane, d);
+// g = d + a, a = s g from a row's end (als_recur_backward): a, what an entry gets from those behind it, is the state.
+template <int D, bool BF, bool SBF> struct Backward {
+    static constexpr int N = 4, K = 4, L = D / N, WAVES = BF || SBF ? 3 : 2;
+    static constexpr bool BACK = true, ONES = false, KEEP = false;
+    RowsOf V, F, H0, states, d_states, d_last, dV, dF, dH0;
+    struct Raw {
+        Part<BF> x, g;
+        Part<SBF> d, h;
+    };
+    __device__ __forceinline__ void load_map(Raw &r, int64_t p, int64_t id, int lane) const {
+        r.g = *(const Part<BF> *)(F.p + id * F.ld + lane * sizeof(Part<BF>));
+        r.d = Part<SBF>{};
+        if (d_states.p) r.d = *(const Part<SBF> *)(d_states.p + p * d_states.ld + lane * sizeof(Part<SBF>));
+    }
+    __device__ __forceinline__ void load(Raw &r, int64_t p, int64_t id, int lane) const {
+        load_map(r, p, id, lane);
+        r.x = *(const Part<BF> *)(V.p + id * V.ld + lane * sizeof(Part<BF>));
+        r.h = *(const Part<SBF> *)(states.p + max(p - 1, (int64_t)0) * states.ld + lane * sizeof(Part<SBF>));
+    }
+    __device__ __forceinline__ void map(const Raw &r, bool some, float (&k)[N], float (&b)[N]) const {
+        float g[N], d[N];
+        widen<BF, N>(r.g, g);
+        widen<SBF, N>(r.d, d);
 #pragma unroll
-                for (int c = 0; c < N; ++c) a[c] += d[c];
-            }
-            const int64_t i = y.ids ? y.ids[p] : p;
-            float dv[N] = {}, df[N] = {};
-            if (i >= 0 && i < y.cols) {
-                float x[N], g[N], h[N] = {};
-                load_piece<BF, N>(V.p + i * V.ld, lane, x);
-                load_piece<BF, N>(F.p + i * F.ld, lane, g);
-                if (p > b) load_piece<SBF, N>(states.p + (p - 1) * states.ld, lane, h);
-                else if (H0.p) load_piece(H0, u, lane, h);
+        for (int c = 0; c < N; ++c) {
+            float take;
+            gate(g[c], k[c], take);
+            k[c] = some ? k[c] : 1.f;
+            b[c] = k[c] * d[c];
+        }
+    }
+    __device__ __forceinline__ void begin(int64_t row, int lane, float (&s)[N]) const {
 #pragma unroll
-                for (int c = 0; c < N; ++c) {
-                    float keep, take;
-                    gate(g[c], keep, take);
-                    dv[c] = take * a[c];
-                    a[c] *= keep;
-                    df[c] = a[c] * take * (h[c] - x[c]);
-                }
-            }
+        for (int c = 0; c < N; ++c) s[c] = 0.f;
+        if (d_last.p) load_piece(d_last, row, lane, s);
+    }
+    __device__ __forceinline__ void entry(const Raw &r, bool some, int64_t p, bool valid, bool first, const int32_t *rows, int i, int lane,
+                                          float (&s)[N]) const {
+        float x[N], g[N], d[N], h[N], dv[N], df[N];
+        widen<BF, N>(r.x, x);
+        widen<BF, N>(r.g, g);
+        widen<SBF, N>(r.d, d);
+        widen<SBF, N>(r.h, h);
+        if (__any(first)) {
+            float before[N] = {};
+            if (H0.p) load_piece(H0, max(rows[i], 0), lane, before);
+#pragma unroll
+            for (int c = 0; c < N; ++c) h[c] = first ? before[c] : h[c];
+        }
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            float keep, take;
+            gate(g[c], keep, take);
+            const float all = d[c] + s[c], on = keep * all;
+            dv[c] = some ? take * all : 0.f;
+            df[c] = some ? on * take * (h[c] - x[c]) : 0.f;
+            s[c] = some ? on : all;
+        }
+        if (valid) {
             store_piece<SBF, N>(dV.p + p * dV.ld, lane, dv);
             store_piece<SBF, N>(dF.p + p * dF.ld, lane, df);
         }
-        if (dH0.p) store_piece(dH0, u, lane, a);
     }
-}
+    __device__ __forceinline__ void finish(int64_t row, bool mine, int lane, const float (&s)[N]) const {
+        if (dH0.p && mine) store_piece(dH0, row, lane, s);
+    }
+};
 
 // One entry per row, from a parent row.  X may be H where there are no parents: a row is read and written by the same lanes.
 template <int D, bool BF>
@@ -118,14 +150,33 @@ static unsigned groups_grid(int64_t rows, int lanes) {
     return (unsigned)std::min<int64_t>((rows * lanes + RECUR_THREADS - 1) / RECUR_THREADS, 1 << 22);
 }
 
+als_status walk_setup(als_ctx *ctx) { return ensure(ctx, ctx->walk_maps, WALK_BYTES); }
+
+// Tables without rows: no entry has an item, and what is read in its place is somewhere that can be read.
+static RowsOf readable(const als_ctx *ctx, const als_table *t) {
+    return t->rows > 0 ? rows_of(t) : RowsOf{(char *)ctx->small.p, 0, t->dtype == ALS_BF16};
+}
+
+template <class Op> static void launch_all(const als_ctx *ctx, const Op &op, const als_csr *Y, hipStream_t s) {
+    const Chunks c = chunks_of(ctx, Y->nnz, Op::N * Op::L, Walk<Op>::TILE);
+    const Lists y = lists_of(Y);
+    if (Y->nnz > c.longest) {  // there may be rows that are cut
+        hipLaunchKernelGGL((pieces_kernel<Op>), dim3((unsigned)c.count), dim3(64), 0, s, op, y, c);
+        hipLaunchKernelGGL((join_kernel<Op, true>), dim3((unsigned)c.count), dim3(64), 0, s, op, y, c);
+    }
+    hipLaunchKernelGGL((walk_all_kernel<Op>), dim3(walk_grid(c, Y->rows)), dim3(64), 0, s, op, y, c);
+}
+
 als_status launch_recur(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
                         const als_table *states, const als_table *last, hipStream_t s) {
+    const RowsOf v = readable(ctx, V), f = readable(ctx, F), h0 = rows_of(H0), all = rows_of(states), end = rows_of(last);
     pick_d(V->d, [&](auto d) {
         pick(V->dtype == ALS_BF16, [&](auto bf) {
-            pick(states && states->dtype == ALS_BF16, [&](auto sbf) {
-                hipLaunchKernelGGL((recur_kernel<d(), bf(), sbf()>), dim3(groups_grid(Y->rows, d() / (bf() ? 8 : 4))), dim3(RECUR_THREADS), 0, s,
-                                   lists_of(Y), rows_of(V), rows_of(F), rows_of(H0), rows_of(states), rows_of(last));
-            });
+            if (states) {
+                pick(states->dtype == ALS_BF16, [&](auto sbf) { launch_all(ctx, Forward<d(), bf(), sbf(), true>{v, f, h0, all, end}, Y, s); });
+            } else {
+                launch_last(ctx, Forward<d(), bf(), false, false>{v, f, h0, all, end}, Y, s);
+            }
         });
     });
     ALS_HIP(ctx, hipGetLastError());
@@ -135,12 +186,12 @@ als_status launch_recur(als_ctx *ctx, const als_csr *Y, const als_table *V, cons
 als_status launch_recur_backward(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
                                  const als_table *states, const als_table *d_states, const als_table *d_last, const als_table *dV,
                                  const als_table *dF, const als_table *dH0, hipStream_t s) {
+    const RowsOf v = readable(ctx, V), f = readable(ctx, F);
     pick_d(V->d, [&](auto d) {
         pick(V->dtype == ALS_BF16, [&](auto bf) {
             pick(states->dtype == ALS_BF16, [&](auto sbf) {
-                hipLaunchKernelGGL((recur_backward_kernel<d(), bf(), sbf()>), dim3(groups_grid(Y->rows, d() / (bf() ? 8 : 4))), dim3(RECUR_THREADS),
-                                   0, s, lists_of(Y), rows_of(V), rows_of(F), rows_of(H0), rows_of(states), rows_of(d_states), rows_of(d_last),
-                                   rows_of(dV), rows_of(dF), rows_of(dH0));
+                launch_all(ctx, Backward<d(), bf(), sbf()>{v, f, rows_of(H0), rows_of(states), rows_of(d_states), rows_of(d_last), rows_of(dV),
+                                                           rows_of(dF), rows_of(dH0)}, Y, s);
             });
         });
     });
