@@ -66,12 +66,12 @@ template <bool BF16, int N, class W> __device__ __forceinline__ void widen(const
     for (int c = 0; c < N; ++c) x[c] = !BF16 ? __uint_as_float(w[c]) : __uint_as_float(c & 1 ? w[c / 2] & 0xffff0000u : w[c / 2] << 16);
 }
 
-// s = 1 / (1 + exp(-g)) and 1 - s, each to its own size: with e = exp(-|g|) they are 1 / (1 + e) and e / (1 + e).
+// s = 1 / (1 + exp(-g)) and 1 - s, each to its own size: with e = exp(-g) they are 1 / (1 + e) and e / (1 + e).  e is kept within
+// 2^126, where s is 2^-126; a NaN stays one.
 __device__ __forceinline__ void gate(float g, float &keep, float &take) {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(g)), large = __builtin_amdgcn_rcpf(1.f + e), small = e * large;
-    const bool up = g >= 0.f;  // NaN: e is NaN, and so are both
-    keep = up ? large : small;
-    take = up ? small : large;
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_elementwise_maximum(g, -87.3365448f));
+    keep = __builtin_amdgcn_rcpf(1.f + e);
+    take = e * keep;
 }
 
 // Entries of row u, whatever indptr holds.

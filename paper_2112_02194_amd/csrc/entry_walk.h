@@ -27,9 +27,14 @@ constexpr int WALK_MAX_CHUNKS = 16384;
 // Chunks, and what is kept of each for rows that cross its border: maps (k, b) of `d` columns.
 //   across  of the part of a long row up to the border that the walk leaves the chunk by
 //   close   of the part that ends within the chunk; or, where states are needed, the state that comes in (b)
+//   rows    the long row whose pieces join_kernel composes on behalf of this chunk
+struct JoinedRow {
+    int32_t row, pieces;  // none: 0 pieces
+};
 struct Chunks {
     int64_t size, count, longest;
     float *across, *close;  // [count][2][d]
+    JoinedRow *rows;          // [count]
 };
 
 struct Marks {
@@ -53,48 +58,66 @@ struct RowFinder {
         first = wave_uniform(at(0));
         end = max(first, wave_uniform(at(y.rows)));
     }
-    // The last row that begins at or before p: 64 places at a time.
-    __device__ int64_t row_of(int64_t p) const {
-        int64_t lo = 0, hi = y.rows;
-        while (hi - lo > 1) {
-            const int64_t step = (hi - lo + 63) / 64, u = lo + (threadIdx.x & 63) * step;
-            const unsigned long long below = __ballot(u < hi && at(u) <= p);
-            const int k = below ? 63 - __builtin_clzll(below) : 0;
-            lo += k * step;
-            hi = min(hi, lo + step);
+    // The last rows that begin at or before p and q: 64 places at a time, both searches' loads under way together.
+    __device__ void rows_of(int64_t p, int64_t q, int64_t &up, int64_t &uq) const {
+        int64_t lo[2] = {0, 0}, hi[2] = {y.rows, y.rows};
+        while (hi[0] - lo[0] > 1 || hi[1] - lo[1] > 1) {
+            int64_t step[2], b[2], u[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                step[i] = (hi[i] - lo[i] + 63) / 64;
+                u[i] = lo[i] + (threadIdx.x & 63) * step[i];
+                b[i] = at(min(u[i], y.rows));
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const unsigned long long below = __ballot(u[i] < hi[i] && b[i] <= (i ? q : p));
+                const int k = below ? 63 - __builtin_clzll(below) : 0;
+                lo[i] += k * step[i];
+                hi[i] = min(hi[i], lo[i] + step[i]);
+            }
         }
-        return lo;
+        up = lo[0];
+        uq = lo[1];
+    }
+    __device__ __forceinline__ int64_t row_of(int64_t p) const {
+        int64_t u, same;
+        rows_of(p, p, u, same);
+        return u;
     }
     struct Row {
         int64_t u, b, e;
     };
-    __device__ __forceinline__ Row row_at(int64_t p) const {
-        const int64_t u = row_of(p);
-        return Row{u, wave_uniform(at(u)), wave_uniform(at(u + 1))};
-    }
 };
 
-// What a chunk has of rows: entries [begin, end) of the walk without long rows' pieces, and the pieces.
+// What a chunk has of rows: entries [low, high), and the long rows that cross its borders.
 struct ChunkRows {
-    int64_t low, high;       // borders of the chunk among the rows' entries
+    int64_t low, high;           // borders of the chunk among the rows' entries
     bool split_low, split_high;  // a long row crosses that border
-    RowFinder::Row at_low, at_high;
+    RowFinder::Row at_low, at_high;  // the rows at the chunk's first entry and behind its last
     // the border at x: behind a short row that lies across it
-    static __device__ __forceinline__ int64_t border(const RowFinder &f, int64_t x, int64_t longest, bool &split, RowFinder::Row &r) {
+    static __device__ __forceinline__ int64_t border(const RowFinder &f, int64_t x, int64_t longest, const RowFinder::Row &r, bool &split) {
         split = false;
-        r = RowFinder::Row{-1, 0, 0};
         if (x <= f.first) return f.first;
         if (x >= f.end) return f.end;
-        r = f.row_at(x);
         if (r.b >= x || r.e <= x) return x;
         if (r.e - r.b <= longest) return min(r.e, f.end);
         split = true;
         return x;
     }
     __device__ __forceinline__ ChunkRows(const RowFinder &f, const Chunks &c, int64_t chunk) {
-        low = border(f, chunk * c.size, c.longest, split_low, at_low);
-        high = border(f, (chunk + 1) * c.size, c.longest, split_high, at_high);
+        const int64_t x = chunk * c.size, last = max(f.end - 1, f.first);
+        f.rows_of(min(max(x, f.first), last), min(max(x + c.size, f.first), last), at_low.u, at_high.u);
+        const int64_t bl = f.at(at_low.u), el = f.at(at_low.u + 1), bh = f.at(at_high.u), eh = f.at(at_high.u + 1);
+        at_low.b = wave_uniform(bl);
+        at_low.e = wave_uniform(el);
+        at_high.b = wave_uniform(bh);
+        at_high.e = wave_uniform(eh);
+        low = border(f, x, c.longest, at_low, split_low);
+        high = border(f, x + c.size, c.longest, at_high, split_high);
     }
+    // where the search for the rows of a walk from `from` on (down from it) begins
+    __device__ __forceinline__ int64_t row_from(int64_t from) const { return from >= at_low.e ? at_low.u + 1 : at_low.u; }
 };
 
 // Ids and marks of entries i = 0 .. n-1 of the walk from `from` on (down from from - 1 where BACK).  `row`: where the search for rows
@@ -142,11 +165,12 @@ template <bool BACK> __device__ void stage_entries(const RowFinder &f, Marks &m,
 //   N, K, L           columns a lane, entries a group of lanes takes in a tile, lanes of a group
 //   BACK, ONES        from the rows' ends; k is 1 everywhere (sums)
 //   Raw               what is loaded of one entry
-//   load(raw, p, id)  of entry p (id >= 0, or any row of the tables where the entry has no item)
-//   map(raw, some, k, b)   its map; the identity where it has no item (`some` false)
+//   load(raw, p, id)  of entry p; id -1: it has no item, and what is loaded in the item's place leaves the state as it is
+//   load_map(raw, p, id)   what its map takes of that
+//   map(raw, k, b)    its map
 //   begin(row, s)     a row's first state
 //   KEEP: output(p, valid, s)   after an entry whose map was kept in registers
-//   otherwise: entry(raw, some, p, valid, ending, ends, i, s)   moves s on by itself; ends[i]: the row that ends there
+//   otherwise: entry(raw, has an item, p, valid, ending, ends, i, s)   moves s on by itself; ends[i]: the row that ends there
 //   finish(row, mine, s)   a row's last state, where `mine`
 template <class Op> struct Walk {
     static constexpr int N = Op::N, K = Op::K, L = Op::L, GROUPS = 64 / L, TILE = GROUPS * K;
@@ -160,9 +184,9 @@ template <class Op> struct Walk {
         for (int c = 0; c < N; ++c) s[c] = 0.f;
     }
 
-    // The groups' maps joined: s_in for every group, and the tile's map as a whole in the last group's lanes (k, b, seen).
+    // The groups' maps joined: the state that comes into every group, and s behind the tile.
     // seen: the group's entries hold a row's start, so that nothing of what comes in reaches its end.
-    __device__ __forceinline__ void join(float (&k)[N], float (&b)[N], bool &seen, float (&in)[N]) {
+    __device__ __forceinline__ void join(float (&k)[N], float (&b)[N], bool seen, float (&in)[N]) {
 #pragma unroll
         for (int step = 1; step < GROUPS; step *= 2) {
             const unsigned long long starts = __ballot(seen);
@@ -180,19 +204,19 @@ template <class Op> struct Walk {
             }
             if (group >= step) seen = seen || (starts >> (threadIdx.x - step * L) & 1);
         }
-        const unsigned long long starts = __ballot(seen);
-        const bool before = group > 0 && (starts >> (threadIdx.x - L) & 1);
+        // the state behind each group; it comes into the next one, the last group's into the next tile
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            const float bo = __shfl_up(b[c], L), ko = Op::ONES ? 1.f : __shfl_up(k[c], L);
-            in[c] = group == 0 ? s[c] : before ? bo : Op::ONES ? s[c] + bo : fmaf(ko, s[c], bo);
+            const float after = seen ? b[c] : Op::ONES ? s[c] + b[c] : fmaf(k[c], s[c], b[c]);
+            const float prior = __shfl_up(after, L);
+            in[c] = group == 0 ? s[c] : prior;
+            s[c] = __shfl(after, (GROUPS - 1) * L + lane);
         }
     }
 
     // Entries [from, from + n) (down from from - 1 where BACK) with all their rows; s is the state that comes in.
-    __device__ void entries(Marks &m, int64_t from, int64_t n) {
-        if (n <= 0) return;
-        int64_t row = rows.row_of(Op::BACK ? from - 1 : from);
+    // row: where the search for their rows begins.
+    __device__ void entries(Marks &m, int64_t from, int64_t n, int64_t row) {
         for (int64_t done = 0; done < n; done += WALK_STAGE) {
             const int64_t here = Op::BACK ? from - done : from + done;
             const int many = (int)min(n - done, (int64_t)WALK_STAGE);
@@ -200,22 +224,21 @@ template <class Op> struct Walk {
             for (int tile = 0; tile < many; tile += TILE) {
                 const int i0 = tile + group * K;
                 typename Op::Raw raw[K];
-                int some = 0, starts = 0, ends = 0;  // a bit per entry: has an item, a row starts, ends there
+                int starts = 0, ends = 0;  // a bit per entry: a row starts, ends there
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     const int id = m.id[i0 + j];
-                    some |= (id >= 0) << j;
                     starts |= (m.start[i0 + j] >= 0) << j;
                     ends |= (m.end[i0 + j] >= 0) << j;
                     // entries behind the last one: any that is there
-                    op.load(raw[j], Op::BACK ? here - 1 - min(i0 + j, many - 1) : here + min(i0 + j, many - 1), max(id, 0), lane);
+                    op.load(raw[j], Op::BACK ? here - 1 - min(i0 + j, many - 1) : here + min(i0 + j, many - 1), id, lane);
                 }
                 // No branch that some lanes take but for stores: a value is chosen, what is read for it is somewhere that can be read.
                 float k[N], b[N], keep[Op::KEEP && !Op::ONES ? K : 1][N], add[Op::KEEP ? K : 1][N];
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     float kj[N], bj[N];
-                    op.map(raw[j], some >> j & 1, kj, bj);
+                    op.map(raw[j], kj, bj);
                     const bool starting = starts >> j & 1;
                     if (j == 0) {
 #pragma unroll
@@ -235,18 +258,8 @@ template <class Op> struct Walk {
                         if constexpr (Op::KEEP) add[j][c] = bj[c];
                     }
                 }
-                bool seen = starts != 0;
                 float h[N];
-                join(k, b, seen, h);
-                {
-                    const bool all = __ballot(seen) >> 63;
-                    const int from_lane = (GROUPS - 1) * L + lane;
-#pragma unroll
-                    for (int c = 0; c < N; ++c) {
-                        const float bo = __shfl(b[c], from_lane), ko = Op::ONES ? 1.f : __shfl(k[c], from_lane);
-                        s[c] = all ? bo : Op::ONES ? s[c] + bo : fmaf(ko, s[c], bo);
-                    }
-                }
+                join(k, b, starts != 0, h);
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     const bool starting = starts >> j & 1, ending = ends >> j & 1;
@@ -262,7 +275,7 @@ template <class Op> struct Walk {
                         for (int c = 0; c < N; ++c) h[c] = Op::ONES ? h[c] + add[j][c] : fmaf(keep[j][c], h[c], add[j][c]);
                         op.output(p, i0 + j < many, lane, h);
                     } else {
-                        op.entry(raw[j], some >> j & 1, p, i0 + j < many, ending, m.end, i0 + j, lane, h);
+                        op.entry(raw[j], m.id[i0 + j] >= 0, p, i0 + j < many, ending, m.end, i0 + j, lane, h);
                     }
                     if (__any(ending)) op.finish(max(m.end[i0 + j], 0), ending, lane, h);
                 }
@@ -286,20 +299,23 @@ template <class Op> struct Walk {
         }
         for (int64_t done = 0; done < n; done += TILE) {
             typename Op::Raw raw[K];
-            bool some[K];
+            int id[K];
 #pragma unroll
             for (int j = 0; j < K; ++j) {
                 const int64_t i = done + group * K + j, at = min(i, n - 1), p = Op::BACK ? from - 1 - at : from + at;
-                int id = rows.y.ids ? rows.y.ids[p] : (int)p;
-                some[j] = i < n && id >= 0 && id < rows.y.cols;
-                if (!some[j]) id = 0;
-                op.load_map(raw[j], p, id, lane);
+                id[j] = rows.y.ids ? rows.y.ids[p] : (int)p;
+                if (i >= n || id[j] >= rows.y.cols) id[j] = -1;
+            }
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const int64_t at = min(done + group * K + j, n - 1);
+                op.load_map(raw[j], Op::BACK ? from - 1 - at : from + at, id[j], lane);
             }
             float k[N], b[N];
 #pragma unroll
             for (int j = 0; j < K; ++j) {
                 float kj[N], bj[N];
-                op.map(raw[j], some[j], kj, bj);
+                op.map(raw[j], kj, bj);
                 if (Op::BACK && done + group * K + j >= n) {  // gradients of entries without an item count, those behind the end do not
 #pragma unroll
                     for (int c = 0; c < N; ++c) bj[c] = 0.f;
@@ -357,6 +373,14 @@ template <class Op> __device__ void empty_rows(const Op &op, const RowFinder &f,
     }
 }
 
+// The long row that join_kernel composes on behalf of a chunk (uniform in the wavefront).
+__device__ __forceinline__ void leave_long_row(const Chunks &c, int64_t chunk, bool some, const RowFinder::Row &r) {
+    if (threadIdx.x == 0) {
+        const int64_t first = r.b / c.size, last = min((r.e - 1) / c.size, c.count - 1);
+        c.rows[chunk] = JoinedRow{(int32_t)r.u, some ? (int32_t)max(last - first, (int64_t)0) : 0};
+    }
+}
+
 // Last states: every chunk's short rows, and the maps of its long rows' pieces.
 template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_last_kernel(Op op, Lists y, Chunks c) {
     constexpr int D = Op::N * Op::L;
@@ -365,11 +389,12 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_last_k
     const int64_t chunk = blockIdx.x;
     if (chunk >= c.count) return empty_rows(op, f, chunk - c.count, gridDim.x - c.count);
     const ChunkRows r(f, c, chunk);
+    const bool through = r.split_low && r.split_high && r.at_low.u == r.at_high.u;
+    leave_long_row(c, chunk, r.split_low && !through, r.at_low);
     int64_t low = r.low, high = r.high;
-    if (low >= high) return;
-    if (r.split_low) {
+    if (r.split_low && low < high) {
         const int64_t e = min(r.at_low.e, high);
-        Walk<Op>(op, f).piece(low, e - low, -1, (e == r.at_low.e && !(r.split_high && r.at_high.u == r.at_low.u) ? c.close : c.across) + chunk * 2 * D);
+        Walk<Op>(op, f).piece(low, e - low, -1, (through ? c.across : c.close) + chunk * 2 * D);
         low = e;
     }
     if (r.split_high && low < high) {
@@ -377,10 +402,10 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_last_k
         Walk<Op>(op, f).piece(b, high - b, r.at_high.u, c.across + chunk * 2 * D);
         high = b;
     }
-    Walk<Op>(op, f).entries(m, low, high - low);
+    if (low < high) Walk<Op>(op, f).entries(m, low, high - low, r.row_from(low));
 }
 
-// All entries' outputs; rows that come in begin with the state that carry_kernel left.
+// All entries' outputs; rows that come in begin with the state that join_kernel left.
 template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_all_kernel(Op op, Lists y, Chunks c) {
     constexpr int D = Op::N * Op::L;
     __shared__ __align__(16) Marks m;
@@ -388,12 +413,13 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_all_ke
     const int64_t chunk = blockIdx.x;
     if (chunk >= c.count) return empty_rows(op, f, chunk - c.count, gridDim.x - c.count);
     const ChunkRows r(f, c, chunk);
+    if (r.low >= r.high) return;
     Walk<Op> walk(op, f);
     if (Op::BACK ? r.split_high : r.split_low) {
 #pragma unroll
         for (int j = 0; j < Op::N; ++j) walk.s[j] = c.close[(chunk * 2 + 1) * D + walk.lane * Op::N + j];
     }
-    walk.entries(m, Op::BACK ? r.high : r.low, r.high - r.low);
+    walk.entries(m, Op::BACK ? r.high : r.low, r.high - r.low, Op::BACK ? r.at_high.u : r.row_from(r.low));
 }
 
 // The map of the part of a long row that leads to the border where the walk leaves the chunk.
@@ -402,66 +428,90 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kern
     const RowFinder f(y);
     const int64_t chunk = blockIdx.x;
     const ChunkRows r(f, c, chunk);
-    if (!(Op::BACK ? r.split_low : r.split_high) || r.low >= r.high) return;
     const RowFinder::Row row = Op::BACK ? r.at_low : r.at_high;
+    const bool out = Op::BACK ? r.split_low : r.split_high;
+    const bool through = r.split_low && r.split_high && r.at_low.u == r.at_high.u;
+    leave_long_row(c, chunk, out && !through, row);
+    if (!out || r.low >= r.high) return;
     const int64_t low = max(r.low, row.b), high = min(r.high, row.e);
-    const bool whole = Op::BACK ? row.e <= r.high : row.b >= r.low;
-    Walk<Op>(op, f).piece(Op::BACK ? high : low, high - low, whole ? row.u : -1, c.across + chunk * 2 * D);
+    Walk<Op>(op, f).piece(Op::BACK ? high : low, high - low, through ? -1 : row.u, c.across + chunk * 2 * D);
 }
 
-// A long row's pieces one after the other, by the wavefront of the chunk that the walk along the row begins in (CARRY: the state
-// at every border it crosses goes to the chunk behind it) or ends in (otherwise: the row's last state).
-template <class Op, bool CARRY> __global__ __launch_bounds__(64) void join_kernel(Op op, Lists y, Chunks c) {
-    constexpr int D = Op::N * Op::L, AHEAD = 8;
-    const RowFinder f(y);
-    const int64_t chunk = blockIdx.x;
-    const ChunkRows r(f, c, chunk);
-    RowFinder::Row row;
-    if (CARRY) {
-        // begins here: it crosses the border that the walk leaves by, and not the other one
-        if (!(Op::BACK ? r.split_low : r.split_high) || r.low >= r.high) return;
-        row = Op::BACK ? r.at_low : r.at_high;
-        if (Op::BACK ? r.split_high && r.at_high.u == row.u : r.split_low && r.at_low.u == row.u) return;
-    } else {
-        if (!r.split_low || (r.split_high && r.at_high.u == r.at_low.u)) return;
-        row = r.at_low;
-    }
-    const int64_t first = row.b / c.size, last = (row.e - 1) / c.size, from = Op::BACK ? last : first;
-    const int64_t pieces = min(last - first, c.count - 1);  // but for the closing one
-    const int lane = threadIdx.x;
-    if (lane >= Op::L) return;
-    float s[Op::N];
+// A long row's pieces one after the other, on behalf of the chunk that the walk along the row begins in (CARRY: the state at every
+// border it crosses goes to the chunk behind it) or ends in (otherwise: the row's last state).  The pieces are dealt out in
+// stretches to groups of lanes, whose maps are joined through LDS.  A workgroup looks at JOIN_CHUNKS chunks.
+constexpr int JOIN_THREADS = 512, JOIN_CHUNKS = 16;
+template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(Op op, Chunks c) {
+    constexpr int N = Op::N, D = N * Op::L, AHEAD = 4, GROUPS = JOIN_THREADS / Op::L;
+    __shared__ float maps[GROUPS][2][D];
+    __shared__ JoinedRow found[JOIN_CHUNKS];
+    const int lane = threadIdx.x % Op::L, group = threadIdx.x / Op::L;
+    const int64_t chunk0 = (int64_t)blockIdx.x * JOIN_CHUNKS;
+    if (threadIdx.x < JOIN_CHUNKS) found[threadIdx.x] = chunk0 + threadIdx.x < c.count ? c.rows[chunk0 + threadIdx.x] : JoinedRow{0, 0};
+    __syncthreads();
+    for (int n = 0; n < JOIN_CHUNKS; ++n) {
+        const int pieces = found[n].pieces;
+        if (pieces == 0) continue;
+        const int64_t chunk = chunk0 + n;
+        // piece i of the walk is kept with chunk at(i); without CARRY the chunk itself has the closing one
+        auto at = [&](int i) { return min(max(CARRY ? (Op::BACK ? chunk - i : chunk + i) : chunk - pieces + i, (int64_t)0), c.count - 1); };
+        const int each = (pieces + GROUPS - 1) / GROUPS, begin = min(group * each, pieces), end = min(begin + each, pieces);
+        const int groups = (pieces + each - 1) / each;
+        float k[N], s[N];
 #pragma unroll
-    for (int j = 0; j < Op::N; ++j) s[j] = 0.f;
-    for (int64_t i0 = 0; i0 < pieces; i0 += AHEAD) {
-        float k[AHEAD][Op::N], b[AHEAD][Op::N];
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            const int64_t i = min(i0 + a, pieces - 1), at = min(max(Op::BACK ? from - i : from + i, (int64_t)0), c.count - 1);
-#pragma unroll
-            for (int j = 0; j < Op::N; ++j) {
-                k[a][j] = c.across[at * 2 * D + lane * Op::N + j];
-                b[a][j] = c.across[(at * 2 + 1) * D + lane * Op::N + j];
-            }
+        for (int j = 0; j < N; ++j) {
+            k[j] = 1.f;
+            s[j] = 0.f;
         }
+        auto walk = [&](auto &&then) {
+            for (int i0 = begin; i0 < end; i0 += AHEAD) {
+                float kp[AHEAD][N], bp[AHEAD][N];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            const int64_t i = i0 + a;
-            if (i < pieces) {
+                for (int a = 0; a < AHEAD; ++a) {
+                    const float *map = c.across + at(min(i0 + a, end - 1)) * 2 * D + lane * N;
 #pragma unroll
-                for (int j = 0; j < Op::N; ++j) s[j] = i ? fmaf(k[a][j], s[j], b[a][j]) : b[a][j];
-                if (CARRY) {
-                    const int64_t to = min(max(Op::BACK ? from - i - 1 : from + i + 1, (int64_t)0), c.count - 1);
+                    for (int j = 0; j < N; ++j) {
+                        kp[a][j] = map[j];
+                        bp[a][j] = map[D + j];
+                    }
+                }
 #pragma unroll
-                    for (int j = 0; j < Op::N; ++j) c.close[(to * 2 + 1) * D + lane * Op::N + j] = s[j];
+                for (int a = 0; a < AHEAD; ++a) {
+                    const bool on = i0 + a < end, first = i0 + a == 0;  // the first piece has the row's own first state in it
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        s[j] = !on ? s[j] : first ? bp[a][j] : fmaf(kp[a][j], s[j], bp[a][j]);
+                        k[j] = on ? k[j] * kp[a][j] : k[j];
+                    }
+                    then(i0 + a, on);
                 }
             }
-        }
-    }
-    if (!CARRY) {
+        };
+        walk([](int, bool) {});
 #pragma unroll
-        for (int j = 0; j < Op::N; ++j) s[j] = fmaf(c.close[chunk * 2 * D + lane * Op::N + j], s[j], c.close[(chunk * 2 + 1) * D + lane * Op::N + j]);
-        op.finish(row.u, true, lane, s);
+        for (int j = 0; j < N; ++j) {
+            maps[group][0][lane * N + j] = k[j];
+            maps[group][1][lane * N + j] = s[j];
+        }
+        __syncthreads();
+        const int upto = CARRY ? min(group, groups) : groups;
+        for (int g = 0; g < upto; ++g)
+#pragma unroll
+            for (int j = 0; j < N; ++j) s[j] = g ? fmaf(maps[g][0][lane * N + j], s[j], maps[g][1][lane * N + j]) : maps[0][1][lane * N + j];
+        if (CARRY) {
+            walk([&](int i, bool on) {
+                if (!on) return;
+                float *to = c.close + (at(i + 1) * 2 + 1) * D + lane * N;
+#pragma unroll
+                for (int j = 0; j < N; ++j) to[j] = s[j];
+            });
+        } else if (group == 0) {
+            const float *map = c.close + chunk * 2 * D + lane * N;
+#pragma unroll
+            for (int j = 0; j < N; ++j) s[j] = fmaf(map[j], s[j], map[D + j]);
+            op.finish(found[n].row, true, lane, s);
+        }
+        __syncthreads();
     }
 }
 
@@ -475,17 +525,21 @@ inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int d, int tile) {
     c.longest = c.size;
     c.across = (float *)ctx->walk_maps.p;
     c.close = c.across + (int64_t)WALK_MAX_CHUNKS * 2 * 128;
+    c.rows = (JoinedRow *)(c.close + (int64_t)WALK_MAX_CHUNKS * 2 * 128);
     return c;
 }
-constexpr size_t WALK_BYTES = (size_t)WALK_MAX_CHUNKS * 4 * 128 * sizeof(float);
+// behind the chunks': rows for entries without an item, 512 bytes each: zeros, gates in fp32, gates in bf16
+constexpr size_t WALK_NONE = (size_t)WALK_MAX_CHUNKS * (4 * 128 * sizeof(float) + sizeof(JoinedRow)), WALK_BYTES = WALK_NONE + 3 * 512;
+inline const char *none_row(const als_ctx *ctx, bool gates, bool bf16) { return (const char *)ctx->walk_maps.p + WALK_NONE + (!gates ? 0 : bf16 ? 1024 : 512); }
 constexpr int EMPTY_GROUPS = 1024;  // workgroups that look for empty rows, at most
+inline unsigned join_grid(const Chunks &c) { return (unsigned)((c.count + JOIN_CHUNKS - 1) / JOIN_CHUNKS); }
 inline unsigned walk_grid(const Chunks &c, int64_t rows) { return (unsigned)(c.count + std::min<int64_t>((rows + 63) / 64, EMPTY_GROUPS)); }
 
 template <class Op> void launch_last(const als_ctx *ctx, const Op &op, const als_csr *Y, hipStream_t s) {
     const Chunks c = chunks_of(ctx, Y->nnz, Op::N * Op::L, Walk<Op>::TILE);
     const Lists y = lists_of(Y);
     hipLaunchKernelGGL((walk_last_kernel<Op>), dim3(walk_grid(c, Y->rows)), dim3(64), 0, s, op, y, c);
-    if (Y->nnz > c.longest) hipLaunchKernelGGL((join_kernel<Op, false>), dim3((unsigned)c.count), dim3(64), 0, s, op, y, c);
+    if (Y->nnz > c.longest) hipLaunchKernelGGL((join_kernel<Op, false>), dim3(join_grid(c)), dim3(JOIN_THREADS), 0, s, op, c);
 }
 
 // F(bool) for a value that only the call knows

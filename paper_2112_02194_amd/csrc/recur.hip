@@ -11,18 +11,19 @@ constexpr int RECUR_THREADS = 256;
 
 // h = s h + (1 - s) x along a row (als_recur).
 template <int D, bool BF, bool SBF, bool STATES> struct Forward {
-    static constexpr int N = BF ? 8 : 4, K = 32 / N, L = D / N, WAVES = 3;
+    static constexpr int N = BF ? 8 : 4, K = 32 / N, L = D / N, WAVES = STATES || (BF && D <= 32) ? 3 : 4;
     static constexpr bool BACK = false, ONES = false, KEEP = true;
     RowsOf V, F, H0, states, last;
+    const char *no_x, *no_g;
     struct Raw {
         Words x, g;
     };
-    __device__ __forceinline__ void load(Raw &r, int64_t, int64_t id, int lane) const {
-        r.x = *(const Words *)(V.p + id * V.ld + lane * 16);
-        r.g = *(const Words *)(F.p + id * F.ld + lane * 16);
+    __device__ __forceinline__ void load(Raw &r, int64_t, int id, int lane) const {
+        r.x = *(const Words *)((id < 0 ? no_x : V.p + id * V.ld) + lane * 16);
+        r.g = *(const Words *)((id < 0 ? no_g : F.p + id * F.ld) + lane * 16);
     }
-    __device__ __forceinline__ void load_map(Raw &r, int64_t p, int64_t id, int lane) const { load(r, p, id, lane); }
-    __device__ __forceinline__ void map(const Raw &r, bool some, float (&k)[N], float (&b)[N]) const {
+    __device__ __forceinline__ void load_map(Raw &r, int64_t p, int id, int lane) const { load(r, p, id, lane); }
+    __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&b)[N]) const {
         float x[N], g[N];
         widen<BF, N>(r.x, x);
         widen<BF, N>(r.g, g);
@@ -31,13 +32,6 @@ template <int D, bool BF, bool SBF, bool STATES> struct Forward {
             float take;
             gate(g[c], k[c], take);
             b[c] = take * x[c];
-        }
-        if (__any(!some)) {
-#pragma unroll
-            for (int c = 0; c < N; ++c) {
-                k[c] = some ? k[c] : 1.f;
-                b[c] = some ? b[c] : 0.f;
-            }
         }
     }
     __device__ __forceinline__ void begin(int64_t row, int lane, float (&s)[N]) const {
@@ -55,24 +49,25 @@ template <int D, bool BF, bool SBF, bool STATES> struct Forward {
 
 // g = d + a, a = s g from a row's end (als_recur_backward): a, what an entry gets from those behind it, is the state.
 template <int D, bool BF, bool SBF> struct Backward {
-    static constexpr int N = 4, K = 4, L = D / N, WAVES = BF || SBF ? 3 : 2;
+    static constexpr int N = 4, K = 4, L = D / N, WAVES = 3;
     static constexpr bool BACK = true, ONES = false, KEEP = false;
     RowsOf V, F, H0, states, d_states, d_last, dV, dF, dH0;
+    const char *no_x, *no_g;
     struct Raw {
         Part<BF> x, g;
         Part<SBF> d, h;
     };
-    __device__ __forceinline__ void load_map(Raw &r, int64_t p, int64_t id, int lane) const {
-        r.g = *(const Part<BF> *)(F.p + id * F.ld + lane * sizeof(Part<BF>));
+    __device__ __forceinline__ void load_map(Raw &r, int64_t p, int id, int lane) const {
+        r.g = *(const Part<BF> *)((id < 0 ? no_g : F.p + id * F.ld) + lane * sizeof(Part<BF>));
         r.d = Part<SBF>{};
         if (d_states.p) r.d = *(const Part<SBF> *)(d_states.p + p * d_states.ld + lane * sizeof(Part<SBF>));
     }
-    __device__ __forceinline__ void load(Raw &r, int64_t p, int64_t id, int lane) const {
+    __device__ __forceinline__ void load(Raw &r, int64_t p, int id, int lane) const {
         load_map(r, p, id, lane);
-        r.x = *(const Part<BF> *)(V.p + id * V.ld + lane * sizeof(Part<BF>));
+        r.x = *(const Part<BF> *)((id < 0 ? no_x : V.p + id * V.ld) + lane * sizeof(Part<BF>));
         r.h = *(const Part<SBF> *)(states.p + max(p - 1, (int64_t)0) * states.ld + lane * sizeof(Part<SBF>));
     }
-    __device__ __forceinline__ void map(const Raw &r, bool some, float (&k)[N], float (&b)[N]) const {
+    __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&b)[N]) const {
         float g[N], d[N];
         widen<BF, N>(r.g, g);
         widen<SBF, N>(r.d, d);
@@ -80,7 +75,6 @@ template <int D, bool BF, bool SBF> struct Backward {
         for (int c = 0; c < N; ++c) {
             float take;
             gate(g[c], k[c], take);
-            k[c] = some ? k[c] : 1.f;
             b[c] = k[c] * d[c];
         }
     }
@@ -106,10 +100,10 @@ template <int D, bool BF, bool SBF> struct Backward {
         for (int c = 0; c < N; ++c) {
             float keep, take;
             gate(g[c], keep, take);
-            const float all = d[c] + s[c], on = keep * all;
+            const float all = d[c] + s[c];
+            s[c] = keep * all;
             dv[c] = some ? take * all : 0.f;
-            df[c] = some ? on * take * (h[c] - x[c]) : 0.f;
-            s[c] = some ? on : all;
+            df[c] = some ? s[c] * take * (h[c] - x[c]) : 0.f;
         }
         if (valid) {
             store_piece<SBF, N>(dV.p + p * dV.ld, lane, dv);
@@ -150,11 +144,17 @@ static unsigned groups_grid(int64_t rows, int lanes) {
     return (unsigned)std::min<int64_t>((rows * lanes + RECUR_THREADS - 1) / RECUR_THREADS, 1 << 22);
 }
 
-als_status walk_setup(als_ctx *ctx) { return ensure(ctx, ctx->walk_maps, WALK_BYTES); }
-
-// Tables without rows: no entry has an item, and what is read in its place is somewhere that can be read.
-static RowsOf readable(const als_ctx *ctx, const als_table *t) {
-    return t->rows > 0 ? rows_of(t) : RowsOf{(char *)ctx->small.p, 0, t->dtype == ALS_BF16};
+als_status walk_setup(als_ctx *ctx) {
+    als_status st = ensure(ctx, ctx->walk_maps, WALK_BYTES);
+    if (st != ALS_OK) return st;
+    uint32_t none[3][128];
+    for (int i = 0; i < 128; ++i) {
+        none[0][i] = 0;
+        none[1][i] = 0x7f800000u;  // +inf: 1 / (1 + exp(-inf)) keeps all
+        none[2][i] = 0x7f807f80u;
+    }
+    ALS_HIP(ctx, hipMemcpy((char *)ctx->walk_maps.p + WALK_NONE, none, sizeof(none), hipMemcpyHostToDevice));
+    return ALS_OK;
 }
 
 template <class Op> static void launch_all(const als_ctx *ctx, const Op &op, const als_csr *Y, hipStream_t s) {
@@ -162,20 +162,21 @@ template <class Op> static void launch_all(const als_ctx *ctx, const Op &op, con
     const Lists y = lists_of(Y);
     if (Y->nnz > c.longest) {  // there may be rows that are cut
         hipLaunchKernelGGL((pieces_kernel<Op>), dim3((unsigned)c.count), dim3(64), 0, s, op, y, c);
-        hipLaunchKernelGGL((join_kernel<Op, true>), dim3((unsigned)c.count), dim3(64), 0, s, op, y, c);
+        hipLaunchKernelGGL((join_kernel<Op, true>), dim3(join_grid(c)), dim3(JOIN_THREADS), 0, s, op, c);
     }
     hipLaunchKernelGGL((walk_all_kernel<Op>), dim3(walk_grid(c, Y->rows)), dim3(64), 0, s, op, y, c);
 }
 
 als_status launch_recur(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
                         const als_table *states, const als_table *last, hipStream_t s) {
-    const RowsOf v = readable(ctx, V), f = readable(ctx, F), h0 = rows_of(H0), all = rows_of(states), end = rows_of(last);
+    const RowsOf v = rows_of(V), f = rows_of(F), h0 = rows_of(H0), all = rows_of(states), end = rows_of(last);
+    const char *no_x = none_row(ctx, false, false), *no_g = none_row(ctx, true, V->dtype == ALS_BF16);
     pick_d(V->d, [&](auto d) {
         pick(V->dtype == ALS_BF16, [&](auto bf) {
             if (states) {
-                pick(states->dtype == ALS_BF16, [&](auto sbf) { launch_all(ctx, Forward<d(), bf(), sbf(), true>{v, f, h0, all, end}, Y, s); });
+                pick(states->dtype == ALS_BF16, [&](auto sbf) { launch_all(ctx, Forward<d(), bf(), sbf(), true>{v, f, h0, all, end, no_x, no_g}, Y, s); });
             } else {
-                launch_last(ctx, Forward<d(), bf(), false, false>{v, f, h0, all, end}, Y, s);
+                launch_last(ctx, Forward<d(), bf(), false, false>{v, f, h0, all, end, no_x, no_g}, Y, s);
             }
         });
     });
@@ -186,12 +187,12 @@ als_status launch_recur(als_ctx *ctx, const als_csr *Y, const als_table *V, cons
 als_status launch_recur_backward(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
                                  const als_table *states, const als_table *d_states, const als_table *d_last, const als_table *dV,
                                  const als_table *dF, const als_table *dH0, hipStream_t s) {
-    const RowsOf v = readable(ctx, V), f = readable(ctx, F);
+    const char *no_x = none_row(ctx, false, false), *no_g = none_row(ctx, true, V->dtype == ALS_BF16);
     pick_d(V->d, [&](auto d) {
         pick(V->dtype == ALS_BF16, [&](auto bf) {
             pick(states->dtype == ALS_BF16, [&](auto sbf) {
-                launch_all(ctx, Backward<d(), bf(), sbf()>{v, f, rows_of(H0), rows_of(states), rows_of(d_states), rows_of(d_last), rows_of(dV),
-                                                           rows_of(dF), rows_of(dH0)}, Y, s);
+                launch_all(ctx, Backward<d(), bf(), sbf()>{rows_of(V), rows_of(F), rows_of(H0), rows_of(states), rows_of(d_states), rows_of(d_last), rows_of(dV),
+                                                           rows_of(dF), rows_of(dH0), no_x, no_g}, Y, s);
             });
         });
     });

@@ -8,25 +8,22 @@ template <int D, bool BF> struct SumRows {
     static constexpr bool BACK = false, ONES = true, KEEP = true;
     RowsOf E, X;
     const float *values;
+    const char *no_x;
     struct Raw {
         Words x;
         float w;
     };
-    __device__ __forceinline__ void load(Raw &r, int64_t p, int64_t id, int lane) const {
-        r.x = *(const Words *)(E.p + id * E.ld + lane * 16);
-        r.w = values ? values[p] : 1.f;
+    __device__ __forceinline__ void load(Raw &r, int64_t p, int id, int lane) const {
+        r.x = *(const Words *)((id < 0 ? no_x : E.p + id * E.ld) + lane * 16);
+        r.w = id < 0 || !values ? 1.f : values[p];
     }
-    __device__ __forceinline__ void load_map(Raw &r, int64_t p, int64_t id, int lane) const { load(r, p, id, lane); }
-    __device__ __forceinline__ void map(const Raw &r, bool some, float (&k)[N], float (&b)[N]) const {
+    __device__ __forceinline__ void load_map(Raw &r, int64_t p, int id, int lane) const { load(r, p, id, lane); }
+    __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&b)[N]) const {
         widen<BF, N>(r.x, b);
 #pragma unroll
         for (int c = 0; c < N; ++c) {
             k[c] = 1.f;
             b[c] *= r.w;
-        }
-        if (__any(!some)) {
-#pragma unroll
-            for (int c = 0; c < N; ++c) b[c] = some ? b[c] : 0.f;
         }
     }
     __device__ __forceinline__ void begin(int64_t, int, float (&s)[N]) const {
@@ -40,10 +37,8 @@ template <int D, bool BF> struct SumRows {
 };
 
 als_status launch_sum_rows(als_ctx *ctx, const als_csr *Y, const als_table *E, const als_table *X, hipStream_t s) {
-    // a table without rows: no entry has an item, and what is read in its place is somewhere that can be read
-    const RowsOf e = E->rows > 0 ? rows_of(E) : RowsOf{(char *)ctx->small.p, 0, E->dtype == ALS_BF16};
     pick_d(E->d, [&](auto d) {
-        pick(E->dtype == ALS_BF16, [&](auto bf) { launch_last(ctx, SumRows<d(), bf()>{e, rows_of(X), Y->values}, Y, s); });
+        pick(E->dtype == ALS_BF16, [&](auto bf) { launch_last(ctx, SumRows<d(), bf()>{rows_of(E), rows_of(X), Y->values, none_row(ctx, false, false)}, Y, s); });
     });
     ALS_HIP(ctx, hipGetLastError());
     return ALS_OK;
