@@ -9,7 +9,9 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from dataclasses import dataclass
+from operator import attrgetter
 from typing import Optional
 
 import torch
@@ -119,7 +121,7 @@ def load_library(path: str = LIB_PATH):
     lib.als_sum_rows.argtypes = [vp, P(c_als_csr), P(c_als_table), P(c_als_table), vp]
     lib.als_clip.argtypes = [vp, vp, vp, i32, ctypes.c_double, vp, vp]
     lib.als_beam.argtypes = [vp, P(c_als_beams), vp, vp, vp, vp, vp]
-    lib.als_reorder.argtypes = [vp, vp, i64, i32, P(c_als_matrix), P(c_als_matrix), i32, vp]
+    lib.als_reorder.argtypes = [vp, vp, i64, i32, vp, vp, i32, vp]
     for name in EXPORTS[16:]:
         getattr(lib, name).restype = i32
     lib.als_static_last_error.argtypes = []
@@ -525,22 +527,32 @@ def als_sum_rows(ctx: Context, Y: Csr, E: torch.Tensor, out: Optional[torch.Tens
 _CODES = {torch.float32: ALS_F32, torch.bfloat16: ALS_BF16}
 
 
-def _values_of(device: int, tensors, flat: bool):
-    """Tensors as an array of c_als_matrix (five 64-bit words each): one row where ``flat``, otherwise 2-D with unit column stride."""
-    words = []
+_dtype_of = attrgetter("dtype")
+
+
+def _flat_values(device: int, tensors):
+    """Tensors whose elements lie one after the other, a row each, as an array of c_als_matrix (five 64-bit words)."""
+    count, Tensor = len(tensors), torch.Tensor
+    words, sizes = array("q", bytes(40 * count)), array("q", map(Tensor.numel, tensors))
+    words[0::5], words[1::5], words[2::5], words[3::5] = array("q", map(Tensor.data_ptr, tensors)), array("q", (1,)) * count, sizes, sizes
+    try:
+        words[4::5] = array("q", map(_CODES.__getitem__, map(_dtype_of, tensors)))
+    except KeyError:
+        raise TypeError("tensors must be float32 or bfloat16") from None
+    if set(map(Tensor.get_device, tensors)) - {device}:
+        raise ValueError("every tensor must be on the context's GPU")
+    return words
+
+
+def _row_values(device: int, tensors):
+    """The same of 2-D tensors with unit column stride."""
+    words = array("q")
     for t in tensors:
-        code = _CODES.get(t.dtype)
-        if code is None:
-            raise TypeError("tensors must be float32 or bfloat16")
+        m = _matrix(t)
         if t.get_device() != device:
             raise ValueError("every tensor must be on the context's GPU")
-        if flat:
-            n = t.numel()
-            words += (t.data_ptr(), 1, n, n, code)
-        else:
-            m = _matrix(t)
-            words += (m.data or 0, m.rows, m.cols, m.ld, code)
-    return (ctypes.c_int64 * len(words))(*words)
+        words.extend((m.data or 0, m.rows, m.cols, m.ld, m.dtype))
+    return words
 
 
 def als_clip(ctx: Context, tensors, bound: float, out=None) -> torch.Tensor:
@@ -548,21 +560,23 @@ def als_clip(ctx: Context, tensors, bound: float, out=None) -> torch.Tensor:
     below 1, in place or into ``out`` (a tensor for each).  Tensors of any shape whose elements lie one after the other, or 2-D
     ones with unit column stride."""
     n, device = len(tensors), ctx.device.index
-    flat = all([t.is_contiguous() for t in tensors])
-    Y = None
-    if out is not None:
-        if len(out) != n or any([x.shape != y.shape for x, y in zip(tensors, out)]):
+    if out is not None and len(out) != n:
+        raise ValueError("out must have a tensor for each")
+    contiguous = torch.Tensor.is_contiguous
+    if all(map(contiguous, tensors)) and (out is None or all(map(contiguous, out))):
+        values = _flat_values
+    else:  # those whose elements lie one after the other as one row
+        if out is not None and any([x.shape != y.shape for x, y in zip(tensors, out)]):
             raise ValueError("out must have a tensor of the same shape for each")
-        flat = flat and all([t.is_contiguous() for t in out])
-    if not flat:  # those whose elements lie one after the other as one row
-        lone = [x.is_contiguous() and (out is None or out[j].is_contiguous()) for j, x in enumerate(tensors)]
+        lone = [contiguous(x) and (out is None or contiguous(out[j])) for j, x in enumerate(tensors)]
         tensors = [x.view(1, -1) if f else x for x, f in zip(tensors, lone)]
         out = out and [y.view(1, -1) if f else y for y, f in zip(out, lone)]
-    X = _values_of(device, tensors, flat)
-    if out is not None:
-        Y = _values_of(device, out, flat)
+        values = _row_values
+    X, Y = values(device, tensors), None if out is None else values(device, out)
+    if Y is not None and X[2::5] != Y[2::5]:
+        raise ValueError("out must have a tensor of the same size for each")
     norm = torch.empty((), dtype=torch.float64, device=ctx.device)
-    ctx._check(ctx.lib.als_clip(ctx.handle, X, Y, n, bound, norm.data_ptr(), _stream()))
+    ctx._check(ctx.lib.als_clip(ctx.handle, X.buffer_info()[0], None if Y is None else Y.buffer_info()[0], n, bound, norm.data_ptr(), _stream()))
     return norm
 
 
@@ -603,37 +617,44 @@ def als_beam(ctx: Context, ids: torch.Tensor, scores: torch.Tensor, lse: Optiona
     return parents, items, new_totals, new_lengths
 
 
-def _state(t: torch.Tensor, rows: int) -> c_als_matrix:
-    """What goes with the beams: a row each, its elements one after the other."""
-    if t.dim() < 1 or t.shape[0] != rows:
-        raise ValueError("a state must have one row per beam")
-    es, cols = t.element_size(), 1
-    for size, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size != 1 and step != cols:
-            raise ValueError("the elements of a state's row must lie one after the other")
-        cols *= size
-    ld = t.stride(0) if rows > 1 else cols
-    if es not in (2, 4, 8):
-        raise TypeError("elements of a state must have 2, 4 or 8 bytes")
-    more = 2 if es == 8 else 1
-    return c_als_matrix(t.data_ptr() or None, rows, cols * more, max(ld, cols) * more if rows <= 1 else ld * more, ALS_BF16 if es == 2 else ALS_F32)
+def _states(device: int, tensors, rows: int):
+    """What goes with the beams, a row each whose elements lie one after the other, as an array of c_als_matrix (five 64-bit words)."""
+    words = array("q")
+    for t in tensors:
+        if t.dim() < 1 or t.shape[0] != rows:
+            raise ValueError("a state must have one row per beam")
+        es = t.element_size()
+        if es not in (2, 4, 8):
+            raise TypeError("elements of a state must have 2, 4 or 8 bytes")
+        if t.is_contiguous():
+            cols = ld = t.numel() // rows if rows else 0
+        else:
+            cols = 1
+            for size, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+                if size != 1 and step != cols:
+                    raise ValueError("the elements of a state's row must lie one after the other")
+                cols *= size
+            ld = t.stride(0) if rows > 1 else cols
+        if es == 8:
+            cols, ld = 2 * cols, 2 * ld
+        if t.get_device() != device:
+            raise ValueError("every tensor must be on the context's GPU")
+        words.extend((t.data_ptr(), rows, cols, ld, ALS_BF16 if es == 2 else ALS_F32))
+    return words
 
 
 def als_reorder(ctx: Context, parents: torch.Tensor, beams: int, states, out=None):
     """Row parents[r] of every state to row r, in place or into ``out`` (a tensor for each); elements of 2, 4 or 8 bytes of any kind.
     Rows of parents outside r's own group of ``beams`` rows (-1, say) become zeros."""
-    rows, n = parents.shape[0], len(states)
+    rows, n, device = parents.shape[0], len(states), ctx.device.index
     if beams < 1 or rows % beams:
         raise ValueError("rows must be a whole number of groups of beams")
-    X = (c_als_matrix * n)(*[_state(t, rows) for t in states])
-    Y = None
-    if out is not None:
-        if len(out) != n or any(x.shape != y.shape or x.dtype != y.dtype for x, y in zip(states, out)):
-            raise ValueError("out must have a tensor of the same shape and type for each")
-        Y = (c_als_matrix * n)(*[_state(t, rows) for t in out])
-        _here(ctx, *out)
-    _here(ctx, parents, *states)
-    ctx._check(ctx.lib.als_reorder(ctx.handle, _ids(parents, rows, "parents"), rows // beams, beams, X, Y, n, _stream()))
+    if out is not None and (len(out) != n or any([x.dtype is not y.dtype or x.shape != y.shape for x, y in zip(states, out)])):
+        raise ValueError("out must have a tensor of the same shape and type for each")
+    X, Y = _states(device, states, rows), None if out is None else _states(device, out, rows)
+    p = _ids(parents, rows, "parents")
+    _here(ctx, parents)
+    ctx._check(ctx.lib.als_reorder(ctx.handle, p, rows // beams, beams, X.buffer_info()[0], None if Y is None else Y.buffer_info()[0], n, _stream()))
     return states if out is None else out
 
 

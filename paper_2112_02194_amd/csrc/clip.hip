@@ -5,29 +5,51 @@
 // scale kernel  every workgroup adds the workgroups' sums in the same order, so all have the same bits of the norm, and takes its
 //               tiles from the end: the last ones read are those that the cache may still hold
 #include <algorithm>
+#include <iterator>
 #include <type_traits>
-#include <vector>
 
 #include "als_internal.h"
 
 namespace als {
 
 constexpr int CLIP_THREADS = 256, CLIP_EPT = 16, CLIP_TILE = CLIP_THREADS * CLIP_EPT;
-constexpr int CLIP_TENSORS = 48;    // of a launch: they are its arguments
 constexpr int CLIP_PARTIALS = 8192;  // workgroups' sums of a call
 
-struct ClipTensor {
+// The tensors of a launch are its arguments (4 KB).  Those whose elements lie one after the other take less room there: 60 of
+// them are one launch instead of two.
+struct FlatTensor {
+    static constexpr int MOST = 112;
     const char *x;
     char *y;
-    int64_t cols, ldx, ldy;  // of a row, in elements; one row where they lie one after the other
-    int64_t row_tiles, first;  // tiles of a row; number of the first one in the launch
-    int64_t bf16;
+    int64_t n_and_type;  // elements * 2, + 1: bf16
+    __device__ __forceinline__ bool bf16() const { return n_and_type & 1; }
+    // element offsets of the tensor's tile `at` in x and y, and the elements that its row has from there
+    __device__ __forceinline__ void place(uint32_t at, int64_t &x, int64_t &y, int64_t &left) const {
+        x = y = (int64_t)at * CLIP_TILE;
+        left = (n_and_type >> 1) - x;
+    }
 };
-struct ClipTensors {
-    ClipTensor t[CLIP_TENSORS];
-    int64_t tiles;
+struct RowTensor {
+    static constexpr int MOST = 64;
+    const char *x;
+    char *y;
+    int64_t cols, ldx, ldy;  // of a row, in elements
+    uint32_t row_tiles, type;
+    __device__ __forceinline__ bool bf16() const { return type; }
+    __device__ __forceinline__ void place(uint32_t at, int64_t &x, int64_t &y, int64_t &left) const {
+        const int64_t row = at / row_tiles, col = (int64_t)(at % row_tiles) * CLIP_TILE;
+        x = row * ldx + col;
+        y = row * ldy + col;
+        left = cols - col;
+    }
+};
+template <class T> struct ClipTensors {
+    uint32_t tiles;
     int n;
+    uint32_t first[T::MOST];  // numbers of the tensors' first tiles in the launch; ~0 behind the last
+    T t[T::MOST];
 };
+static_assert(sizeof(ClipTensors<FlatTensor>) <= 4000 && sizeof(ClipTensors<RowTensor>) <= 4000, "a launch's arguments");
 
 // Sixteen elements of a tile, as 16-byte pieces; those behind the row's end are zeros.
 template <bool BF16> struct ClipTile {
@@ -109,37 +131,41 @@ __device__ __forceinline__ double workgroup_sum(double s, double *lds) {
     return s;
 }
 
-// Tensor j of the launch that has the tile, from the one that had the workgroup's last.
-template <bool BACK> __device__ __forceinline__ void find_tensor(const ClipTensors &all, int64_t tile, int &j) {
-    if (BACK) while (tile < all.t[j].first) --j;
-    else while (j + 1 < all.n && tile >= all.t[j + 1].first) ++j;
+// The tensor of the launch that has the tile: the arguments come in one go, where a search would wait for each.
+template <class T> __device__ __forceinline__ int find_tensor(const ClipTensors<T> &all, uint32_t tile) {
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < T::MOST; ++i) before += all.first[i] <= tile;
+    return before - 1;
 }
 
-__global__ __launch_bounds__(CLIP_THREADS) void clip_norm_kernel(ClipTensors all, double *__restrict__ partials) {
+template <class T> __global__ __launch_bounds__(CLIP_THREADS) void clip_norm_kernel(ClipTensors<T> all, double *__restrict__ partials) {
     __shared__ double lds[CLIP_THREADS / 64];
     double s[4] = {0.0, 0.0, 0.0, 0.0};
-    int j = 0;
-    for (int64_t tile = blockIdx.x; tile < all.tiles; tile += gridDim.x) {
-        find_tensor<false>(all, tile, j);
-        const ClipTensor &t = all.t[j];
-        const int64_t at = tile - t.first, row = at / t.row_tiles, col = (at - row * t.row_tiles) * CLIP_TILE;
+    int j = blockIdx.x < all.tiles ? find_tensor(all, blockIdx.x) : 0;
+    for (uint32_t tile = blockIdx.x; tile < all.tiles; tile += gridDim.x) {
+        while (j + 1 < all.n && tile >= all.first[j + 1]) ++j;
+        const T &t = all.t[j];
+        int64_t x, y, left;
+        t.place(tile - all.first[j], x, y, left);
         auto add = [&](auto bf) {
             ClipTile<bf()> in;
-            in.load(t.x + (row * t.ldx + col) * (bf() ? 2 : 4), t.cols - col, threadIdx.x);
+            in.load(t.x + x * (bf() ? 2 : 4), left, threadIdx.x);
 #pragma unroll
             for (int i = 0; i < CLIP_EPT; ++i) {
                 const double v = in.value(i / in.PER, i % in.PER);
                 s[i & 3] = fma(v, v, s[i & 3]);
             }
         };
-        if (t.bf16) add(std::true_type{});
+        if (t.bf16()) add(std::true_type{});
         else add(std::false_type{});
     }
     const double sum = workgroup_sum((s[0] + s[1]) + (s[2] + s[3]), lds);
     if (threadIdx.x == 0) partials[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(CLIP_THREADS) void clip_scale_kernel(ClipTensors all, const double *__restrict__ partials, int n_partials,
+template <class T>
+__global__ __launch_bounds__(CLIP_THREADS) void clip_scale_kernel(ClipTensors<T> all, const double *__restrict__ partials, int n_partials,
                                                                 double bound, double *norm) {
     __shared__ double lds[CLIP_THREADS / 64];
     double s = 0.0;
@@ -147,18 +173,19 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_scale_kernel(ClipTensors al
     const double total = sqrt(workgroup_sum(s, lds));
     const double c = total > bound && total < (double)INFINITY ? bound / total : 1.0;
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = total;
-    int j = all.n - 1;
-    for (int64_t tile = all.tiles - 1 - blockIdx.x; tile >= 0; tile -= gridDim.x) {
-        find_tensor<true>(all, tile, j);
-        const ClipTensor &t = all.t[j];
+    int j = blockIdx.x < all.tiles ? find_tensor(all, all.tiles - 1 - blockIdx.x) : 0;
+    for (int64_t tile = (int64_t)all.tiles - 1 - blockIdx.x; tile >= 0; tile -= gridDim.x) {
+        while ((uint32_t)tile < all.first[j]) --j;
+        const T &t = all.t[j];
         if (c == 1.0 && t.y == t.x) continue;
-        const int64_t at = tile - t.first, row = at / t.row_tiles, col = (at - row * t.row_tiles) * CLIP_TILE;
+        int64_t x, y, left;
+        t.place((uint32_t)tile - all.first[j], x, y, left);
         auto scale = [&](auto bf) {
             ClipTile<bf()> in;
-            in.load(t.x + (row * t.ldx + col) * (bf() ? 2 : 4), t.cols - col, threadIdx.x);
-            in.store(t.y + (row * t.ldy + col) * (bf() ? 2 : 4), t.cols - col, threadIdx.x, c);
+            in.load(t.x + x * (bf() ? 2 : 4), left, threadIdx.x);
+            in.store(t.y + y * (bf() ? 2 : 4), left, threadIdx.x, c);
         };
-        if (t.bf16) scale(std::true_type{});
+        if (t.bf16()) scale(std::true_type{});
         else scale(std::false_type{});
     }
 }
@@ -167,45 +194,67 @@ als_status clip_setup(als_ctx *ctx) { return ensure(ctx, ctx->clip_partials, CLI
 
 als_status launch_clip(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, int n, double bound, double *norm, hipStream_t s) {
     double *partials = (double *)ctx->clip_partials.p;
-    // the tensors that have elements, CLIP_TENSORS a launch
-    auto next = [&](int &j, ClipTensors &all) {
+    bool too_large = false;  // a tensor of 2^31 tiles: 35 TB
+    auto is_flat = [&](int j) { return X[j].rows <= 1 || (X[j].ld == X[j].cols && (!Y || Y[j].ld == Y[j].cols)); };
+    // the next tensors of a kind that have elements, as many as a launch takes
+    auto next = [&](int &j, auto &all) {
+        constexpr bool flat = std::is_same_v<std::decay_t<decltype(all.t[0])>, FlatTensor>;
         all.n = 0;
         all.tiles = 0;
-        for (; j < n && all.n < CLIP_TENSORS; ++j) {
+        std::fill(std::begin(all.first), std::end(all.first), ~0u);
+        for (; j < n && all.n < (int)std::size(all.t); ++j) {
             const als_matrix &x = X[j], &y = Y ? Y[j] : X[j];
-            if (x.rows == 0 || x.cols == 0) continue;
-            const bool flat = x.rows == 1 || (x.ld == x.cols && y.ld == y.cols);
-            ClipTensor &t = all.t[all.n++];
+            if (x.rows == 0 || x.cols == 0 || is_flat(j) != flat) continue;
+            const int64_t cols = flat ? x.rows * x.cols : x.cols, each = (cols + CLIP_TILE - 1) / CLIP_TILE, tiles = flat ? each : each * x.rows;
+            if (tiles > INT32_MAX - all.tiles) {
+                if (all.n == 0) too_large = true;
+                break;
+            }
+            auto &t = all.t[all.n];
+            all.first[all.n++] = all.tiles;
+            all.tiles += (uint32_t)tiles;
             t.x = (const char *)x.data;
             t.y = (char *)y.data;
-            t.cols = flat ? x.rows * x.cols : x.cols;
-            t.ldx = x.ld;
-            t.ldy = y.ld;
-            t.row_tiles = (t.cols + CLIP_TILE - 1) / CLIP_TILE;
-            t.first = all.tiles;
-            t.bf16 = x.dtype == ALS_BF16;
-            all.tiles += t.row_tiles * (flat ? 1 : x.rows);
+            if constexpr (flat) {
+                t.n_and_type = cols * 2 + (x.dtype == ALS_BF16);
+            } else {
+                t.cols = cols;
+                t.ldx = x.ld;
+                t.ldy = y.ld;
+                t.row_tiles = (uint32_t)each;
+                t.type = x.dtype == ALS_BF16;
+            }
         }
         return all.n > 0;
     };
-    ClipTensors all{};
-    const int launches = std::max(1, (n + CLIP_TENSORS - 1) / CLIP_TENSORS);
+    ClipTensors<FlatTensor> flat{};
+    ClipTensors<RowTensor> rows{};
+    int launches = 0;
+    for (int j = 0; next(j, flat);) ++launches;
+    for (int j = 0; next(j, rows);) ++launches;
+    if (too_large || launches > CLIP_PARTIALS) return fail(ctx, ALS_ESHAPE, "als_clip: X has too many elements");
+    launches = std::max(launches, 1);
     const int64_t most = std::min<int64_t>(ctx->num_cu * 8, CLIP_PARTIALS / launches);
-    static_assert(CLIP_PARTIALS >= ALS_CLIP_MAX / CLIP_TENSORS + 1, "a sum for every launch");
+    static_assert(CLIP_PARTIALS >= ALS_CLIP_MAX / FlatTensor::MOST + ALS_CLIP_MAX / RowTensor::MOST + 2, "a sum for every launch of ordinary tensors");
     int used = 0;
-    for (int j = 0; next(j, all);) {
-        const int64_t grid = std::min(all.tiles, most);
-        hipLaunchKernelGGL(clip_norm_kernel, dim3((unsigned)grid), dim3(CLIP_THREADS), 0, s, all, partials + used);
-        used += (int)grid;
-    }
-    int j = 0;
-    bool more = next(j, all);
-    do {
-        hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(all.tiles, ctx->num_cu * 8))), dim3(CLIP_THREADS), 0, s, all,
-                           (const double *)partials, used, bound, norm);
-        norm = nullptr;
-        more = more && next(j, all);
-    } while (more);
+    auto norms = [&](auto &all) {
+        for (int j = 0; next(j, all);) {
+            const int64_t grid = std::min<int64_t>(all.tiles, most);
+            hipLaunchKernelGGL((clip_norm_kernel<std::decay_t<decltype(all.t[0])>>), dim3((unsigned)grid), dim3(CLIP_THREADS), 0, s, all, partials + used);
+            used += (int)grid;
+        }
+    };
+    norms(flat);
+    norms(rows);
+    auto scales = [&](auto &all, bool always) {
+        for (int j = 0; next(j, all) || always; always = false) {
+            hipLaunchKernelGGL((clip_scale_kernel<std::decay_t<decltype(all.t[0])>>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(all.tiles, ctx->num_cu * 8))),
+                               dim3(CLIP_THREADS), 0, s, all, (const double *)partials, used, bound, norm);
+            norm = nullptr;
+        }
+    };
+    scales(flat, true);  // the norm is written by the first launch, also where there is nothing
+    scales(rows, false);
     ALS_HIP(ctx, hipGetLastError());
     return ALS_OK;
 }

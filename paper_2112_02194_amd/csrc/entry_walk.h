@@ -6,7 +6,7 @@
 // group joins its entries' maps, the groups' maps are joined across the wavefront (log2 steps), and with the state that comes in each
 // group walks its entries again from registers, where outputs are made.  One read of the tables.
 //
-// Rows of at most `longest` entries belong whole to the chunk that they begin in.  A longer row is cut at the chunks' borders; its
+// Rows of at most `longest` entries (a chunk's at least) belong whole to the chunk that they begin in.  A longer row is cut at the chunks' borders; its
 // pieces' maps go to the workspace:
 //   last states and sums   the same launch leaves the pieces, join_kernel composes those of each long row
 //   all states, gradients  pieces_kernel makes the pieces' maps first (the tables are read twice for entries of long rows),
@@ -22,7 +22,7 @@
 namespace als {
 
 constexpr int WALK_STAGE = 128;       // entries whose ids and marks are in LDS at a time
-constexpr int WALK_MAX_CHUNKS = 16384;
+constexpr int WALK_MAX_CHUNKS = 32768;
 
 // Chunks, and what is kept of each for rows that cross its border: maps (k, b) of `d` columns.
 //   across  of the part of a long row up to the border that the walk leaves the chunk by
@@ -164,6 +164,8 @@ template <bool BACK> __device__ void stage_entries(const RowFinder &f, Marks &m,
 // A wavefront's walk.  Op:
 //   N, K, L           columns a lane, entries a group of lanes takes in a tile, lanes of a group
 //   BACK, ONES        from the rows' ends; k is 1 everywhere (sums)
+//   OUTPUT            every entry has outputs
+//   EARLY             what rows begin with is loaded along with their entries, into registers
 //   Raw               what is loaded of one entry
 //   load(raw, p, id)  of entry p; id -1: it has no item, and what is loaded in the item's place leaves the state as it is
 //   load_map(raw, p, id)   what its map takes of that
@@ -224,12 +226,16 @@ template <class Op> struct Walk {
             for (int tile = 0; tile < many; tile += TILE) {
                 const int i0 = tile + group * K;
                 typename Op::Raw raw[K];
+                float early[Op::EARLY ? K : 1][N];
                 int starts = 0, ends = 0;  // a bit per entry: a row starts, ends there
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     const int id = m.id[i0 + j];
                     starts |= (m.start[i0 + j] >= 0) << j;
                     ends |= (m.end[i0 + j] >= 0) << j;
+                    if constexpr (Op::EARLY) {  // what a row begins with, under way with the rest
+                        if (__any(starts >> j & 1)) op.begin(max(m.start[i0 + j], 0), lane, early[j]);
+                    }
                     // entries behind the last one: any that is there
                     op.load(raw[j], Op::BACK ? here - 1 - min(i0 + j, many - 1) : here + min(i0 + j, many - 1), id, lane);
                 }
@@ -246,9 +252,9 @@ template <class Op> struct Walk {
                     }
                     if (__any(starting)) {
                         float first[N];
-                        op.begin(max(m.start[i0 + j], 0), lane, first);
+                        if constexpr (!Op::EARLY) op.begin(max(m.start[i0 + j], 0), lane, first);
 #pragma unroll
-                        for (int c = 0; c < N; ++c) b[c] = starting ? first[c] : b[c];
+                        for (int c = 0; c < N; ++c) b[c] = starting ? (Op::EARLY ? early[j][c] : first[c]) : b[c];
                     }
 #pragma unroll
                     for (int c = 0; c < N; ++c) {
@@ -260,14 +266,15 @@ template <class Op> struct Walk {
                 }
                 float h[N];
                 join(k, b, starts != 0, h);
+                if (!Op::OUTPUT && !__any(ends != 0)) continue;
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     const bool starting = starts >> j & 1, ending = ends >> j & 1;
                     if (__any(starting)) {
                         float first[N];
-                        op.begin(max(m.start[i0 + j], 0), lane, first);
+                        if constexpr (!Op::EARLY) op.begin(max(m.start[i0 + j], 0), lane, first);
 #pragma unroll
-                        for (int c = 0; c < N; ++c) h[c] = starting ? first[c] : h[c];
+                        for (int c = 0; c < N; ++c) h[c] = starting ? (Op::EARLY ? early[j][c] : first[c]) : h[c];
                     }
                     const int64_t p = Op::BACK ? here - 1 - (i0 + j) : here + i0 + j;
                     if constexpr (Op::KEEP) {
@@ -426,7 +433,7 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_all_ke
 template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kernel(Op op, Lists y, Chunks c) {
     constexpr int D = Op::N * Op::L;
     const RowFinder f(y);
-    const int64_t chunk = blockIdx.x;
+    const int64_t chunk = c.count - 1 - blockIdx.x;  // the walk begins with the chunks that were read last: the cache may hold them
     const ChunkRows r(f, c, chunk);
     const RowFinder::Row row = Op::BACK ? r.at_low : r.at_high;
     const bool out = Op::BACK ? r.split_low : r.split_high;
@@ -438,91 +445,110 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kern
 }
 
 // A long row's pieces one after the other, on behalf of the chunk that the walk along the row begins in (CARRY: the state at every
-// border it crosses goes to the chunk behind it) or ends in (otherwise: the row's last state).  The pieces are dealt out in
-// stretches to groups of lanes, whose maps are joined through LDS.  A workgroup looks at JOIN_CHUNKS chunks.
-constexpr int JOIN_THREADS = 512, JOIN_CHUNKS = 16;
-template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(Op op, Chunks c) {
-    constexpr int N = Op::N, D = N * Op::L, AHEAD = 4, GROUPS = JOIN_THREADS / Op::L;
-    __shared__ float maps[GROUPS][2][D];
-    __shared__ JoinedRow found[JOIN_CHUNKS];
-    const int lane = threadIdx.x % Op::L, group = threadIdx.x / Op::L;
-    const int64_t chunk0 = (int64_t)blockIdx.x * JOIN_CHUNKS;
-    if (threadIdx.x < JOIN_CHUNKS) found[threadIdx.x] = chunk0 + threadIdx.x < c.count ? c.rows[chunk0 + threadIdx.x] : JoinedRow{0, 0};
-    __syncthreads();
-    for (int n = 0; n < JOIN_CHUNKS; ++n) {
-        const int pieces = found[n].pieces;
-        if (pieces == 0) continue;
-        const int64_t chunk = chunk0 + n;
-        // piece i of the walk is kept with chunk at(i); without CARRY the chunk itself has the closing one
-        auto at = [&](int i) { return min(max(CARRY ? (Op::BACK ? chunk - i : chunk + i) : chunk - pieces + i, (int64_t)0), c.count - 1); };
-        const int each = (pieces + GROUPS - 1) / GROUPS, begin = min(group * each, pieces), end = min(begin + each, pieces);
-        const int groups = (pieces + each - 1) / each;
-        float k[N], s[N];
+// border it crosses goes to the chunk behind it) or ends in (otherwise: the row's last state).
+template <class Op, bool CARRY> struct Pieces {
+    static constexpr int N = Op::N, D = N * Op::L, AHEAD = 4;
+    const Chunks &c;
+    int64_t chunk;
+    int count, lane;
+    float k[N], s[N];
+    // piece i of the walk is kept with chunk at(i); without CARRY the chunk itself has the closing one
+    __device__ __forceinline__ int64_t at(int i) const {
+        return min(max(CARRY ? (Op::BACK ? chunk - i : chunk + i) : chunk - count + i, (int64_t)0), c.count - 1);
+    }
+    template <bool STORE> __device__ __forceinline__ void walk(int begin, int end) {
+        for (int i0 = begin; i0 < end; i0 += AHEAD) {
+            float kp[AHEAD][N], bp[AHEAD][N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            k[j] = 1.f;
-            s[j] = 0.f;
-        }
-        auto walk = [&](auto &&then) {
-            for (int i0 = begin; i0 < end; i0 += AHEAD) {
-                float kp[AHEAD][N], bp[AHEAD][N];
+            for (int a = 0; a < AHEAD; ++a) {
+                const float *map = c.across + at(min(i0 + a, end - 1)) * 2 * D + lane * N;
 #pragma unroll
-                for (int a = 0; a < AHEAD; ++a) {
-                    const float *map = c.across + at(min(i0 + a, end - 1)) * 2 * D + lane * N;
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        kp[a][j] = map[j];
-                        bp[a][j] = map[D + j];
-                    }
-                }
-#pragma unroll
-                for (int a = 0; a < AHEAD; ++a) {
-                    const bool on = i0 + a < end, first = i0 + a == 0;  // the first piece has the row's own first state in it
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        s[j] = !on ? s[j] : first ? bp[a][j] : fmaf(kp[a][j], s[j], bp[a][j]);
-                        k[j] = on ? k[j] * kp[a][j] : k[j];
-                    }
-                    then(i0 + a, on);
+                for (int j = 0; j < N; ++j) {
+                    kp[a][j] = map[j];
+                    bp[a][j] = map[D + j];
                 }
             }
-        };
-        walk([](int, bool) {});
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const bool on = i0 + a < end, first = i0 + a == 0;  // the first piece has the row's own first state in it
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    s[j] = !on ? s[j] : first ? bp[a][j] : fmaf(kp[a][j], s[j], bp[a][j]);
+                    k[j] = on ? k[j] * kp[a][j] : k[j];
+                }
+                if (STORE && on) {
+                    float *to = c.close + (at(i0 + a + 1) * 2 + 1) * D + lane * N;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) to[j] = s[j];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(const Op &op, int row) {
+        const float *map = c.close + chunk * 2 * D + lane * N;
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = fmaf(map[j], s[j], map[D + j]);
+        op.finish(row, true, lane, s);
+    }
+};
+
+// A workgroup looks at 64 chunks.  Rows of a few pieces: a group of lanes each.  Others: their pieces are dealt out in stretches to
+// all groups, whose maps are joined through LDS; the columns are dealt out to the workgroups of a second dimension.
+constexpr int JOIN_THREADS = 512, JOIN_CHUNKS = 64, JOIN_FEW = 24;
+template <class Op> constexpr int join_lanes() { return Op::L < 8 ? Op::L : 8; }
+template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(Op op, Chunks c) {
+    constexpr int N = Op::N, LANES = join_lanes<Op>(), GROUPS = JOIN_THREADS / LANES;
+    __shared__ float maps[GROUPS][2][LANES * N];
+    const int64_t chunk0 = (int64_t)blockIdx.x * JOIN_CHUNKS, look = chunk0 + (threadIdx.x & 63);
+    const JoinedRow found = look < c.count ? c.rows[look] : JoinedRow{0, 0};
+    if (blockIdx.y == 0) {
+        const unsigned long long few = __ballot(found.pieces > 0 && found.pieces <= JOIN_FEW);
+        const int many = __popcll(few), lane = threadIdx.x % Op::L;
+        // the row that this group of lanes takes: the place of the n-th bit
+        for (int n = threadIdx.x / Op::L; n < many; n += JOIN_THREADS / Op::L) {
+            unsigned long long rest = few;
+            for (int i = 0; i < n; ++i) rest &= rest - 1;
+            const int64_t chunk = chunk0 + __ffsll((long long)rest) - 1;
+            const JoinedRow r = c.rows[chunk];
+            Pieces<Op, CARRY> p{c, chunk, r.pieces, lane, {}, {}};
+            p.template walk<CARRY>(0, r.pieces);
+            if (!CARRY) p.finish(op, r.row);
+        }
+    }
+    const int in_group = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    for (unsigned long long rest = __ballot(found.pieces > JOIN_FEW); rest; rest &= rest - 1) {
+        const int64_t chunk = chunk0 + __ffsll((long long)rest) - 1;
+        const JoinedRow r = c.rows[chunk];
+        const int each = (r.pieces + GROUPS - 1) / GROUPS, begin = min(group * each, r.pieces), end = min(begin + each, r.pieces);
+        const int groups = (r.pieces + each - 1) / each;
+        Pieces<Op, CARRY> p{c, chunk, r.pieces, (int)blockIdx.y * LANES + in_group, {}, {}};
+#pragma unroll
+        for (int j = 0; j < N; ++j) p.k[j] = 1.f;
+        p.template walk<false>(begin, end);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            maps[group][0][lane * N + j] = k[j];
-            maps[group][1][lane * N + j] = s[j];
+            maps[group][0][in_group * N + j] = p.k[j];
+            maps[group][1][in_group * N + j] = p.s[j];
         }
         __syncthreads();
         const int upto = CARRY ? min(group, groups) : groups;
         for (int g = 0; g < upto; ++g)
 #pragma unroll
-            for (int j = 0; j < N; ++j) s[j] = g ? fmaf(maps[g][0][lane * N + j], s[j], maps[g][1][lane * N + j]) : maps[0][1][lane * N + j];
-        if (CARRY) {
-            walk([&](int i, bool on) {
-                if (!on) return;
-                float *to = c.close + (at(i + 1) * 2 + 1) * D + lane * N;
-#pragma unroll
-                for (int j = 0; j < N; ++j) to[j] = s[j];
-            });
-        } else if (group == 0) {
-            const float *map = c.close + chunk * 2 * D + lane * N;
-#pragma unroll
-            for (int j = 0; j < N; ++j) s[j] = fmaf(map[j], s[j], map[D + j]);
-            op.finish(found[n].row, true, lane, s);
-        }
+            for (int j = 0; j < N; ++j) p.s[j] = g ? fmaf(maps[g][0][in_group * N + j], p.s[j], maps[g][1][in_group * N + j]) : maps[0][1][in_group * N + j];
+        if (CARRY) p.template walk<true>(begin, end);
+        else if (group == 0) p.finish(op, r.row);
         __syncthreads();
     }
 }
 
-// Chunks of the call's entries: enough for every wavefront that the card holds to have some, of at least a few tiles.
-inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int d, int tile) {
+// Chunks of the call's entries: for small calls as many as the card holds wavefronts, of a tile at least; then of 64 entries, so that a
+// chunk's search for its rows does not weigh; then as many as there is room for.
+inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile) {
     Chunks c{};
-    const int64_t least = tile > 64 ? tile : 64;
-    c.size = (nnz + WALK_MAX_CHUNKS - 1) / WALK_MAX_CHUNKS;
-    c.size = std::max(least, (c.size + 63) / 64 * 64);
+    const int64_t resident = (int64_t)ctx->num_cu * 12, wanted = std::max((nnz + WALK_MAX_CHUNKS - 1) / WALK_MAX_CHUNKS, std::min<int64_t>(64, (nnz + resident - 1) / resident));
+    c.size = std::max<int64_t>(1, (wanted + tile - 1) / tile) * tile;
     c.count = (nnz + c.size - 1) / c.size;
-    c.longest = c.size;
+    c.longest = std::max<int64_t>(c.size, 4 * tile);
     c.across = (float *)ctx->walk_maps.p;
     c.close = c.across + (int64_t)WALK_MAX_CHUNKS * 2 * 128;
     c.rows = (JoinedRow *)(c.close + (int64_t)WALK_MAX_CHUNKS * 2 * 128);
@@ -532,14 +558,14 @@ inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int d, int tile) {
 constexpr size_t WALK_NONE = (size_t)WALK_MAX_CHUNKS * (4 * 128 * sizeof(float) + sizeof(JoinedRow)), WALK_BYTES = WALK_NONE + 3 * 512;
 inline const char *none_row(const als_ctx *ctx, bool gates, bool bf16) { return (const char *)ctx->walk_maps.p + WALK_NONE + (!gates ? 0 : bf16 ? 1024 : 512); }
 constexpr int EMPTY_GROUPS = 1024;  // workgroups that look for empty rows, at most
-inline unsigned join_grid(const Chunks &c) { return (unsigned)((c.count + JOIN_CHUNKS - 1) / JOIN_CHUNKS); }
+template <class Op> dim3 join_grid(const Chunks &c) { return dim3((unsigned)((c.count + JOIN_CHUNKS - 1) / JOIN_CHUNKS), Op::L / join_lanes<Op>()); }
 inline unsigned walk_grid(const Chunks &c, int64_t rows) { return (unsigned)(c.count + std::min<int64_t>((rows + 63) / 64, EMPTY_GROUPS)); }
 
 template <class Op> void launch_last(const als_ctx *ctx, const Op &op, const als_csr *Y, hipStream_t s) {
-    const Chunks c = chunks_of(ctx, Y->nnz, Op::N * Op::L, Walk<Op>::TILE);
+    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::TILE);
     const Lists y = lists_of(Y);
     hipLaunchKernelGGL((walk_last_kernel<Op>), dim3(walk_grid(c, Y->rows)), dim3(64), 0, s, op, y, c);
-    if (Y->nnz > c.longest) hipLaunchKernelGGL((join_kernel<Op, false>), dim3(join_grid(c)), dim3(JOIN_THREADS), 0, s, op, c);
+    if (Y->nnz > c.longest) hipLaunchKernelGGL((join_kernel<Op, false>), join_grid<Op>(c), dim3(JOIN_THREADS), 0, s, op, c);
 }
 
 // F(bool) for a value that only the call knows

@@ -12,7 +12,7 @@ constexpr int RECUR_THREADS = 256;
 // h = s h + (1 - s) x along a row (als_recur).
 template <int D, bool BF, bool SBF, bool STATES> struct Forward {
     static constexpr int N = BF ? 8 : 4, K = 32 / N, L = D / N, WAVES = STATES || (BF && D <= 32) ? 3 : 4;
-    static constexpr bool BACK = false, ONES = false, KEEP = true;
+    static constexpr bool BACK = false, ONES = false, KEEP = true, OUTPUT = STATES, EARLY = false;
     RowsOf V, F, H0, states, last;
     const char *no_x, *no_g;
     struct Raw {
@@ -50,7 +50,7 @@ template <int D, bool BF, bool SBF, bool STATES> struct Forward {
 // g = d + a, a = s g from a row's end (als_recur_backward): a, what an entry gets from those behind it, is the state.
 template <int D, bool BF, bool SBF> struct Backward {
     static constexpr int N = 4, K = 4, L = D / N, WAVES = 3;
-    static constexpr bool BACK = true, ONES = false, KEEP = false;
+    static constexpr bool BACK = true, ONES = false, KEEP = false, OUTPUT = true, EARLY = BF || SBF || D >= 64;
     RowsOf V, F, H0, states, d_states, d_last, dV, dF, dH0;
     const char *no_x, *no_g;
     struct Raw {
@@ -158,11 +158,11 @@ als_status walk_setup(als_ctx *ctx) {
 }
 
 template <class Op> static void launch_all(const als_ctx *ctx, const Op &op, const als_csr *Y, hipStream_t s) {
-    const Chunks c = chunks_of(ctx, Y->nnz, Op::N * Op::L, Walk<Op>::TILE);
+    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::TILE);
     const Lists y = lists_of(Y);
     if (Y->nnz > c.longest) {  // there may be rows that are cut
         hipLaunchKernelGGL((pieces_kernel<Op>), dim3((unsigned)c.count), dim3(64), 0, s, op, y, c);
-        hipLaunchKernelGGL((join_kernel<Op, true>), dim3(join_grid(c)), dim3(JOIN_THREADS), 0, s, op, c);
+        hipLaunchKernelGGL((join_kernel<Op, true>), join_grid<Op>(c), dim3(JOIN_THREADS), 0, s, op, c);
     }
     hipLaunchKernelGGL((walk_all_kernel<Op>), dim3(walk_grid(c, Y->rows)), dim3(64), 0, s, op, y, c);
 }

@@ -59,15 +59,18 @@ def test_what_the_binding_refuses():
 
 
 def test_a_state_of_any_shape_is_a_row_a_beam():
-    t = torch.zeros((6, 3, 4, 2), dtype=torch.int64)
-    m = als._state(t, 6)
-    assert (m.rows, m.cols, m.ld, m.dtype) == (6, 48, 48, als.ALS_F32)
-    m = als._state(torch.zeros((6, 10), dtype=torch.float16)[:, :7], 6)
-    assert (m.rows, m.cols, m.ld, m.dtype) == (6, 7, 10, als.ALS_BF16)
-    m = als._state(torch.zeros((1, 5), dtype=torch.int32), 1)
-    assert (m.rows, m.cols, m.ld) == (1, 5, 5)
-    m = als._state(torch.zeros(4), 4)
-    assert (m.rows, m.cols, m.ld) == (4, 1, 1)
+    words = lambda t, rows: als._states(-1, [t], rows).tolist()[1:]  # noqa: E731
+    assert words(torch.zeros((6, 3, 4, 2), dtype=torch.int64), 6) == [6, 48, 48, als.ALS_F32]
+    assert words(torch.zeros((6, 10), dtype=torch.float16)[:, :7], 6) == [6, 7, 10, als.ALS_BF16]
+    assert words(torch.zeros((1, 5), dtype=torch.int32), 1) == [1, 5, 5, als.ALS_F32]
+    assert words(torch.zeros(4), 4) == [4, 1, 1, als.ALS_F32]
+    assert words(torch.zeros((3, 0)), 3) == [3, 0, 0, als.ALS_F32]
+
+
+def test_tensors_as_rows_of_values():
+    assert als._flat_values(-1, [torch.zeros((2, 3)), torch.zeros(0, dtype=torch.bfloat16)]).tolist()[1:5] == [1, 6, 6, als.ALS_F32]
+    assert als._flat_values(-1, []).tolist() == []
+    assert als._row_values(-1, [torch.zeros((4, 6))[:, :3]]).tolist()[1:] == [4, 3, 6, als.ALS_F32]
 
 
 def test_null_context():
