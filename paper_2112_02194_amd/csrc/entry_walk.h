@@ -22,6 +22,7 @@
 namespace als {
 
 constexpr int WALK_STAGE = 128;       // entries whose ids and marks are in LDS at a time
+constexpr int LAST_STAGE = 512;       // the same where only last states are wanted: the groups' maps are joined once a stage
 constexpr int WALK_MAX_CHUNKS = 32768;
 
 // Chunks, and what is kept of each for rows that cross its border: maps (k, b) of `d` columns.
@@ -37,8 +38,8 @@ struct Chunks {
     JoinedRow *rows;          // [count]
 };
 
-struct Marks {
-    int32_t id[WALK_STAGE], start[WALK_STAGE], end[WALK_STAGE];  // item, or -1; row that begins, ends there in the walk, or -1
+template <int STAGE> struct Marks {
+    int32_t id[STAGE], start[STAGE], end[STAGE];  // item, or -1; row that begins, ends there in the walk, or -1
 };
 
 // A value that all lanes of the wavefront have.
@@ -122,11 +123,11 @@ struct ChunkRows {
 
 // Ids and marks of entries i = 0 .. n-1 of the walk from `from` on (down from from - 1 where BACK).  `row`: where the search for rows
 // begins, moved along.  Workgroups are single wavefronts.
-template <bool BACK> __device__ void stage_entries(const RowFinder &f, Marks &m, int64_t from, int n, int64_t &row) {
+template <bool BACK, int STAGE> __device__ void stage_entries(const RowFinder &f, Marks<STAGE> &m, int64_t from, int n, int64_t &row) {
     const int lane = threadIdx.x;
     __syncthreads();
-#pragma unroll
-    for (int i = lane; i < WALK_STAGE; i += 64) {
+#pragma unroll 2
+    for (int i = lane; i < STAGE; i += 64) {
         int id = -1;
         if (i < n) {
             const int64_t p = BACK ? from - 1 - i : from + i;
@@ -164,7 +165,7 @@ template <bool BACK> __device__ void stage_entries(const RowFinder &f, Marks &m,
 // A wavefront's walk.  Op:
 //   N, K, L           columns a lane, entries a group of lanes takes in a tile, lanes of a group
 //   BACK, ONES        from the rows' ends; k is 1 everywhere (sums)
-//   OUTPUT            every entry has outputs
+//   STEP              entries a group takes at a time where only last states or maps are wanted
 //   EARLY             what rows begin with is loaded along with their entries, into registers
 //   Raw               what is loaded of one entry
 //   load(raw, p, id)  of entry p; id -1: it has no item, and what is loaded in the item's place leaves the state as it is
@@ -218,11 +219,11 @@ template <class Op> struct Walk {
 
     // Entries [from, from + n) (down from from - 1 where BACK) with all their rows; s is the state that comes in.
     // row: where the search for their rows begins.
-    __device__ void entries(Marks &m, int64_t from, int64_t n, int64_t row) {
+    __device__ void entries(Marks<WALK_STAGE> &m, int64_t from, int64_t n, int64_t row) {
         for (int64_t done = 0; done < n; done += WALK_STAGE) {
             const int64_t here = Op::BACK ? from - done : from + done;
             const int many = (int)min(n - done, (int64_t)WALK_STAGE);
-            stage_entries<Op::BACK>(rows, m, here, many, row);
+            stage_entries<Op::BACK, WALK_STAGE>(rows, m, here, many, row);
             for (int tile = 0; tile < many; tile += TILE) {
                 const int i0 = tile + group * K;
                 typename Op::Raw raw[K];
@@ -266,7 +267,6 @@ template <class Op> struct Walk {
                 }
                 float h[N];
                 join(k, b, starts != 0, h);
-                if (!Op::OUTPUT && !__any(ends != 0)) continue;
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     const bool starting = starts >> j & 1, ending = ends >> j & 1;
@@ -290,74 +290,160 @@ template <class Op> struct Walk {
         }
     }
 
+    // The same where only rows' last states are wanted: every group walks a stretch of a stage's entries from a state of zero, and
+    // the stretches' maps are joined once.  A row that ends in a stretch but began before it waits for that.
+    static constexpr int STEP = Op::STEP, LAST_TILE = GROUPS * STEP;
+    __device__ void last_states(Marks<LAST_STAGE> &m, int64_t from, int64_t n, int64_t row) {
+        static_assert(LAST_STAGE % (2 * LAST_TILE) == 0 || LAST_STAGE % LAST_TILE == 0, "");
+        for (int64_t done = 0; done < n; done += LAST_STAGE) {
+            const int64_t here = from + done;
+            const int many = (int)min(n - done, (int64_t)LAST_STAGE);
+            stage_entries<false, LAST_STAGE>(rows, m, here, many, row);
+            const int stretch = (many + LAST_TILE - 1) / LAST_TILE * STEP, first = group * stretch;
+            float k[N], b[N], head_k[N], head_b[N];
+            int head = -1;
+            bool seen = false;
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                k[c] = head_k[c] = 1.f;
+                b[c] = head_b[c] = 0.f;
+            }
+            typename Op::Raw raw[2][STEP];
+            auto load = [&](auto which, int at) {
+#pragma unroll
+                for (int j = 0; j < STEP; ++j) {
+                    const int i = min(first + at + j, LAST_STAGE - 1);
+                    op.load(raw[which()][j], here + min(i, many - 1), m.id[i], lane);
+                }
+            };
+            auto walk = [&](auto which, int at) {
+                const bool open = __any(!seen);
+#pragma unroll
+                for (int j = 0; j < STEP; ++j) {
+                    const int i = min(first + at + j, LAST_STAGE - 1);
+                    const int start = m.start[i], end = m.end[i];
+                    float kj[N], bj[N];
+                    op.map(raw[which()][j], kj, bj);
+                    if (__any(start >= 0)) {
+                        float s0[N];
+                        op.begin(max(start, 0), lane, s0);
+#pragma unroll
+                        for (int c = 0; c < N; ++c) b[c] = start >= 0 ? s0[c] : b[c];
+                        seen = seen || start >= 0;
+                    }
+#pragma unroll
+                    for (int c = 0; c < N; ++c) b[c] = Op::ONES ? b[c] + bj[c] : fmaf(kj[c], b[c], bj[c]);
+                    if (!Op::ONES && open) {
+#pragma unroll
+                        for (int c = 0; c < N; ++c) k[c] *= kj[c];
+                    }
+                    if (__any(end >= 0)) {
+                        if (__any(end >= 0 && !seen)) {
+                            const bool wait = end >= 0 && !seen;
+#pragma unroll
+                            for (int c = 0; c < N; ++c) {
+                                head_k[c] = wait ? k[c] : head_k[c];
+                                head_b[c] = wait ? b[c] : head_b[c];
+                            }
+                            head = wait ? end : head;
+                        }
+                        op.finish(max(end, 0), end >= 0 && seen, lane, b);
+                    }
+                }
+            };
+            constexpr std::integral_constant<int, 0> even{};
+            constexpr std::integral_constant<int, 1> odd{};
+            load(even, 0);
+            for (int at = 0; at < stretch; at += 2 * STEP) {
+                if (at + STEP < stretch) load(odd, at + STEP);
+                walk(even, at);
+                if (at + STEP < stretch) {
+                    if (at + 2 * STEP < stretch) load(even, at + 2 * STEP);
+                    walk(odd, at + STEP);
+                }
+            }
+            float in[N];
+            join(k, b, seen, in);
+            if (__any(head >= 0)) {
+#pragma unroll
+                for (int c = 0; c < N; ++c) head_b[c] = Op::ONES ? head_b[c] + in[c] : fmaf(head_k[c], in[c], head_b[c]);
+                op.finish(max(head, 0), head >= 0, lane, head_b);
+            }
+        }
+    }
+
     // The map of entries [from, from + n) of one row (down from from - 1 where BACK), of the row's first state and them where
-    // `row` >= 0; to `out` [2][d].
+    // `row` >= 0; to `out` [2][d].  Every group takes a stretch.
     __device__ void piece(int64_t from, int64_t n, int64_t row, float *out) {
-        float wk[N], wb[N];
+        const int64_t stretch = (n + LAST_TILE - 1) / LAST_TILE * STEP, first = group * stretch;
+        float k[N], b[N];
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            wk[c] = 1.f;
-            wb[c] = 0.f;
+            k[c] = 1.f;
+            b[c] = 0.f;
         }
-        if (row >= 0) {
-            op.begin(row, lane, wb);
+        if (row >= 0) {  // the first group's stretch begins with the row
+            float s0[N];
+            op.begin(row, lane, s0);
 #pragma unroll
-            for (int c = 0; c < N; ++c) wk[c] = 0.f;
+            for (int c = 0; c < N; ++c) {
+                b[c] = group == 0 ? s0[c] : 0.f;
+                k[c] = group == 0 ? 0.f : 1.f;
+            }
         }
-        for (int64_t done = 0; done < n; done += TILE) {
-            typename Op::Raw raw[K];
-            int id[K];
+        int id[STEP];
+        typename Op::Raw raw[STEP];
+        auto find = [&](int64_t at) {
 #pragma unroll
-            for (int j = 0; j < K; ++j) {
-                const int64_t i = done + group * K + j, at = min(i, n - 1), p = Op::BACK ? from - 1 - at : from + at;
+            for (int j = 0; j < STEP; ++j) {
+                const int64_t i = first + at + j, inside = min(i, n - 1), p = Op::BACK ? from - 1 - inside : from + inside;
                 id[j] = rows.y.ids ? rows.y.ids[p] : (int)p;
                 if (i >= n || id[j] >= rows.y.cols) id[j] = -1;
             }
+        };
+        find(0);
+        for (int64_t at = 0; at < stretch; at += STEP) {
 #pragma unroll
-            for (int j = 0; j < K; ++j) {
-                const int64_t at = min(done + group * K + j, n - 1);
-                op.load_map(raw[j], Op::BACK ? from - 1 - at : from + at, id[j], lane);
+            for (int j = 0; j < STEP; ++j) {
+                const int64_t inside = min(first + at + j, n - 1);
+                op.load_map(raw[j], Op::BACK ? from - 1 - inside : from + inside, id[j], lane);
             }
-            float k[N], b[N];
+            if (at + STEP < stretch) find(at + STEP);
 #pragma unroll
-            for (int j = 0; j < K; ++j) {
+            for (int j = 0; j < STEP; ++j) {
                 float kj[N], bj[N];
                 op.map(raw[j], kj, bj);
-                if (Op::BACK && done + group * K + j >= n) {  // gradients of entries without an item count, those behind the end do not
+                if (Op::BACK) {  // gradients of entries without an item count, those behind the end do not
+                    const bool on = first + at + j < n;
 #pragma unroll
-                    for (int c = 0; c < N; ++c) bj[c] = 0.f;
-                }
-#pragma unroll
-                for (int c = 0; c < N; ++c) {
-                    b[c] = j ? (Op::ONES ? b[c] + bj[c] : fmaf(kj[c], b[c], bj[c])) : bj[c];
-                    k[c] = j ? k[c] * kj[c] : kj[c];
-                }
-            }
-            // joined in pairs; the last group's lanes have the tile's map
-#pragma unroll
-            for (int step = 1; step < GROUPS; step *= 2) {
-#pragma unroll
-                for (int c = 0; c < N; ++c) {
-                    const float bo = __shfl_up(b[c], step * L), ko = __shfl_up(k[c], step * L);
-                    if (group >= step) {
-                        b[c] = fmaf(k[c], bo, b[c]);
-                        k[c] *= ko;
+                    for (int c = 0; c < N; ++c) {
+                        bj[c] = on ? bj[c] : 0.f;
+                        kj[c] = on ? kj[c] : 1.f;
                     }
                 }
-            }
-            const int from_lane = (GROUPS - 1) * L + lane;
 #pragma unroll
-            for (int c = 0; c < N; ++c) {
-                const float bt = __shfl(b[c], from_lane), kt = __shfl(k[c], from_lane);
-                wb[c] = fmaf(kt, wb[c], bt);
-                wk[c] *= kt;
+                for (int c = 0; c < N; ++c) {
+                    b[c] = Op::ONES ? b[c] + bj[c] : fmaf(kj[c], b[c], bj[c]);
+                    k[c] *= kj[c];
+                }
             }
         }
-        if (group == 0) {
+#pragma unroll
+        for (int step = 1; step < GROUPS; step *= 2) {
 #pragma unroll
             for (int c = 0; c < N; ++c) {
-                out[lane * N + c] = wk[c];
-                out[N * L + lane * N + c] = wb[c];
+                const float bo = __shfl_up(b[c], step * L), ko = __shfl_up(k[c], step * L);
+                if (group >= step) {
+                    b[c] = fmaf(k[c], bo, b[c]);
+                    k[c] *= ko;
+                }
+            }
+        }
+        if (group == GROUPS - 1) {
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                out[lane * N + c] = k[c];
+                out[N * L + lane * N + c] = b[c];
             }
         }
     }
@@ -391,7 +477,7 @@ __device__ __forceinline__ void leave_long_row(const Chunks &c, int64_t chunk, b
 // Last states: every chunk's short rows, and the maps of its long rows' pieces.
 template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_last_kernel(Op op, Lists y, Chunks c) {
     constexpr int D = Op::N * Op::L;
-    __shared__ __align__(16) Marks m;
+    __shared__ __align__(16) Marks<LAST_STAGE> m;
     const RowFinder f(y);
     const int64_t chunk = blockIdx.x;
     if (chunk >= c.count) return empty_rows(op, f, chunk - c.count, gridDim.x - c.count);
@@ -409,13 +495,13 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_last_k
         Walk<Op>(op, f).piece(b, high - b, r.at_high.u, c.across + chunk * 2 * D);
         high = b;
     }
-    if (low < high) Walk<Op>(op, f).entries(m, low, high - low, r.row_from(low));
+    if (low < high) Walk<Op>(op, f).last_states(m, low, high - low, r.row_from(low));
 }
 
 // All entries' outputs; rows that come in begin with the state that join_kernel left.
 template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_all_kernel(Op op, Lists y, Chunks c) {
     constexpr int D = Op::N * Op::L;
-    __shared__ __align__(16) Marks m;
+    __shared__ __align__(16) Marks<WALK_STAGE> m;
     const RowFinder f(y);
     const int64_t chunk = blockIdx.x;
     if (chunk >= c.count) return empty_rows(op, f, chunk - c.count, gridDim.x - c.count);
@@ -562,7 +648,7 @@ template <class Op> dim3 join_grid(const Chunks &c) { return dim3((unsigned)((c.
 inline unsigned walk_grid(const Chunks &c, int64_t rows) { return (unsigned)(c.count + std::min<int64_t>((rows + 63) / 64, EMPTY_GROUPS)); }
 
 template <class Op> void launch_last(const als_ctx *ctx, const Op &op, const als_csr *Y, hipStream_t s) {
-    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::TILE);
+    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::LAST_TILE);
     const Lists y = lists_of(Y);
     hipLaunchKernelGGL((walk_last_kernel<Op>), dim3(walk_grid(c, Y->rows)), dim3(64), 0, s, op, y, c);
     if (Y->nnz > c.longest) hipLaunchKernelGGL((join_kernel<Op, false>), join_grid<Op>(c), dim3(JOIN_THREADS), 0, s, op, c);

@@ -11,8 +11,9 @@ constexpr int RECUR_THREADS = 256;
 
 // h = s h + (1 - s) x along a row (als_recur).
 template <int D, bool BF, bool SBF, bool STATES> struct Forward {
-    static constexpr int N = BF ? 8 : 4, K = 32 / N, L = D / N, WAVES = STATES || (BF && D <= 32) ? 3 : 4;
-    static constexpr bool BACK = false, ONES = false, KEEP = true, OUTPUT = STATES, EARLY = false;
+    static constexpr int N = BF ? 8 : 4, K = 32 / N, L = D / N, WAVES = STATES || BF ? 3 : 4;
+    static constexpr bool BACK = false, ONES = false, KEEP = true, EARLY = false;
+    static constexpr int STEP = 4;
     RowsOf V, F, H0, states, last;
     const char *no_x, *no_g;
     struct Raw {
@@ -50,7 +51,8 @@ template <int D, bool BF, bool SBF, bool STATES> struct Forward {
 // g = d + a, a = s g from a row's end (als_recur_backward): a, what an entry gets from those behind it, is the state.
 template <int D, bool BF, bool SBF> struct Backward {
     static constexpr int N = 4, K = 4, L = D / N, WAVES = 3;
-    static constexpr bool BACK = true, ONES = false, KEEP = false, OUTPUT = true, EARLY = BF || SBF || D >= 64;
+    static constexpr bool BACK = true, ONES = false, KEEP = false, EARLY = BF || SBF || D >= 64;
+    static constexpr int STEP = 4;
     RowsOf V, F, H0, states, d_states, d_last, dV, dF, dH0;
     const char *no_x, *no_g;
     struct Raw {

@@ -5,7 +5,8 @@ namespace als {
 
 template <int D, bool BF> struct SumRows {
     static constexpr int N = BF ? 8 : 4, K = 32 / N, L = D / N, WAVES = 4;
-    static constexpr bool BACK = false, ONES = true, KEEP = true, OUTPUT = false, EARLY = false;
+    static constexpr bool BACK = false, ONES = true, KEEP = true, EARLY = false;
+    static constexpr int STEP = 4;
     RowsOf E, X;
     const float *values;
     const char *no_x;
