@@ -629,12 +629,12 @@ template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void 
 
 // Chunks of the call's entries: for small calls as many as the card holds wavefronts, of a tile at least; then of 64 entries, so that a
 // chunk's search for its rows does not weigh; then as many as there is room for.
-inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile) {
+inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile, int longest) {
     Chunks c{};
     const int64_t resident = (int64_t)ctx->num_cu * 12, wanted = std::max((nnz + WALK_MAX_CHUNKS - 1) / WALK_MAX_CHUNKS, std::min<int64_t>(64, (nnz + resident - 1) / resident));
     c.size = std::max<int64_t>(1, (wanted + tile - 1) / tile) * tile;
     c.count = (nnz + c.size - 1) / c.size;
-    c.longest = std::max<int64_t>(c.size, 4 * tile);
+    c.longest = std::max<int64_t>(c.size * longest, 4 * tile);
     c.across = (float *)ctx->walk_maps.p;
     c.close = c.across + (int64_t)WALK_MAX_CHUNKS * 2 * 128;
     c.rows = (JoinedRow *)(c.close + (int64_t)WALK_MAX_CHUNKS * 2 * 128);
@@ -648,7 +648,7 @@ template <class Op> dim3 join_grid(const Chunks &c) { return dim3((unsigned)((c.
 inline unsigned walk_grid(const Chunks &c, int64_t rows) { return (unsigned)(c.count + std::min<int64_t>((rows + 63) / 64, EMPTY_GROUPS)); }
 
 template <class Op> void launch_last(const als_ctx *ctx, const Op &op, const als_csr *Y, hipStream_t s) {
-    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::LAST_TILE);
+    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::LAST_TILE, 1);
     const Lists y = lists_of(Y);
     hipLaunchKernelGGL((walk_last_kernel<Op>), dim3(walk_grid(c, Y->rows)), dim3(64), 0, s, op, y, c);
     if (Y->nnz > c.longest) hipLaunchKernelGGL((join_kernel<Op, false>), join_grid<Op>(c), dim3(JOIN_THREADS), 0, s, op, c);

@@ -160,7 +160,7 @@ als_status walk_setup(als_ctx *ctx) {
 }
 
 template <class Op> static void launch_all(const als_ctx *ctx, const Op &op, const als_csr *Y, hipStream_t s) {
-    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::TILE);
+    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::TILE, 2);  // entries of long rows are read twice
     const Lists y = lists_of(Y);
     if (Y->nnz > c.longest) {  // there may be rows that are cut
         hipLaunchKernelGGL((pieces_kernel<Op>), dim3((unsigned)c.count), dim3(64), 0, s, op, y, c);
