@@ -24,6 +24,7 @@ namespace als {
 constexpr int WALK_STAGE = 128;       // entries whose ids and marks are in LDS at a time
 constexpr int LAST_STAGE = 512;       // the same where only last states are wanted: the groups' maps are joined once a stage
 constexpr int WALK_MAX_CHUNKS = 32768;
+constexpr int FEW_CHUNKS = 48;          // a row's pieces among so few are composed by every wavefront that needs them
 
 // Chunks, and what is kept of each for rows that cross its border: maps (k, b) of `d` columns.
 //   across  of the part of a long row up to the border that the walk leaves the chunk by
@@ -498,38 +499,6 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_last_k
     if (low < high) Walk<Op>(op, f).last_states(m, low, high - low, r.row_from(low));
 }
 
-// All entries' outputs; rows that come in begin with the state that join_kernel left.
-template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_all_kernel(Op op, Lists y, Chunks c) {
-    constexpr int D = Op::N * Op::L;
-    __shared__ __align__(16) Marks<WALK_STAGE> m;
-    const RowFinder f(y);
-    const int64_t chunk = blockIdx.x;
-    if (chunk >= c.count) return empty_rows(op, f, chunk - c.count, gridDim.x - c.count);
-    const ChunkRows r(f, c, chunk);
-    if (r.low >= r.high) return;
-    Walk<Op> walk(op, f);
-    if (Op::BACK ? r.split_high : r.split_low) {
-#pragma unroll
-        for (int j = 0; j < Op::N; ++j) walk.s[j] = c.close[(chunk * 2 + 1) * D + walk.lane * Op::N + j];
-    }
-    walk.entries(m, Op::BACK ? r.high : r.low, r.high - r.low, Op::BACK ? r.at_high.u : r.row_from(r.low));
-}
-
-// The map of the part of a long row that leads to the border where the walk leaves the chunk.
-template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kernel(Op op, Lists y, Chunks c) {
-    constexpr int D = Op::N * Op::L;
-    const RowFinder f(y);
-    const int64_t chunk = c.count - 1 - blockIdx.x;  // the walk begins with the chunks that were read last: the cache may hold them
-    const ChunkRows r(f, c, chunk);
-    const RowFinder::Row row = Op::BACK ? r.at_low : r.at_high;
-    const bool out = Op::BACK ? r.split_low : r.split_high;
-    const bool through = r.split_low && r.split_high && r.at_low.u == r.at_high.u;
-    leave_long_row(c, chunk, out && !through, row);
-    if (!out || r.low >= r.high) return;
-    const int64_t low = max(r.low, row.b), high = min(r.high, row.e);
-    Walk<Op>(op, f).piece(Op::BACK ? high : low, high - low, through ? -1 : row.u, c.across + chunk * 2 * D);
-}
-
 // A long row's pieces one after the other, on behalf of the chunk that the walk along the row begins in (CARRY: the state at every
 // border it crosses goes to the chunk behind it) or ends in (otherwise: the row's last state).
 template <class Op, bool CARRY> struct Pieces {
@@ -577,6 +546,48 @@ template <class Op, bool CARRY> struct Pieces {
         op.finish(row, true, lane, s);
     }
 };
+
+// All entries' outputs; rows that come in begin with the state that join_kernel left, or, where chunks are few, with what the
+// wavefront composes of the row's pieces itself: that saves a launch.
+template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_all_kernel(Op op, Lists y, Chunks c) {
+    constexpr int D = Op::N * Op::L;
+    __shared__ __align__(16) Marks<WALK_STAGE> m;
+    const RowFinder f(y);
+    const int64_t chunk = blockIdx.x;
+    if (chunk >= c.count) return empty_rows(op, f, chunk - c.count, gridDim.x - c.count);
+    const ChunkRows r(f, c, chunk);
+    if (r.low >= r.high) return;
+    Walk<Op> walk(op, f);
+    if (Op::BACK ? r.split_high : r.split_low) {
+        if (c.count <= FEW_CHUNKS) {
+            const int64_t from = Op::BACK ? min((r.at_high.e - 1) / c.size, c.count - 1) : r.at_low.b / c.size;
+            const int pieces = (int)(Op::BACK ? from - chunk : chunk - from);
+            Pieces<Op, true> p{c, from, pieces, walk.lane, {}, {}};
+            p.template walk<false>(0, pieces);
+#pragma unroll
+            for (int j = 0; j < Op::N; ++j) walk.s[j] = p.s[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < Op::N; ++j) walk.s[j] = c.close[(chunk * 2 + 1) * D + walk.lane * Op::N + j];
+        }
+    }
+    walk.entries(m, Op::BACK ? r.high : r.low, r.high - r.low, Op::BACK ? r.at_high.u : r.row_from(r.low));
+}
+
+// The map of the part of a long row that leads to the border where the walk leaves the chunk.
+template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kernel(Op op, Lists y, Chunks c) {
+    constexpr int D = Op::N * Op::L;
+    const RowFinder f(y);
+    const int64_t chunk = c.count - 1 - blockIdx.x;  // the walk begins with the chunks that were read last: the cache may hold them
+    const ChunkRows r(f, c, chunk);
+    const RowFinder::Row row = Op::BACK ? r.at_low : r.at_high;
+    const bool out = Op::BACK ? r.split_low : r.split_high;
+    const bool through = r.split_low && r.split_high && r.at_low.u == r.at_high.u;
+    leave_long_row(c, chunk, out && !through, row);
+    if (!out || r.low >= r.high) return;
+    const int64_t low = max(r.low, row.b), high = min(r.high, row.e);
+    Walk<Op>(op, f).piece(Op::BACK ? high : low, high - low, through ? -1 : row.u, c.across + chunk * 2 * D);
+}
 
 // A workgroup looks at 64 chunks.  Rows of a few pieces: a group of lanes each.  Others: their pieces are dealt out in stretches to
 // all groups, whose maps are joined through LDS; the columns are dealt out to the workgroups of a second dimension.
@@ -634,7 +645,7 @@ inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile, int longest) 
     const int64_t resident = (int64_t)ctx->num_cu * 12, wanted = std::max((nnz + WALK_MAX_CHUNKS - 1) / WALK_MAX_CHUNKS, std::min<int64_t>(64, (nnz + resident - 1) / resident));
     c.size = std::max<int64_t>(1, (wanted + tile - 1) / tile) * tile;
     c.count = (nnz + c.size - 1) / c.size;
-    c.longest = std::max<int64_t>(c.size * longest, 4 * tile);
+    c.longest = longest * std::max<int64_t>(c.size, 4 * tile);
     c.across = (float *)ctx->walk_maps.p;
     c.close = c.across + (int64_t)WALK_MAX_CHUNKS * 2 * 128;
     c.rows = (JoinedRow *)(c.close + (int64_t)WALK_MAX_CHUNKS * 2 * 128);

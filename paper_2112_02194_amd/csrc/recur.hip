@@ -164,7 +164,8 @@ template <class Op> static void launch_all(const als_ctx *ctx, const Op &op, con
     const Lists y = lists_of(Y);
     if (Y->nnz > c.longest) {  // there may be rows that are cut
         hipLaunchKernelGGL((pieces_kernel<Op>), dim3((unsigned)c.count), dim3(64), 0, s, op, y, c);
-        hipLaunchKernelGGL((join_kernel<Op, true>), join_grid<Op>(c), dim3(JOIN_THREADS), 0, s, op, c);
+        if (c.count > FEW_CHUNKS)
+            hipLaunchKernelGGL((join_kernel<Op, true>), join_grid<Op>(c), dim3(JOIN_THREADS), 0, s, op, c);
     }
     hipLaunchKernelGGL((walk_all_kernel<Op>), dim3(walk_grid(c, Y->rows)), dim3(64), 0, s, op, y, c);
 }
