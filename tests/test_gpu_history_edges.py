@@ -249,3 +249,53 @@ def test_what_the_c_interface_allows(ctx, gpu_device):
     got = als.als_beam(ctx, ids[:0], scores[:0], None, None, 3)
     assert [t.numel() for t in got] == [0, 0, 0, 0]
     torch.cuda.synchronize()
+
+
+def the_example():
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "next_items.py")
+    spec = importlib.util.spec_from_file_location("next_items", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+def test_the_example_continues_histories(gpu_device):
+    say("examples/next_items.py")
+    r = the_example().main(nodes=6000, epochs=2, gate_steps=3, answered=20)
+    assert all(np.isfinite(v) for pair in r["training"] for v in pair) and 0 < r["gates"] < 1
+    items, total = r["items"], r["log_probability"]
+    assert items.shape == (20, 4, 5) and torch.all(items >= 0)
+    for row in items.view(-1, 5).tolist():
+        assert len(set(row)) == 5  # no item twice
+    assert torch.all(total <= 1e-4) and torch.all(total[:, :-1] >= total[:, 1:])
+
+
+def test_the_gradients_of_the_example_are_differences(ctx, gpu_device):
+    """Directions in the tables that the recurrence reads, with the items that queries are compared with held.  The loss in 64 bits by
+    the reference; central differences with a step of 2^-12 are off by 2^-24 / 6 of third derivatives, the gradients by some
+    hundred fp32 roundings: below 1e-4 of the sum of the magnitudes that go into the product."""
+    say("examples/next_items.py: gradients against differences")
+    ex = the_example()
+    gen = torch.Generator().manual_seed(2)
+    items, d = 30, 16
+    V, F = (torch.randn((items, d), generator=gen).to(gpu_device) for _ in range(2))
+    Y = csr(*history([4, 0, 9, 130, 1, 2], items, 3, stray=False), items, gpu_device)
+    by_item = ex.entries_by_item(Y.indices, items)
+    _, gV, gF = ex.loss_and_gradients(ctx, Y, by_item, V, F)
+    behind, some = ex.next_entries(Y.indptr, Y.nnz)
+    target = V[Y.indices[behind].long()].double()
+
+    def loss(v, f):
+        states = torch.from_numpy(ref.recur(Y.indptr.cpu().numpy(), Y.indices.cpu().numpy(), f64(v), f64(f))[1]).to(gpu_device)
+        return float(torch.where(some[:, None], states - target, 0.0).square().sum() / (2 * some.sum()))
+
+    for k, grad in enumerate((gV, gF)):
+        for _ in range(2):
+            way = torch.randn((items, d), generator=gen).to(gpu_device)
+            step = 2.0 ** -12
+            up, down = (loss(V.double() + (s * step * way.double() if k == 0 else 0), F.double() + (s * step * way.double() if k == 1 else 0)) for s in (1, -1))
+            want = (up - down) / (2 * step)
+            assert abs(float((grad.double() * way.double()).sum()) - want) <= 1e-4 * float((grad.double() * way.double()).abs().sum()) + 1e-9
