@@ -170,7 +170,7 @@ __global__ __launch_bounds__(REORDER_THREADS) void reorder_kernel(ReorderStates 
         const bool in_place = t.x == t.y;
         Words v[REORDER_EACH];
         int left[REORDER_EACH];  // bytes of the piece that are written
-        int64_t from[REORDER_EACH];
+        int32_t from[REORDER_EACH];
         // all parents, then all pieces: each of the two waits for memory once
 #pragma unroll
         for (int i = 0; i < REORDER_EACH; ++i) {
@@ -181,18 +181,18 @@ __global__ __launch_bounds__(REORDER_THREADS) void reorder_kernel(ReorderStates 
         for (int i = 0; i < REORDER_EACH; ++i) {
             const int piece = i * REORDER_THREADS + threadIdx.x;
             const int64_t row = first + (piece >> t.width), byte = column + (int64_t)(piece & ((1 << t.width) - 1)) * 16;
-            const int64_t group = row - (uint32_t)row % (uint32_t)beams;
+            const int32_t group = (int32_t)(row - (uint32_t)row % (uint32_t)beams);
             left[i] = row < end && byte < t.bytes && !(in_place && from[i] == row) ? (int)min(t.bytes - byte, (int64_t)16) : 0;
-            const bool there = from[i] >= group && from[i] < group + beams && left[i] > 0;
+            const bool there = from[i] >= group && from[i] - group < beams && left[i] > 0;
             v[i] = Words{0, 0, 0, 0};
             if (t.bytes >= 16) {  // otherwise no row has a whole piece
                 const bool whole = there && left[i] == 16;
-                const Words w = *(const Any *)(t.x + (whole ? from[i] * t.ldx + byte : 0));
+                const Words w = *(const Any *)(t.x + (whole ? (int64_t)from[i] * t.ldx + byte : 0));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[i][e] = whole ? w[e] : 0;
             }
             if (there && left[i] < 16) {  // elements of 2 or 4 bytes up to the row's end
-                const char *p = t.x + from[i] * t.ldx + byte;
+                const char *p = t.x + (int64_t)from[i] * t.ldx + byte;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (4 * e < left[i]) {
