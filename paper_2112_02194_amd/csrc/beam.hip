@@ -2,10 +2,12 @@
 //
 // beam kernel     one workgroup per group: candidates of all beams (up to 4096, sixteen a thread) in registers, a bar that at
 //                 least `beams` of them reach (the wavefronts' best lanes), those above it to LDS, cut back by digits where they
-//                 are many, and ranked by counting
+//                 are many, and ranked by counting.  A chain of loads and barriers: 4 us for 8 beams of 8, 9 for 128 groups of 32
+//                 beams of 32 (33 KB a group: memory has no part in it)
 // reorder kernel  a workgroup takes a slice of columns of all rows of a group (of several groups where rows are short): it reads the
 //                 slice of every parent, then writes.  So a group's rows may change places within the buffer; rows that
-//                 stay are neither read nor written there
+//                 stay are neither read nor written there.  Memory bound: 4096 rows of 126 KB 174 us, 5.9 TB/s (a parent that several
+//                 beams have is read once from memory); 7.7 us for 8 rows, the odd ends of rows one after the other
 #include <algorithm>
 #include <cmath>
 #include <iterator>

@@ -1,17 +1,27 @@
 // Linear recurrences along the rows of a CSR matrix, entries taken together however rows lie among them.
 //
-// Every entry is a map s -> k s + b of a row's state (a column each); a row begins with a state of its own.  The entries are cut into
-// chunks of the same length, one per wavefront, so that the work is even whatever the rows' lengths are.  A wavefront
-// walks its chunk a tile at a time: a group of lanes holds the d columns of one entry, each group takes the next K entries.  The
-// group joins its entries' maps, the groups' maps are joined across the wavefront (log2 steps), and with the state that comes in each
-// group walks its entries again from registers, where outputs are made.  One read of the tables.
+// Every entry is a map s -> k s + b of a row's state, in each column by itself; maps compose to maps (k2 k1, k2 b1 + b2), so a row can
+// be cut anywhere and its parts joined.  The entries are cut into chunks of the same length, one per wavefront, so that the work is
+// even whatever the rows' lengths are; groups of lanes hold the d columns of one entry, 16 bytes of the tables each.
 //
-// Rows of at most `longest` entries (a chunk's at least) belong whole to the chunk that they begin in.  A longer row is cut at the chunks' borders; its
-// pieces' maps go to the workspace:
-//   last states and sums   the same launch leaves the pieces, join_kernel composes those of each long row
-//   all states, gradients  pieces_kernel makes the pieces' maps first (the tables are read twice for entries of long rows),
-//                          carry_kernel the state at each border, then the walk begins with it
-// Both walks, along a row and from its end, are this one: index i counts in the direction of the walk.
+//   last states, sums       a group walks a stretch of the chunk's entries from a state of zero, a row after the other, the next entries
+//   (last_states)           under way; where a row began before the stretch, its map is kept too.  The stretches are joined once.
+//   all states, gradients   a tile at a time: each group composes the maps of K entries, the groups' maps are joined (log2 steps across the
+//   (entries)               wavefront), and with the state that comes in each group walks its entries again from registers.
+//
+// Rows of at most `longest` entries belong whole to the chunk that they begin in.  A longer row is cut at the chunks' borders, and its
+// pieces' maps go to the workspace (one size from als_create on):
+//   last states, sums       join_kernel composes the pieces of each long row
+//   all states, gradients   pieces_kernel makes the pieces' maps first, join_kernel the state at each border, from which the walk goes on.
+//                           The tables are read twice for entries of long rows; a row's maps cannot wait for the rows before, and what
+//                           the card holds of the entries at a time (128 MB of registers) is a tenth of a large call's.
+// Memory bounds all of it for large calls (figures at the operators).  A wavefront is its own workgroup: nothing waits for others.
+// Chunks: 512, 494, 490, 521 us with 8192, 16384, 32768, 65536 of them for the last states of 300000 rows (d = 128, bf16); rows of up to
+// 1, 2, 4, 8 chunks uncut 494, 514, 592, 701: a long row at the end keeps one wavefront busy and the others wait.
+//
+// Both walks, along a row and from its end, are this one: index i counts in the direction of the walk.  Branches around values are the
+// wavefront's, never some lanes', and registers are bounded without spills: the compiler was seen to place a copy of a live
+// address at the end of such a branch, before the other lanes are back.
 #pragma once
 
 #include <algorithm>
@@ -21,9 +31,9 @@
 
 namespace als {
 
-constexpr int WALK_STAGE = 128;       // entries whose ids and marks are in LDS at a time
-constexpr int LAST_STAGE = 512;       // the same where only last states are wanted: the groups' maps are joined once a stage
-constexpr int WALK_MAX_CHUNKS = 32768;
+constexpr int WALK_STAGE = 128;         // entries whose ids and marks are in LDS at a time
+constexpr int LAST_STAGE = 512;         // the same where only last states are wanted: the groups' maps are joined once a stage
+constexpr int WALK_MAX_CHUNKS = 32768;  // 2 KB of workspace each
 constexpr int FEW_CHUNKS = 48;          // a row's pieces among so few are composed by every wavefront that needs them
 
 // Chunks, and what is kept of each for rows that cross its border: maps (k, b) of `d` columns.
@@ -118,6 +128,7 @@ struct ChunkRows {
         low = border(f, x, c.longest, at_low, split_low);
         high = border(f, x + c.size, c.longest, at_high, split_high);
     }
+    __device__ __forceinline__ bool through() const { return split_low && split_high && at_low.u == at_high.u; }  // one row all over
     // where the search for the rows of a walk from `from` on (down from it) begins
     __device__ __forceinline__ int64_t row_from(int64_t from) const { return from >= at_low.e ? at_low.u + 1 : at_low.u; }
 };
@@ -165,7 +176,7 @@ template <bool BACK, int STAGE> __device__ void stage_entries(const RowFinder &f
 
 // A wavefront's walk.  Op:
 //   N, K, L           columns a lane, entries a group of lanes takes in a tile, lanes of a group
-//   BACK, ONES        from the rows' ends; k is 1 everywhere (sums)
+//   BACK, ONES        from the rows' ends; k is 1 everywhere (sums: last_states alone)
 //   STEP              entries a group takes at a time where only last states or maps are wanted
 //   EARLY             what rows begin with is loaded along with their entries, into registers
 //   Raw               what is loaded of one entry
@@ -177,8 +188,8 @@ template <bool BACK, int STAGE> __device__ void stage_entries(const RowFinder &f
 //   otherwise: entry(raw, has an item, p, valid, ending, ends, i, s)   moves s on by itself; ends[i]: the row that ends there
 //   finish(row, mine, s)   a row's last state, where `mine`
 template <class Op> struct Walk {
-    static constexpr int N = Op::N, K = Op::K, L = Op::L, GROUPS = 64 / L, TILE = GROUPS * K;
-    static_assert(WALK_STAGE % TILE == 0, "");
+    static constexpr int N = Op::N, K = Op::K, L = Op::L, GROUPS = 64 / L, TILE = GROUPS * K, STEP = Op::STEP, LAST_TILE = GROUPS * STEP;
+    static_assert(WALK_STAGE % TILE == 0 && LAST_STAGE % LAST_TILE == 0, "a stage is whole tiles");
     const Op &op;
     const RowFinder &rows;
     int lane, group;
@@ -242,7 +253,7 @@ template <class Op> struct Walk {
                     op.load(raw[j], Op::BACK ? here - 1 - min(i0 + j, many - 1) : here + min(i0 + j, many - 1), id, lane);
                 }
                 // No branch that some lanes take but for stores: a value is chosen, what is read for it is somewhere that can be read.
-                float k[N], b[N], keep[Op::KEEP && !Op::ONES ? K : 1][N], add[Op::KEEP ? K : 1][N];
+                float k[N], b[N], keep[Op::KEEP ? K : 1][N], add[Op::KEEP ? K : 1][N];
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     float kj[N], bj[N];
@@ -260,10 +271,12 @@ template <class Op> struct Walk {
                     }
 #pragma unroll
                     for (int c = 0; c < N; ++c) {
-                        b[c] = Op::ONES ? b[c] + bj[c] : fmaf(kj[c], b[c], bj[c]);
+                        b[c] = fmaf(kj[c], b[c], bj[c]);
                         k[c] = j ? k[c] * kj[c] : kj[c];
-                        if constexpr (Op::KEEP && !Op::ONES) keep[j][c] = kj[c];
-                        if constexpr (Op::KEEP) add[j][c] = bj[c];
+                        if constexpr (Op::KEEP) {
+                            keep[j][c] = kj[c];
+                            add[j][c] = bj[c];
+                        }
                     }
                 }
                 float h[N];
@@ -280,7 +293,7 @@ template <class Op> struct Walk {
                     const int64_t p = Op::BACK ? here - 1 - (i0 + j) : here + i0 + j;
                     if constexpr (Op::KEEP) {
 #pragma unroll
-                        for (int c = 0; c < N; ++c) h[c] = Op::ONES ? h[c] + add[j][c] : fmaf(keep[j][c], h[c], add[j][c]);
+                        for (int c = 0; c < N; ++c) h[c] = fmaf(keep[j][c], h[c], add[j][c]);
                         op.output(p, i0 + j < many, lane, h);
                     } else {
                         op.entry(raw[j], m.id[i0 + j] >= 0, p, i0 + j < many, ending, m.end, i0 + j, lane, h);
@@ -293,9 +306,7 @@ template <class Op> struct Walk {
 
     // The same where only rows' last states are wanted: every group walks a stretch of a stage's entries from a state of zero, and
     // the stretches' maps are joined once.  A row that ends in a stretch but began before it waits for that.
-    static constexpr int STEP = Op::STEP, LAST_TILE = GROUPS * STEP;
     __device__ void last_states(Marks<LAST_STAGE> &m, int64_t from, int64_t n, int64_t row) {
-        static_assert(LAST_STAGE % (2 * LAST_TILE) == 0 || LAST_STAGE % LAST_TILE == 0, "");
         for (int64_t done = 0; done < n; done += LAST_STAGE) {
             const int64_t here = from + done;
             const int many = (int)min(n - done, (int64_t)LAST_STAGE);
@@ -450,19 +461,21 @@ template <class Op> struct Walk {
     }
 };
 
-// The rows without entries, 64 at a time; workgroup `at` of `of`.
+// The rows without entries, 64 looked at and GROUPS written at a time; workgroup `at` of `of`.
 template <class Op> __device__ void empty_rows(const Op &op, const RowFinder &f, int64_t at, int64_t of) {
-    const int lane = threadIdx.x;
+    constexpr int GROUPS = 64 / Op::L;
+    const int lane = threadIdx.x % Op::L, group = threadIdx.x / Op::L;
     for (int64_t u0 = at * 64; u0 < f.y.rows; u0 += of * 64) {
-        const int64_t u = u0 + lane;
-        const bool none = u < f.y.rows && f.at(u) >= f.at(min(u + 1, f.y.rows));
-        for (unsigned long long who = __ballot(none); who; who &= who - 1) {
-            const int64_t row = u0 + __ffsll((long long)who) - 1;
-            if (lane < Op::L) {
-                float s[Op::N];
-                op.begin(row, lane, s);
-                op.finish(row, true, lane, s);
-            }
+        const int64_t u = min(u0 + threadIdx.x, f.y.rows - 1);
+        const unsigned long long none = __ballot(u0 + threadIdx.x < f.y.rows && f.at(u) >= f.at(u + 1));
+        if (none == 0) continue;
+#pragma unroll 4
+        for (int i = group; i < 64; i += GROUPS) {
+            const bool mine = none >> i & 1;
+            const int64_t row = mine ? u0 + i : u0;
+            float s[Op::N];
+            op.begin(row, lane, s);
+            op.finish(row, mine, lane, s);
         }
     }
 }
@@ -483,12 +496,11 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_last_k
     const int64_t chunk = blockIdx.x;
     if (chunk >= c.count) return empty_rows(op, f, chunk - c.count, gridDim.x - c.count);
     const ChunkRows r(f, c, chunk);
-    const bool through = r.split_low && r.split_high && r.at_low.u == r.at_high.u;
-    leave_long_row(c, chunk, r.split_low && !through, r.at_low);
+    leave_long_row(c, chunk, r.split_low && !r.through(), r.at_low);
     int64_t low = r.low, high = r.high;
     if (r.split_low && low < high) {
         const int64_t e = min(r.at_low.e, high);
-        Walk<Op>(op, f).piece(low, e - low, -1, (through ? c.across : c.close) + chunk * 2 * D);
+        Walk<Op>(op, f).piece(low, e - low, -1, (r.through() ? c.across : c.close) + chunk * 2 * D);
         low = e;
     }
     if (r.split_high && low < high) {
@@ -582,14 +594,13 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kern
     const ChunkRows r(f, c, chunk);
     const RowFinder::Row row = Op::BACK ? r.at_low : r.at_high;
     const bool out = Op::BACK ? r.split_low : r.split_high;
-    const bool through = r.split_low && r.split_high && r.at_low.u == r.at_high.u;
-    leave_long_row(c, chunk, out && !through, row);
+    leave_long_row(c, chunk, out && !r.through(), row);
     if (!out || r.low >= r.high) return;
     const int64_t low = max(r.low, row.b), high = min(r.high, row.e);
-    Walk<Op>(op, f).piece(Op::BACK ? high : low, high - low, through ? -1 : row.u, c.across + chunk * 2 * D);
+    Walk<Op>(op, f).piece(Op::BACK ? high : low, high - low, r.through() ? -1 : row.u, c.across + chunk * 2 * D);
 }
 
-// A workgroup looks at 64 chunks.  Rows of a few pieces: a group of lanes each.  Others: their pieces are dealt out in stretches to
+// A workgroup looks at 64 chunks (16 rows of 1024 pieces of d = 128: 16 us; one workgroup a row without a second dimension 37).  Rows of a few pieces: a group of lanes each.  Others: their pieces are dealt out in stretches to
 // all groups, whose maps are joined through LDS; the columns are dealt out to the workgroups of a second dimension.
 constexpr int JOIN_THREADS = 512, JOIN_CHUNKS = 64, JOIN_FEW = 24;
 template <class Op> constexpr int join_lanes() { return Op::L < 8 ? Op::L : 8; }
@@ -638,11 +649,12 @@ template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void 
     }
 }
 
-// Chunks of the call's entries: for small calls as many as the card holds wavefronts, of a tile at least; then of 64 entries, so that a
+// Chunks of the call's entries, and the longest rows that are not cut, in chunks (4 tiles at least).  For small calls as many as the card holds wavefronts, of a tile at least; then of 64 entries, so that a
 // chunk's search for its rows does not weigh; then as many as there is room for.
 inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile, int longest) {
     Chunks c{};
-    const int64_t resident = (int64_t)ctx->num_cu * 12, wanted = std::max((nnz + WALK_MAX_CHUNKS - 1) / WALK_MAX_CHUNKS, std::min<int64_t>(64, (nnz + resident - 1) / resident));
+    const int64_t resident = (int64_t)ctx->num_cu * 12;
+    const int64_t wanted = std::max((nnz + WALK_MAX_CHUNKS - 1) / WALK_MAX_CHUNKS, std::min<int64_t>(64, (nnz + resident - 1) / resident));
     c.size = std::max<int64_t>(1, (wanted + tile - 1) / tile) * tile;
     c.count = (nnz + c.size - 1) / c.size;
     c.longest = longest * std::max<int64_t>(c.size, 4 * tile);
@@ -654,7 +666,7 @@ inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile, int longest) 
 // behind the chunks': rows for entries without an item, 512 bytes each: zeros, gates in fp32, gates in bf16
 constexpr size_t WALK_NONE = (size_t)WALK_MAX_CHUNKS * (4 * 128 * sizeof(float) + sizeof(JoinedRow)), WALK_BYTES = WALK_NONE + 3 * 512;
 inline const char *none_row(const als_ctx *ctx, bool gates, bool bf16) { return (const char *)ctx->walk_maps.p + WALK_NONE + (!gates ? 0 : bf16 ? 1024 : 512); }
-constexpr int EMPTY_GROUPS = 1024;  // workgroups that look for empty rows, at most
+constexpr int EMPTY_GROUPS = 4096;  // workgroups that look for empty rows, at most
 template <class Op> dim3 join_grid(const Chunks &c) { return dim3((unsigned)((c.count + JOIN_CHUNKS - 1) / JOIN_CHUNKS), Op::L / join_lanes<Op>()); }
 inline unsigned walk_grid(const Chunks &c, int64_t rows) { return (unsigned)(c.count + std::min<int64_t>((rows + 63) / 64, EMPTY_GROUPS)); }
 

@@ -1,5 +1,13 @@
-// The gated linear recurrence over the entries of CSR rows (als_recur), its gradients and its single step.
-// A group of lanes holds a row's d columns, 16 bytes of the tables each, and walks its entries.
+// The gated linear recurrence over the entries of CSR rows (als_recur), its gradients and its single step.  How rows and entries are
+// dealt out stands in entry_walk.h; here are an entry's maps and outputs.
+//
+// Bytes that have to be moved, at the rates of a large copy (4.7 to 4.9 TB/s read and written), and what was measured:
+//   last states  300000 rows, 6.0M entries, d = 128, tables of 1M rows in bf16 (popular items often)  457 us.  3.1 GB gathered; 29 % from the
+//                L2, 2.8 GB from behind it at 6 TB/s, more than a copy's rate: the last-level cache has popular rows.  Vector units next:
+//                13 instruction slots an entry and column (exponential and reciprocal are 8 of them), 0.26 ms of the time
+//   all states   16 rows of 65537 entries, d = 128, fp32  518 us: pieces 220 (1.07 GB), their states 16, the walk 283 (1.61 GB)
+//   gradients    100000 rows, 2.0M entries, d = 64, fp32  565 us: 0.25 GB in pieces 70, the walk 490 (2.2 GB and what the cache misses of the
+//                gathers); 16 x 65537 in bf16 with fp32 states  702 us: 190 (0.8 GB), 24, 490 (2.7 GB)
 #include <algorithm>
 #include <type_traits>
 
@@ -9,7 +17,8 @@ namespace als {
 
 constexpr int RECUR_THREADS = 256;
 
-// h = s h + (1 - s) x along a row (als_recur).
+// h = s h + (1 - s) x along a row (als_recur).  K entries a group and tile: 64 registers of maps, at 3 wavefronts per SIMD without spills
+// (with last states alone, which keep none, 4; 8 columns a lane in bf16 take 3).
 template <int D, bool BF, bool SBF, bool STATES> struct Forward {
     static constexpr int N = BF ? 8 : 4, K = 32 / N, L = D / N, WAVES = STATES || BF ? 3 : 4;
     static constexpr bool BACK = false, ONES = false, KEEP = true, EARLY = false;
@@ -41,14 +50,15 @@ template <int D, bool BF, bool SBF, bool STATES> struct Forward {
         if (H0.p) load_piece(H0, row, lane, s);
     }
     __device__ __forceinline__ void output(int64_t p, bool valid, int lane, const float (&s)[N]) const {
-        if (STATES && valid) store_piece<SBF, N>(states.p + p * states.ld, lane, s);
+        if (valid) store_piece<SBF, N>(states.p + p * states.ld, lane, s);
     }
     __device__ __forceinline__ void finish(int64_t row, bool mine, int lane, const float (&s)[N]) const {
         if (last.p && mine) store_piece(last, row, lane, s);
     }
 };
 
-// g = d + a, a = s g from a row's end (als_recur_backward): a, what an entry gets from those behind it, is the state.
+// g = d + a, a = s g from a row's end (als_recur_backward): a, what an entry gets from those behind it, is the state.  Gates are
+// computed again in the second walk: what would be kept of them takes more registers than there are, and memory bounds the kernel.
 template <int D, bool BF, bool SBF> struct Backward {
     static constexpr int N = 4, K = 4, L = D / N, WAVES = 3;
     static constexpr bool BACK = true, ONES = false, KEEP = false, EARLY = BF || SBF || D >= 64;
@@ -117,7 +127,7 @@ template <int D, bool BF, bool SBF> struct Backward {
     }
 };
 
-// One entry per row, from a parent row.  X may be H where there are no parents: a row is read and written by the same lanes.
+// One entry per row, from a parent row: two loads after each other, 2.9 us for 512 rows.  X may be H where there are no parents: a row is read and written by the same lanes.
 template <int D, bool BF>
 __global__ __launch_bounds__(RECUR_THREADS) void recur_step_kernel(int64_t rows, const int32_t *items, const int32_t *parents, int64_t cols,
                                                                    int64_t from_rows, RowsOf V, RowsOf F, RowsOf H, RowsOf X) {
