@@ -258,7 +258,8 @@ als_status als_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules,
 /* ------------------------------------------------------------------------------------------------------------------
  * Ordered histories: queries from histories whose order counts, their gradients, answers of several items one after the
  * other.  Everything below is asynchronous on `stream`, allocates nothing and may be recorded into a HIP graph from the
- * first call on.  The order of all sums is fixed.
+ * first call on; the workspace (67 MB, one size) is there from als_create on.  The order of all sums is fixed.
+ * Y->rows, Y->cols and groups * beams are at most 2^31 - 1; entries and offsets have 64 bits.
  * ------------------------------------------------------------------------------------------------------------------ */
 
 /* A gated linear recurrence over the entries of every row of Y, in their stored order and for each of the d columns:
