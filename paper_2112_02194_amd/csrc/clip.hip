@@ -6,7 +6,7 @@
 // scale kernel  every workgroup adds the workgroups' sums in the same order, so all have the same bits of the norm, and takes its
 //               tiles from the end: the last ones read are those that the cache may still hold (1.52 ms, 5.3 TB/s; in place and below the
 //               bound nothing is read or written)
-// Small calls are the host's: 60 tensors of 2M elements in all 6 + 8 us here, 47 with the marshalling of 120 tensors.
+// Rows with gaps share a tile where they are short (5M x 64 fp32, 128 apart: 0.74 ms, a tile a row 16.2).  Small calls are the host's: 60 tensors of 2M elements in all 6 + 8 us here, 47 with the marshalling of 120 tensors.
 #include <algorithm>
 #include <iterator>
 #include <type_traits>
@@ -26,24 +26,47 @@ struct FlatTensor {
     char *y;
     int64_t n_and_type;  // elements * 2, + 1: bf16
     __device__ __forceinline__ bool bf16() const { return n_and_type & 1; }
-    // element offsets of the tensor's tile `at` in x and y, and the elements that its row has from there
-    __device__ __forceinline__ void place(uint32_t at, int64_t &x, int64_t &y, int64_t &left) const {
-        x = y = (int64_t)at * CLIP_TILE;
-        left = (n_and_type >> 1) - x;
+    // the tensor's tile `at`
+    template <class Tile> __device__ __forceinline__ void load(Tile &in, uint32_t at) const {
+        const int64_t from = (int64_t)at * CLIP_TILE;
+        in.load(x + from * Tile::ES, (n_and_type >> 1) - from);
+    }
+    template <class Tile> __device__ __forceinline__ void store(const Tile &in, uint32_t at, double c) const {
+        const int64_t from = (int64_t)at * CLIP_TILE;
+        in.store(y + from * Tile::ES, (n_and_type >> 1) - from, c);
     }
 };
+// A tile is a part of a row, or of several rows where they are short: 2^width pieces of 16 bytes of each.
 struct RowTensor {
     static constexpr int MOST = 64;
     const char *x;
     char *y;
-    int64_t cols, ldx, ldy;  // of a row, in elements
-    uint32_t row_tiles, type;
+    int64_t rows, cols, ldx, ldy;  // in elements
+    uint32_t row_tiles;
+    uint16_t width, type;
     __device__ __forceinline__ bool bf16() const { return type; }
-    __device__ __forceinline__ void place(uint32_t at, int64_t &x, int64_t &y, int64_t &left) const {
-        const int64_t row = at / row_tiles, col = (int64_t)(at % row_tiles) * CLIP_TILE;
-        x = row * ldx + col;
-        y = row * ldy + col;
-        left = cols - col;
+    // piece q of tile `at`: its place, and the elements that the row has from there
+    template <int PER> __device__ __forceinline__ void piece(uint32_t at, int q, int64_t &row, int64_t &col, int64_t &left) const {
+        constexpr int LOG = PER == 4 ? 10 : 9;  // pieces of a tile
+        row = ((int64_t)(at / row_tiles) << (LOG - width)) + (q >> width);
+        col = (int64_t)(at % row_tiles) * CLIP_TILE + (q & ((1 << width) - 1)) * PER;
+        left = row < rows ? cols - col : 0;
+    }
+    template <class Tile> __device__ __forceinline__ void load(Tile &in, uint32_t at) const {
+#pragma unroll
+        for (int j = 0; j < Tile::PIECES; ++j) {
+            int64_t row, col, left;
+            piece<Tile::PER>(at, j * CLIP_THREADS + threadIdx.x, row, col, left);
+            in.load_piece(j, x + (row * ldx + col) * Tile::ES, left);
+        }
+    }
+    template <class Tile> __device__ __forceinline__ void store(const Tile &in, uint32_t at, double c) const {
+#pragma unroll
+        for (int j = 0; j < Tile::PIECES; ++j) {
+            int64_t row, col, left;
+            piece<Tile::PER>(at, j * CLIP_THREADS + threadIdx.x, row, col, left);
+            in.store_piece(j, y + (row * ldy + col) * Tile::ES, left, c);
+        }
     }
 };
 template <class T> struct ClipTensors {
@@ -54,74 +77,73 @@ template <class T> struct ClipTensors {
 };
 static_assert(sizeof(ClipTensors<FlatTensor>) <= 4000 && sizeof(ClipTensors<RowTensor>) <= 4000, "a launch's arguments");
 
-// Sixteen elements of a tile, as 16-byte pieces; those behind the row's end are zeros.
+// Sixteen elements of a tile, as 16-byte pieces; those behind a row's end are zeros.
 template <bool BF16> struct ClipTile {
-    static constexpr int PER = BF16 ? 8 : 4, PIECES = CLIP_EPT / PER;
+    static constexpr int ES = BF16 ? 2 : 4, PER = 16 / ES, PIECES = CLIP_EPT / PER;
     typedef uint32_t Words __attribute__((ext_vector_type(4)));
     typedef Words Any __attribute__((aligned(2)));
     Words raw[PIECES];
-    static __device__ __forceinline__ int item(int j, int tid) { return (j * CLIP_THREADS + tid) * PER; }
-    __device__ __forceinline__ void load(const char *tile, int64_t left, int tid) {
-        constexpr int ES = BF16 ? 2 : 4;
-        if (left >= CLIP_TILE) {
-#pragma unroll
-            for (int j = 0; j < PIECES; ++j) raw[j] = *(const Any *)(tile + item(j, tid) * ES);
+    static __device__ __forceinline__ int item(int j) { return (j * CLIP_THREADS + threadIdx.x) * PER; }
+    // left: elements from p on
+    __device__ __forceinline__ void load_piece(int j, const char *p, int64_t left) {
+        raw[j] = Words{0, 0, 0, 0};
+        if (left >= PER) {
+            raw[j] = *(const Any *)p;
         } else {
 #pragma unroll
-            for (int j = 0; j < PIECES; ++j) {
-                const int at = item(j, tid);
-                raw[j] = Words{0, 0, 0, 0};
-                if (at + PER <= left) {
-                    raw[j] = *(const Any *)(tile + at * ES);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < PER; ++e)
-                        if (at + e < left) {
-                            if constexpr (BF16) raw[j][e / 2] |= (uint32_t)((const uint16_t *)tile)[at + e] << (e & 1) * 16;
-                            else raw[j][e] = ((const uint32_t *)tile)[at + e];
-                        }
+            for (int e = 0; e < PER; ++e)
+                if (e < left) {
+                    if constexpr (BF16) raw[j][e / 2] |= (uint32_t)((const uint16_t *)p)[e] << (e & 1) * 16;
+                    else raw[j][e] = ((const uint32_t *)p)[e];
                 }
-            }
+        }
+    }
+    __device__ __forceinline__ void load(const char *tile, int64_t left) {
+        if (left >= CLIP_TILE) {
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) raw[j] = *(const Any *)(tile + item(j) * ES);
+        } else {
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) load_piece(j, tile + item(j) * ES, left - item(j));
         }
     }
     __device__ __forceinline__ float value(int j, int e) const {
         return !BF16 ? __uint_as_float(raw[j][e]) : __uint_as_float(e & 1 ? raw[j][e / 2] & 0xffff0000u : raw[j][e / 2] << 16);
     }
     // times c; a factor near or below the normal range of fp32 has no bits to spare there: products in fp64
-    __device__ __forceinline__ void store(char *tile, int64_t left, int tid, double wide) const {
+    __device__ __forceinline__ void store_piece(int j, char *p, int64_t left, double wide) const {
         typedef __bf16 Half __attribute__((ext_vector_type(8)));
         typedef Half AnyHalf __attribute__((aligned(2)));
         typedef float Full __attribute__((ext_vector_type(4)));
         typedef Full AnyFull __attribute__((aligned(4)));
         const float c = (float)wide;
-        const bool small = wide < 0x1p-100;
+        float v[PER];
 #pragma unroll
-        for (int j = 0; j < PIECES; ++j) {
-            const int at = item(j, tid);
-            float v[PER];
+        for (int e = 0; e < PER; ++e) v[e] = c == 1.f ? value(j, e) : value(j, e) * c;
+        if (wide < 0x1p-100) {
 #pragma unroll
-            for (int e = 0; e < PER; ++e) v[e] = c == 1.f ? value(j, e) : value(j, e) * c;
-            if (small) {
-#pragma unroll
-                for (int e = 0; e < PER; ++e) v[e] = (float)(value(j, e) * wide);
-            }
-            if (at + PER <= left) {
-                if constexpr (BF16) {
-                    typedef float Eight __attribute__((ext_vector_type(8)));
-                    const Eight w = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-                    *(AnyHalf *)(tile + at * 2) = __builtin_convertvector(w, Half);
-                } else {
-                    *(AnyFull *)(tile + at * 4) = Full{v[0], v[1], v[2], v[3]};
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < PER; ++e)
-                    if (at + e < left) {
-                        if constexpr (BF16) ((__bf16 *)tile)[at + e] = (__bf16)v[e];
-                        else ((float *)tile)[at + e] = v[e];
-                    }
-            }
+            for (int e = 0; e < PER; ++e) v[e] = (float)(value(j, e) * wide);
         }
+        if (left >= PER) {
+            if constexpr (BF16) {
+                typedef float Eight __attribute__((ext_vector_type(8)));
+                const Eight w = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+                *(AnyHalf *)p = __builtin_convertvector(w, Half);
+            } else {
+                *(AnyFull *)p = Full{v[0], v[1], v[2], v[3]};
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+                if (e < left) {
+                    if constexpr (BF16) ((__bf16 *)p)[e] = (__bf16)v[e];
+                    else ((float *)p)[e] = v[e];
+                }
+        }
+    }
+    __device__ __forceinline__ void store(char *tile, int64_t left, double c) const {
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) store_piece(j, tile + item(j) * ES, left - item(j), c);
     }
 };
 
@@ -149,11 +171,9 @@ template <class T> __global__ __launch_bounds__(CLIP_THREADS) void clip_norm_ker
     for (uint32_t tile = blockIdx.x; tile < all.tiles; tile += gridDim.x) {
         while (j + 1 < all.n && tile >= all.first[j + 1]) ++j;
         const T &t = all.t[j];
-        int64_t x, y, left;
-        t.place(tile - all.first[j], x, y, left);
         auto add = [&](auto bf) {
             ClipTile<bf()> in;
-            in.load(t.x + x * (bf() ? 2 : 4), left, threadIdx.x);
+            t.load(in, tile - all.first[j]);
 #pragma unroll
             for (int i = 0; i < CLIP_EPT; ++i) {
                 const double v = in.value(i / in.PER, i % in.PER);
@@ -181,12 +201,10 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_scale_kernel(ClipTensors<T>
         while ((uint32_t)tile < all.first[j]) --j;
         const T &t = all.t[j];
         if (c == 1.0 && t.y == t.x) continue;
-        int64_t x, y, left;
-        t.place((uint32_t)tile - all.first[j], x, y, left);
         auto scale = [&](auto bf) {
             ClipTile<bf()> in;
-            in.load(t.x + x * (bf() ? 2 : 4), left, threadIdx.x);
-            in.store(t.y + y * (bf() ? 2 : 4), left, threadIdx.x, c);
+            t.load(in, (uint32_t)tile - all.first[j]);
+            t.store(in, (uint32_t)tile - all.first[j], c);
         };
         if (t.bf16()) scale(std::true_type{});
         else scale(std::false_type{});
@@ -208,7 +226,11 @@ als_status launch_clip(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, i
         for (; j < n && all.n < (int)std::size(all.t); ++j) {
             const als_matrix &x = X[j], &y = Y ? Y[j] : X[j];
             if (x.rows == 0 || x.cols == 0 || is_flat(j) != flat) continue;
-            const int64_t cols = flat ? x.rows * x.cols : x.cols, each = (cols + CLIP_TILE - 1) / CLIP_TILE, tiles = flat ? each : each * x.rows;
+            const int64_t cols = flat ? x.rows * x.cols : x.cols, each = (cols + CLIP_TILE - 1) / CLIP_TILE;
+            const int per = x.dtype == ALS_BF16 ? 8 : 4;
+            int width = 0;  // of rows with gaps: 2^width pieces of a tile are one row's
+            while ((int64_t)per << width < std::min<int64_t>(cols, CLIP_TILE)) ++width;
+            const int64_t rows = CLIP_TILE / per >> width, tiles = flat ? each : each * ((x.rows + rows - 1) / rows);
             if (tiles > INT32_MAX - all.tiles) {
                 if (all.n == 0) too_large = true;
                 break;
@@ -221,10 +243,12 @@ als_status launch_clip(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, i
             if constexpr (flat) {
                 t.n_and_type = cols * 2 + (x.dtype == ALS_BF16);
             } else {
+                t.rows = x.rows;
                 t.cols = cols;
                 t.ldx = x.ld;
                 t.ldy = y.ld;
                 t.row_tiles = (uint32_t)each;
+                t.width = (uint16_t)width;
                 t.type = x.dtype == ALS_BF16;
             }
         }

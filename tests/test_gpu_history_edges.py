@@ -23,6 +23,10 @@ def ctx(gpu_device):
     c.close()
 
 
+def wide(t):
+    return t.cpu().to(torch.float64)
+
+
 def apart(t, dev, ld):
     """The same rows `ld` elements apart, the space between them as it comes."""
     rows, d = t.shape
@@ -299,3 +303,39 @@ def test_the_gradients_of_the_example_are_differences(ctx, gpu_device):
             up, down = (loss(V.double() + (s * step * way.double() if k == 0 else 0), F.double() + (s * step * way.double() if k == 1 else 0)) for s in (1, -1))
             want = (up - down) / (2 * step)
             assert abs(float((grad.double() * way.double()).sum()) - want) <= 1e-4 * float((grad.double() * way.double()).abs().sum()) + 1e-9
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape,gap", [((3000, 1), 2), ((1025, 16), 16), ((777, 65), 7), ((2049, 128), 1), ((33, 4095), 5), ((5, 4097), 9),
+                                       ((1, 9), 1), ((2, 2), 1000)])
+def test_clip_of_rows_with_gaps(ctx, gpu_device, shape, gap, dtype):
+    """Several rows share a tile where they are short; what lies between rows is neither counted nor written."""
+    say(f"als_clip: {shape} with gaps of {gap}, {dtype}")
+    gen = torch.Generator().manual_seed(5)
+    host = torch.randn(shape, generator=gen).to(dtype)
+    other = torch.randn(100, generator=gen).to(dtype)
+
+    def with_gaps(fill):
+        big = torch.full((shape[0], shape[1] + gap), fill, dtype=dtype, device=gpu_device)
+        return big, big[:, :shape[1]]
+
+    norm = torch.sqrt(wide(host).square().sum() + wide(other).square().sum()).item()
+    bound = norm / 3
+    for place in ("in place", "out"):
+        big, x = with_gaps(1e30)
+        x.copy_(host.to(gpu_device))
+        lone = other.to(gpu_device)
+        out = None
+        if place == "out":
+            far, y = with_gaps(-7.0)
+            out = [y, torch.empty_like(lone)]
+        got = als.als_clip(ctx, [x, lone], bound, out=out)
+        assert abs(got.item() - norm) <= (host.numel() + other.numel() + 4) * 2.0 ** -53 * norm  # as many additions in fp64
+        space, written = (far, y) if out else (big, x)
+        assert torch.all(space[:, shape[1]:] == (torch.tensor(-7.0) if out else torch.tensor(1e30)).to(dtype).to(gpu_device))
+        # the factor, the product and the stored value are rounded once each
+        want = wide(host) * (bound / norm)
+        tol = 2 * 2.0 ** -24 + torch.finfo(dtype).eps / 2
+        assert torch.all((wide(written) - want).abs() <= 1.01 * tol * want.abs() + 1e-38)
+        if out:
+            assert torch.equal(x.cpu(), host)
