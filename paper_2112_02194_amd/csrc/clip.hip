@@ -6,7 +6,8 @@
 // scale kernel  every workgroup adds the workgroups' sums in the same order, so all have the same bits of the norm, and takes its
 //               tiles from the end: the last ones read are those that the cache may still hold (1.52 ms, 5.3 TB/s; in place and below the
 //               bound nothing is read or written)
-// Rows with gaps share a tile where they are short (5M x 64 fp32, 128 apart: 0.74 ms, a tile a row 16.2).  Small calls are the host's: 60 tensors of 2M elements in all 6 + 8 us here, 47 with the marshalling of 120 tensors.
+// Rows with gaps share a tile where they are short (5M x 64 fp32, 128 apart: 0.74 ms, a tile a row 16.2).  Small calls are the host's:
+// 60 tensors of 2M elements in all 6 + 8 us here, 47 with the marshalling of 120 tensors.
 #include <algorithm>
 #include <iterator>
 #include <type_traits>

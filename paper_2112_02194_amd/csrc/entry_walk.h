@@ -600,8 +600,9 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kern
     Walk<Op>(op, f).piece(Op::BACK ? high : low, high - low, r.through() ? -1 : row.u, c.across + chunk * 2 * D);
 }
 
-// A workgroup looks at 64 chunks (16 rows of 1024 pieces of d = 128: 16 us; one workgroup a row without a second dimension 37).  Rows of a few pieces: a group of lanes each.  Others: their pieces are dealt out in stretches to
-// all groups, whose maps are joined through LDS; the columns are dealt out to the workgroups of a second dimension.
+// A workgroup looks at 64 chunks (16 rows of 1024 pieces of d = 128: 16 us; one workgroup a row without a second dimension 37).  Rows of
+// a few pieces: a group of lanes each.  Others: their pieces are dealt out in stretches to all groups, whose maps are joined through
+// LDS; the columns are dealt out to the workgroups of a second dimension.
 constexpr int JOIN_THREADS = 512, JOIN_CHUNKS = 64, JOIN_FEW = 24;
 template <class Op> constexpr int join_lanes() { return Op::L < 8 ? Op::L : 8; }
 template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(Op op, Chunks c) {
@@ -649,8 +650,9 @@ template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void 
     }
 }
 
-// Chunks of the call's entries, and the longest rows that are not cut, in chunks (4 tiles at least).  For small calls as many as the card holds wavefronts, of a tile at least; then of 64 entries, so that a
-// chunk's search for its rows does not weigh; then as many as there is room for.
+// Chunks of the call's entries, and the longest rows that are not cut, in chunks (4 tiles at least).  For small calls as many as the
+// card holds wavefronts, of a tile at least; then of 64 entries, so that a chunk's search for its rows does not weigh; then as many as
+// there is room for.
 inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile, int longest) {
     Chunks c{};
     const int64_t resident = (int64_t)ctx->num_cu * 12;
