@@ -313,7 +313,8 @@ als_status als_clip(als_ctx *ctx, const als_matrix *X, const als_matrix *Y, int3
  * in fp32, one rounding each; with totals NULL (the first step) 0 for the first beam of a group, and the others have no candidate.
  * Where last is given and last[r] == end, the beam has ended: its only candidate is itself, with its total and the item `end`.
  * An id below 0 and a total that is -inf or NaN are no candidates.  A group's candidates are ordered by total, or, with `factors`, by
- * total * factors[length] (the last factor for longer ones; -inf and NaN are no candidates), equal ones by row and place; length =
+ * total * factors[length] (the last factor for longer ones; -inf and NaN are no candidates; factors may have any sign, and what has no
+ * total is no candidate whatever its factor), equal ones by row and place; length =
  * lengths[r] + 1, lengths[r] of a beam that has ended.  The first `beams` of them become the group's beams, best first.
  * parents: device int32, the row each beam continues; items, totals, lengths (may be NULL): device, of the new beams.
  * Where a group has fewer candidates, the rest have parent -1, item -1, total -inf and length 0.

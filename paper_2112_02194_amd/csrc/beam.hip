@@ -70,7 +70,8 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_kernel(BeamArgs a, int64_t 
             const float total = ended ? (leading ? before[i] : -INFINITY) : id[i] >= 0 ? live : -INFINITY;
             float key = total;
             if (a.factors) key = total * a.factors[min(max(length[i], 0), a.n_factors - 1)];
-            c[i] = at[i] < n && key > -INFINITY ? candidate(key, (uint32_t)at[i]) : 0;
+            // the total as well as the key: a negative factor makes +inf of a total of -inf
+            c[i] = at[i] < n && total > -INFINITY && key > -INFINITY ? candidate(key, (uint32_t)at[i]) : 0;
             all_totals[at[i]] = total;
             if (at[i] < n && leading) {
                 beam_length[beam[i]] = length[i];
