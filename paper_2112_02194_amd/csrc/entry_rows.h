@@ -66,6 +66,14 @@ template <bool BF16, int N, class W> __device__ __forceinline__ void widen(const
     for (int c = 0; c < N; ++c) x[c] = !BF16 ? __uint_as_float(w[c]) : __uint_as_float(c & 1 ? w[c / 2] & 0xffff0000u : w[c / 2] << 16);
 }
 
+// Row `id` of a table, or the row that stands for entries without an item where it is negative.  The address is computed for every
+// lane and then chosen: of a choice with work on one side the compiler makes a branch of some lanes.
+__device__ __forceinline__ const char *item_row(const RowsOf &t, int id, const char *none) {
+    uint64_t at = (uint64_t)t.p + (uint32_t)id * (uint64_t)t.ld;
+    asm("" : "+v"(at));
+    return id < 0 ? none : (const char *)at;
+}
+
 // s = 1 / (1 + exp(-g)) and 1 - s, each to its own size: with e = exp(-g) they are 1 / (1 + e) and e / (1 + e).  e is kept within
 // 2^126, where s is 2^-126; a NaN stays one.
 __device__ __forceinline__ void gate(float g, float &keep, float &take) {

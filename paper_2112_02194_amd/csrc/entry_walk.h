@@ -19,9 +19,10 @@
 // Chunks: 512, 494, 490, 521 us with 8192, 16384, 32768, 65536 of them for the last states of 300000 rows (d = 128, bf16); rows of up to
 // 1, 2, 4, 8 chunks uncut 494, 514, 592, 701: a long row at the end keeps one wavefront busy and the others wait.
 //
-// Both walks, along a row and from its end, are this one: index i counts in the direction of the walk.  Branches around values are the
-// wavefront's, never some lanes', and registers are bounded without spills: the compiler was seen to place a copy of a live
-// address at the end of such a branch, before the other lanes are back.
+// Both walks, along a row and from its end, are this one: index i counts in the direction of the walk.  Branches and loops around values
+// are the wavefront's, never some lanes' (those have stores alone), and no vector register is spilled: the compiler was seen to place a
+// copy of a live address at the end of such a branch, before the other lanes are back.  So what a choice takes is computed for
+// every lane first; test_walk_registers.py looks at what was built.
 #pragma once
 
 #include <algorithm>
@@ -83,7 +84,7 @@ struct RowFinder {
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const unsigned long long below = __ballot(u[i] < hi[i] && b[i] <= (i ? q : p));
+                const unsigned long long below = __ballot((u[i] < hi[i]) & (b[i] <= (i ? q : p)));
                 const int k = below ? 63 - __builtin_clzll(below) : 0;
                 lo[i] += k * step[i];
                 hi[i] = min(hi[i], lo[i] + step[i]);
@@ -140,13 +141,9 @@ template <bool BACK, int STAGE> __device__ void stage_entries(const RowFinder &f
     __syncthreads();
 #pragma unroll 2
     for (int i = lane; i < STAGE; i += 64) {
-        int id = -1;
-        if (i < n) {
-            const int64_t p = BACK ? from - 1 - i : from + i;
-            id = f.y.ids ? f.y.ids[p] : (int)p;
-            if (id >= f.y.cols) id = -1;
-        }
-        m.id[i] = id;
+        const int64_t p = BACK ? from - 1 - min(i, n - 1) : from + min(i, n - 1);  // behind the last one: the last one again
+        const int id = f.y.ids ? f.y.ids[p] : (int)p;
+        m.id[i] = (i < n) & (id < f.y.cols) ? id : -1;
         m.start[i] = m.end[i] = -1;
     }
     __syncthreads();
@@ -154,8 +151,9 @@ template <bool BACK, int STAGE> __device__ void stage_entries(const RowFinder &f
     for (int64_t base = row;;) {
         const int64_t u = BACK ? base - lane : base + lane;
         const bool some = u >= 0 && u < f.y.rows;
-        const int64_t b = some ? f.at(u) : BACK ? t0 : t1, e = some ? f.at(u + 1) : b;
-        const bool active = some && b < e && b < t1 && e > t0;
+        const int64_t inside = min(max(u, (int64_t)0), f.y.rows - 1), bu = f.at(inside), eu = f.at(inside + 1);
+        const int64_t b = some ? bu : BACK ? t0 : t1, e = some ? eu : b;
+        const bool active = some & (b < e) & (b < t1) & (e > t0);
         if (active) {
             if (b >= t0) (BACK ? m.end : m.start)[BACK ? t1 - 1 - b : b - t0] = (int)u;
             if (e <= t1) (BACK ? m.start : m.end)[BACK ? t1 - e : e - 1 - t0] = (int)u;
@@ -445,10 +443,9 @@ template <class Op> struct Walk {
 #pragma unroll
             for (int c = 0; c < N; ++c) {
                 const float bo = __shfl_up(b[c], step * L), ko = __shfl_up(k[c], step * L);
-                if (group >= step) {
-                    b[c] = fmaf(k[c], bo, b[c]);
-                    k[c] *= ko;
-                }
+                const bool take = group >= step;
+                b[c] = take ? fmaf(k[c], bo, b[c]) : b[c];
+                k[c] = take ? k[c] * ko : k[c];
             }
         }
         if (group == GROUPS - 1) {
@@ -523,8 +520,9 @@ template <class Op, bool CARRY> struct Pieces {
     __device__ __forceinline__ int64_t at(int i) const {
         return min(max(CARRY ? (Op::BACK ? chunk - i : chunk + i) : chunk - count + i, (int64_t)0), c.count - 1);
     }
+    // pieces begin .. end - 1, which may be other ones in every lane: the loop is the wavefront's
     template <bool STORE> __device__ __forceinline__ void walk(int begin, int end) {
-        for (int i0 = begin; i0 < end; i0 += AHEAD) {
+        for (int i0 = begin; __any(i0 < end); i0 += AHEAD) {
             float kp[AHEAD][N], bp[AHEAD][N];
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a) {
@@ -540,7 +538,8 @@ template <class Op, bool CARRY> struct Pieces {
                 const bool on = i0 + a < end, first = i0 + a == 0;  // the first piece has the row's own first state in it
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    s[j] = !on ? s[j] : first ? bp[a][j] : fmaf(kp[a][j], s[j], bp[a][j]);
+                    const float behind = fmaf(kp[a][j], s[j], bp[a][j]), now = first ? bp[a][j] : behind;
+                    s[j] = on ? now : s[j];
                     k[j] = on ? k[j] * kp[a][j] : k[j];
                 }
                 if (STORE && on) {
@@ -551,11 +550,11 @@ template <class Op, bool CARRY> struct Pieces {
             }
         }
     }
-    __device__ __forceinline__ void finish(const Op &op, int row) {
+    __device__ __forceinline__ void finish(const Op &op, int row, bool mine) {
         const float *map = c.close + chunk * 2 * D + lane * N;
 #pragma unroll
         for (int j = 0; j < N; ++j) s[j] = fmaf(map[j], s[j], map[D + j]);
-        op.finish(row, true, lane, s);
+        op.finish(row, mine, lane, s);
     }
 };
 
@@ -608,24 +607,28 @@ template <class Op> constexpr int join_lanes() { return Op::L < 8 ? Op::L : 8; }
 template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(Op op, Chunks c) {
     constexpr int N = Op::N, LANES = join_lanes<Op>(), GROUPS = JOIN_THREADS / LANES;
     __shared__ float maps[GROUPS][2][LANES * N];
+    __shared__ int few_at[JOIN_CHUNKS];
     const int64_t chunk0 = (int64_t)blockIdx.x * JOIN_CHUNKS, look = chunk0 + (threadIdx.x & 63);
-    const JoinedRow found = look < c.count ? c.rows[look] : JoinedRow{0, 0};
+    const JoinedRow entry = c.rows[min(look, c.count - 1)];
+    const int pieces = look < c.count ? entry.pieces : 0;
     if (blockIdx.y == 0) {
-        const unsigned long long few = __ballot(found.pieces > 0 && found.pieces <= JOIN_FEW);
+        const unsigned long long few = __ballot((pieces > 0) & (pieces <= JOIN_FEW));
         const int many = __popcll(few), lane = threadIdx.x % Op::L;
-        // the row that this group of lanes takes: the place of the n-th bit
-        for (int n = threadIdx.x / Op::L; n < many; n += JOIN_THREADS / Op::L) {
-            unsigned long long rest = few;
-            for (int i = 0; i < n; ++i) rest &= rest - 1;
-            const int64_t chunk = chunk0 + __ffsll((long long)rest) - 1;
+        // the places of the bits, the same from every wavefront
+        if (few >> (threadIdx.x & 63) & 1) few_at[__popcll(few & ((1ull << (threadIdx.x & 63)) - 1))] = threadIdx.x & 63;
+        __syncthreads();
+        for (int n0 = 0; n0 < many; n0 += JOIN_THREADS / Op::L) {
+            const int n = n0 + threadIdx.x / Op::L;  // the row that this group of lanes takes
+            const bool mine = n < many;
+            const int64_t chunk = chunk0 + few_at[min(n, many - 1)];
             const JoinedRow r = c.rows[chunk];
             Pieces<Op, CARRY> p{c, chunk, r.pieces, lane, {}, {}};
-            p.template walk<CARRY>(0, r.pieces);
-            if (!CARRY) p.finish(op, r.row);
+            p.template walk<CARRY>(0, mine ? r.pieces : 0);
+            if (!CARRY) p.finish(op, r.row, mine);
         }
     }
     const int in_group = threadIdx.x % LANES, group = threadIdx.x / LANES;
-    for (unsigned long long rest = __ballot(found.pieces > JOIN_FEW); rest; rest &= rest - 1) {
+    for (unsigned long long rest = __ballot(pieces > JOIN_FEW); rest; rest &= rest - 1) {
         const int64_t chunk = chunk0 + __ffsll((long long)rest) - 1;
         const JoinedRow r = c.rows[chunk];
         const int each = (r.pieces + GROUPS - 1) / GROUPS, begin = min(group * each, r.pieces), end = min(begin + each, r.pieces);
@@ -641,11 +644,14 @@ template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void 
         }
         __syncthreads();
         const int upto = CARRY ? min(group, groups) : groups;
-        for (int g = 0; g < upto; ++g)
+        for (int g = 0; __any(g < upto); ++g)
 #pragma unroll
-            for (int j = 0; j < N; ++j) p.s[j] = g ? fmaf(maps[g][0][in_group * N + j], p.s[j], maps[g][1][in_group * N + j]) : maps[0][1][in_group * N + j];
+            for (int j = 0; j < N; ++j) {
+                const float bg = maps[g][1][in_group * N + j], behind = fmaf(maps[g][0][in_group * N + j], p.s[j], bg), now = g ? behind : bg;
+                p.s[j] = g < upto ? now : p.s[j];
+            }
         if (CARRY) p.template walk<true>(begin, end);
-        else if (group == 0) p.finish(op, r.row);
+        else p.finish(op, r.row, group == 0);
         __syncthreads();
     }
 }

@@ -29,8 +29,8 @@ template <int D, bool BF, bool SBF, bool STATES> struct Forward {
         Words x, g;
     };
     __device__ __forceinline__ void load(Raw &r, int64_t, int id, int lane) const {
-        r.x = *(const Words *)((id < 0 ? no_x : V.p + id * V.ld) + lane * 16);
-        r.g = *(const Words *)((id < 0 ? no_g : F.p + id * F.ld) + lane * 16);
+        r.x = *(const Words *)(item_row(V, id, no_x) + lane * 16);
+        r.g = *(const Words *)(item_row(F, id, no_g) + lane * 16);
     }
     __device__ __forceinline__ void load_map(Raw &r, int64_t p, int id, int lane) const { load(r, p, id, lane); }
     __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&b)[N]) const {
@@ -70,13 +70,13 @@ template <int D, bool BF, bool SBF> struct Backward {
         Part<SBF> d, h;
     };
     __device__ __forceinline__ void load_map(Raw &r, int64_t p, int id, int lane) const {
-        r.g = *(const Part<BF> *)((id < 0 ? no_g : F.p + id * F.ld) + lane * sizeof(Part<BF>));
+        r.g = *(const Part<BF> *)(item_row(F, id, no_g) + lane * sizeof(Part<BF>));
         r.d = Part<SBF>{};
         if (d_states.p) r.d = *(const Part<SBF> *)(d_states.p + p * d_states.ld + lane * sizeof(Part<SBF>));
     }
     __device__ __forceinline__ void load(Raw &r, int64_t p, int id, int lane) const {
         load_map(r, p, id, lane);
-        r.x = *(const Part<BF> *)((id < 0 ? no_x : V.p + id * V.ld) + lane * sizeof(Part<BF>));
+        r.x = *(const Part<BF> *)(item_row(V, id, no_x) + lane * sizeof(Part<BF>));
         r.h = *(const Part<SBF> *)(states.p + max(p - 1, (int64_t)0) * states.ld + lane * sizeof(Part<SBF>));
     }
     __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&b)[N]) const {

@@ -17,7 +17,7 @@ template <int D, bool BF> struct SumRows {
         float w;
     };
     __device__ __forceinline__ void load(Raw &r, int64_t p, int id, int lane) const {
-        r.x = *(const Words *)((id < 0 ? no_x : E.p + id * E.ld) + lane * 16);
+        r.x = *(const Words *)(item_row(E, id, no_x) + lane * 16);
         r.w = id < 0 || !values ? 1.f : values[p];
     }
     __device__ __forceinline__ void load_map(Raw &r, int64_t p, int id, int lane) const { load(r, p, id, lane); }
