@@ -82,6 +82,29 @@ __device__ __forceinline__ void gate(float g, float &keep, float &take) {
     take = e * keep;
 }
 
+// The share of a state that a map keeps, held so that its bits are those that count: below 7/8 as it is, above it as what is missing to 1,
+// with a minus sign.  Near 1 half a step is 2^-25; that, once an entry, is 1e-3 of a state that 65000 entries with the same gate have
+// made, where what is given away (1 - s, and t + v - t v of two) has all its bits.  All of it kept is -0, and 0 nothing.
+constexpr float KEEPS_ALL = -0.f;
+__device__ __forceinline__ float share_of(float keep, float take) { return take < 0.125f ? -take : keep; }
+// `s` where the sign of `q` is set, 0 elsewhere
+__device__ __forceinline__ float where_negative(float q, float s) { return __int_as_float(__float_as_int(s) & __float_as_int(q) >> 31); }
+// the state s after a map with share q and what it adds
+__device__ __forceinline__ float after_map(float q, float s, float b) { return fmaf(q, s, b) + where_negative(q, s); }
+// The share of two maps after each other: p q of kept ones; -(t + v - t v) of t and v given away, q (1 - t) of one of each.  What is
+// given away stays below 1/2, else 1 + k, which is exact, is what is kept.
+__device__ __forceinline__ float share_of_both(float p, float q) {
+    const float zp = where_negative(q, p), zq = where_negative(p, q);
+    float k = fmaf(p, q, zp) + zq;
+    k = __uint_as_float(__float_as_uint(k) | (__float_as_uint(zp) & 0x80000000u));  // -0 and -0 stay -0
+    return k < -0.5f ? k + 1.f : k;
+}
+// One of two values that both are there.
+__device__ __forceinline__ float chosen(bool first, float a, float b) {
+    asm("" : "+v"(a), "+v"(b));
+    return first ? a : b;
+}
+
 // Entries of row u, whatever indptr holds.
 __device__ __forceinline__ void row_range(const int64_t *indptr, int64_t u, int64_t nnz, int64_t &b, int64_t &e) {
     b = indptr[u];

@@ -1,7 +1,10 @@
 // Linear recurrences along the rows of a CSR matrix, entries taken together however rows lie among them.
 //
 // Every entry is a map s -> k s + b of a row's state, in each column by itself; maps compose to maps (k2 k1, k2 b1 + b2), so a row can
-// be cut anywhere and its parts joined.  The entries are cut into chunks of the same length, one per wavefront, so that the work is
+// be cut anywhere and its parts joined.  What a lane walks one entry after the other are products; 1 - k goes along, and where a state
+// crosses a group's or a piece's border k near 1 is held as what is missing to it (share_of), so that the rounding of a gate near 1
+// counts for some entries, not once for every entry of the row (sums of 1 - k: one multiply-add an entry, recur_rows 469 -> 484 us; shares
+// for every entry by itself: 603).  The entries are cut into chunks of the same length, one per wavefront, so that the work is
 // even whatever the rows' lengths are; groups of lanes hold the d columns of one entry, 16 bytes of the tables each.
 //
 //   last states, sums       a group walks a stretch of the chunk's entries from a state of zero, a row after the other, the next entries
@@ -172,6 +175,9 @@ template <bool BACK, int STAGE> __device__ void stage_entries(const RowFinder &f
     __syncthreads();
 }
 
+// The state behind a map that keeps the share k.
+template <class Op> __device__ __forceinline__ float after(float k, float s, float b) { return Op::ONES ? s + b : after_map(k, s, b); }
+
 // A wavefront's walk.  Op:
 //   N, K, L           columns a lane, entries a group of lanes takes in a tile, lanes of a group
 //   BACK, ONES        from the rows' ends; k is 1 everywhere (sums: last_states alone)
@@ -180,7 +186,7 @@ template <bool BACK, int STAGE> __device__ void stage_entries(const RowFinder &f
 //   Raw               what is loaded of one entry
 //   load(raw, p, id)  of entry p; id -1: it has no item, and what is loaded in the item's place leaves the state as it is
 //   load_map(raw, p, id)   what its map takes of that
-//   map(raw, k, b)    its map
+//   map(raw, k, t, b) its map: what it keeps, 1 - k to bits of its own, what it adds
 //   begin(row, s)     a row's first state
 //   KEEP: output(p, valid, s)   after an entry whose map was kept in registers
 //   otherwise: entry(raw, has an item, p, valid, ending, ends, i, s)   moves s on by itself; ends[i]: the row that ends there
@@ -197,9 +203,9 @@ template <class Op> struct Walk {
         for (int c = 0; c < N; ++c) s[c] = 0.f;
     }
 
-    // The groups' maps joined: the state that comes into every group, and s behind the tile.
+    // The groups' maps (k, 1 - k as t, b) joined: the state that comes into every group, and s behind the tile.
     // seen: the group's entries hold a row's start, so that nothing of what comes in reaches its end.
-    __device__ __forceinline__ void join(float (&k)[N], float (&b)[N], bool seen, float (&in)[N]) {
+    __device__ __forceinline__ void join(float (&k)[N], float (&t)[N], float (&b)[N], bool seen, float (&in)[N]) {
 #pragma unroll
         for (int step = 1; step < GROUPS; step *= 2) {
             const unsigned long long starts = __ballot(seen);
@@ -208,8 +214,9 @@ template <class Op> struct Walk {
             for (int c = 0; c < N; ++c) {
                 const float bo = __shfl_up(b[c], step * L);
                 if (!Op::ONES) {
-                    const float ko = __shfl_up(k[c], step * L);
+                    const float ko = __shfl_up(k[c], step * L), to = __shfl_up(t[c], step * L);
                     b[c] = take ? fmaf(k[c], bo, b[c]) : b[c];
+                    t[c] = take ? fmaf(k[c], to, t[c]) : t[c];
                     k[c] = take ? k[c] * ko : k[c];
                 } else {
                     b[c] = take ? b[c] + bo : b[c];
@@ -220,10 +227,10 @@ template <class Op> struct Walk {
         // the state behind each group; it comes into the next one, the last group's into the next tile
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            const float after = seen ? b[c] : Op::ONES ? s[c] + b[c] : fmaf(k[c], s[c], b[c]);
-            const float prior = __shfl_up(after, L);
+            const float behind = chosen(seen, b[c], after<Op>(share_of(k[c], t[c]), s[c], b[c]));
+            const float prior = __shfl_up(behind, L);
             in[c] = group == 0 ? s[c] : prior;
-            s[c] = __shfl(after, (GROUPS - 1) * L + lane);
+            s[c] = __shfl(behind, (GROUPS - 1) * L + lane);
         }
     }
 
@@ -251,11 +258,11 @@ template <class Op> struct Walk {
                     op.load(raw[j], Op::BACK ? here - 1 - min(i0 + j, many - 1) : here + min(i0 + j, many - 1), id, lane);
                 }
                 // No branch that some lanes take but for stores: a value is chosen, what is read for it is somewhere that can be read.
-                float k[N], b[N], keep[Op::KEEP ? K : 1][N], add[Op::KEEP ? K : 1][N];
+                float k[N], t[N], b[N], keep[Op::KEEP ? K : 1][N], add[Op::KEEP ? K : 1][N];
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
-                    float kj[N], bj[N];
-                    op.map(raw[j], kj, bj);
+                    float kj[N], tj[N], bj[N];
+                    op.map(raw[j], kj, tj, bj);
                     const bool starting = starts >> j & 1;
                     if (j == 0) {
 #pragma unroll
@@ -270,6 +277,7 @@ template <class Op> struct Walk {
 #pragma unroll
                     for (int c = 0; c < N; ++c) {
                         b[c] = fmaf(kj[c], b[c], bj[c]);
+                        t[c] = j ? fmaf(tj[c], k[c], t[c]) : tj[c];
                         k[c] = j ? k[c] * kj[c] : kj[c];
                         if constexpr (Op::KEEP) {
                             keep[j][c] = kj[c];
@@ -278,7 +286,9 @@ template <class Op> struct Walk {
                     }
                 }
                 float h[N];
-                join(k, b, starts != 0, h);
+                join(k, t, b, starts != 0, h);
+                int64_t p0 = Op::BACK ? here - 1 - i0 : here + i0;
+                asm("" : "+v"(p0));  // known here: addresses of all K outputs carried along the loop take 32 registers
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     const bool starting = starts >> j & 1, ending = ends >> j & 1;
@@ -288,7 +298,7 @@ template <class Op> struct Walk {
 #pragma unroll
                         for (int c = 0; c < N; ++c) h[c] = starting ? (Op::EARLY ? early[j][c] : first[c]) : h[c];
                     }
-                    const int64_t p = Op::BACK ? here - 1 - (i0 + j) : here + i0 + j;
+                    const int64_t p = Op::BACK ? p0 - j : p0 + j;
                     if constexpr (Op::KEEP) {
 #pragma unroll
                         for (int c = 0; c < N; ++c) h[c] = fmaf(keep[j][c], h[c], add[j][c]);
@@ -310,13 +320,14 @@ template <class Op> struct Walk {
             const int many = (int)min(n - done, (int64_t)LAST_STAGE);
             stage_entries<false, LAST_STAGE>(rows, m, here, many, row);
             const int stretch = (many + LAST_TILE - 1) / LAST_TILE * STEP, first = group * stretch;
-            float k[N], b[N], head_k[N], head_b[N];
+            float k[N], t[N], b[N], head_k[N], head_b[N];
             int head = -1;
             bool seen = false;
 #pragma unroll
             for (int c = 0; c < N; ++c) {
-                k[c] = head_k[c] = 1.f;
-                b[c] = head_b[c] = 0.f;
+                k[c] = 1.f;
+                head_k[c] = KEEPS_ALL;
+                t[c] = b[c] = head_b[c] = 0.f;
             }
             typename Op::Raw raw[2][STEP];
             auto load = [&](auto which, int at) {
@@ -332,8 +343,8 @@ template <class Op> struct Walk {
                 for (int j = 0; j < STEP; ++j) {
                     const int i = min(first + at + j, LAST_STAGE - 1);
                     const int start = m.start[i], end = m.end[i];
-                    float kj[N], bj[N];
-                    op.map(raw[which()][j], kj, bj);
+                    float kj[N], tj[N], bj[N];
+                    op.map(raw[which()][j], kj, tj, bj);
                     if (__any(start >= 0)) {
                         float s0[N];
                         op.begin(max(start, 0), lane, s0);
@@ -345,14 +356,17 @@ template <class Op> struct Walk {
                     for (int c = 0; c < N; ++c) b[c] = Op::ONES ? b[c] + bj[c] : fmaf(kj[c], b[c], bj[c]);
                     if (!Op::ONES && open) {
 #pragma unroll
-                        for (int c = 0; c < N; ++c) k[c] *= kj[c];
+                        for (int c = 0; c < N; ++c) {
+                            t[c] = fmaf(tj[c], k[c], t[c]);
+                            k[c] *= kj[c];
+                        }
                     }
                     if (__any(end >= 0)) {
                         if (__any(end >= 0 && !seen)) {
                             const bool wait = end >= 0 && !seen;
 #pragma unroll
                             for (int c = 0; c < N; ++c) {
-                                head_k[c] = wait ? k[c] : head_k[c];
+                                head_k[c] = wait ? share_of(k[c], t[c]) : head_k[c];
                                 head_b[c] = wait ? b[c] : head_b[c];
                             }
                             head = wait ? end : head;
@@ -373,10 +387,10 @@ template <class Op> struct Walk {
                 }
             }
             float in[N];
-            join(k, b, seen, in);
+            join(k, t, b, seen, in);
             if (__any(head >= 0)) {
 #pragma unroll
-                for (int c = 0; c < N; ++c) head_b[c] = Op::ONES ? head_b[c] + in[c] : fmaf(head_k[c], in[c], head_b[c]);
+                for (int c = 0; c < N; ++c) head_b[c] = after<Op>(head_k[c], in[c], head_b[c]);
                 op.finish(max(head, 0), head >= 0, lane, head_b);
             }
         }
@@ -386,11 +400,13 @@ template <class Op> struct Walk {
     // `row` >= 0; to `out` [2][d].  Every group takes a stretch.
     __device__ void piece(int64_t from, int64_t n, int64_t row, float *out) {
         const int64_t stretch = (n + LAST_TILE - 1) / LAST_TILE * STEP, first = group * stretch;
-        float k[N], b[N];
+        float k[N], b[N];           // of all entries so far: the share that is kept, what is added
+        float rk[N], rt[N], rb[N];  // of the last up to 32, as products
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            k[c] = 1.f;
-            b[c] = 0.f;
+            k[c] = KEEPS_ALL;
+            rk[c] = 1.f;
+            b[c] = rt[c] = rb[c] = 0.f;
         }
         if (row >= 0) {  // the first group's stretch begins with the row
             float s0[N];
@@ -398,7 +414,7 @@ template <class Op> struct Walk {
 #pragma unroll
             for (int c = 0; c < N; ++c) {
                 b[c] = group == 0 ? s0[c] : 0.f;
-                k[c] = group == 0 ? 0.f : 1.f;
+                k[c] = group == 0 ? 0.f : KEEPS_ALL;
             }
         }
         int id[STEP];
@@ -421,21 +437,32 @@ template <class Op> struct Walk {
             if (at + STEP < stretch) find(at + STEP);
 #pragma unroll
             for (int j = 0; j < STEP; ++j) {
-                float kj[N], bj[N];
-                op.map(raw[j], kj, bj);
+                float kj[N], tj[N], bj[N];
+                op.map(raw[j], kj, tj, bj);
                 if (Op::BACK) {  // gradients of entries without an item count, those behind the end do not
                     const bool on = first + at + j < n;
 #pragma unroll
                     for (int c = 0; c < N; ++c) {
                         bj[c] = on ? bj[c] : 0.f;
                         kj[c] = on ? kj[c] : 1.f;
+                        tj[c] = on ? tj[c] : 0.f;
                     }
                 }
 #pragma unroll
                 for (int c = 0; c < N; ++c) {
-                    b[c] = Op::ONES ? b[c] + bj[c] : fmaf(kj[c], b[c], bj[c]);
-                    k[c] *= kj[c];
+                    rb[c] = Op::ONES ? rb[c] + bj[c] : fmaf(kj[c], rb[c], bj[c]);
+                    if (!Op::ONES) rt[c] = fmaf(tj[c], rk[c], rt[c]);
+                    if (!Op::ONES) rk[c] *= kj[c];
                 }
+            }
+            if (at + STEP < stretch && (at / STEP + 1) % (32 / STEP) != 0) continue;
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                const float q = share_of(rk[c], rt[c]);
+                b[c] = after<Op>(q, b[c], rb[c]);
+                if (!Op::ONES) k[c] = share_of_both(k[c], q);
+                rk[c] = 1.f;
+                rt[c] = rb[c] = 0.f;
             }
         }
 #pragma unroll
@@ -444,8 +471,8 @@ template <class Op> struct Walk {
             for (int c = 0; c < N; ++c) {
                 const float bo = __shfl_up(b[c], step * L), ko = __shfl_up(k[c], step * L);
                 const bool take = group >= step;
-                b[c] = take ? fmaf(k[c], bo, b[c]) : b[c];
-                k[c] = take ? k[c] * ko : k[c];
+                b[c] = chosen(take, after<Op>(k[c], bo, b[c]), b[c]);
+                if (!Op::ONES) k[c] = chosen(take, share_of_both(ko, k[c]), k[c]);
             }
         }
         if (group == GROUPS - 1) {
@@ -520,8 +547,8 @@ template <class Op, bool CARRY> struct Pieces {
     __device__ __forceinline__ int64_t at(int i) const {
         return min(max(CARRY ? (Op::BACK ? chunk - i : chunk + i) : chunk - count + i, (int64_t)0), c.count - 1);
     }
-    // pieces begin .. end - 1, which may be other ones in every lane: the loop is the wavefront's
-    template <bool STORE> __device__ __forceinline__ void walk(int begin, int end) {
+    // pieces begin .. end - 1, which may be other ones in every lane: the loop is the wavefront's.  MAP: the share k too
+    template <bool STORE, bool MAP> __device__ __forceinline__ void walk(int begin, int end) {
         for (int i0 = begin; __any(i0 < end); i0 += AHEAD) {
             float kp[AHEAD][N], bp[AHEAD][N];
 #pragma unroll
@@ -538,9 +565,9 @@ template <class Op, bool CARRY> struct Pieces {
                 const bool on = i0 + a < end, first = i0 + a == 0;  // the first piece has the row's own first state in it
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    const float behind = fmaf(kp[a][j], s[j], bp[a][j]), now = first ? bp[a][j] : behind;
+                    const float behind = after<Op>(kp[a][j], s[j], bp[a][j]), now = first ? bp[a][j] : behind;
                     s[j] = on ? now : s[j];
-                    k[j] = on ? k[j] * kp[a][j] : k[j];
+                    if (MAP && !Op::ONES) k[j] = chosen(on, share_of_both(k[j], kp[a][j]), k[j]);
                 }
                 if (STORE && on) {
                     float *to = c.close + (at(i0 + a + 1) * 2 + 1) * D + lane * N;
@@ -553,7 +580,7 @@ template <class Op, bool CARRY> struct Pieces {
     __device__ __forceinline__ void finish(const Op &op, int row, bool mine) {
         const float *map = c.close + chunk * 2 * D + lane * N;
 #pragma unroll
-        for (int j = 0; j < N; ++j) s[j] = fmaf(map[j], s[j], map[D + j]);
+        for (int j = 0; j < N; ++j) s[j] = after<Op>(map[j], s[j], map[D + j]);
         op.finish(row, mine, lane, s);
     }
 };
@@ -574,7 +601,7 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void walk_all_ke
             const int64_t from = Op::BACK ? min((r.at_high.e - 1) / c.size, c.count - 1) : r.at_low.b / c.size;
             const int pieces = (int)(Op::BACK ? from - chunk : chunk - from);
             Pieces<Op, true> p{c, from, pieces, walk.lane, {}, {}};
-            p.template walk<false>(0, pieces);
+            p.template walk<false, false>(0, pieces);
 #pragma unroll
             for (int j = 0; j < Op::N; ++j) walk.s[j] = p.s[j];
         } else {
@@ -623,7 +650,7 @@ template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void 
             const int64_t chunk = chunk0 + few_at[min(n, many - 1)];
             const JoinedRow r = c.rows[chunk];
             Pieces<Op, CARRY> p{c, chunk, r.pieces, lane, {}, {}};
-            p.template walk<CARRY>(0, mine ? r.pieces : 0);
+            p.template walk<CARRY, false>(0, mine ? r.pieces : 0);
             if (!CARRY) p.finish(op, r.row, mine);
         }
     }
@@ -635,8 +662,8 @@ template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void 
         const int groups = (r.pieces + each - 1) / each;
         Pieces<Op, CARRY> p{c, chunk, r.pieces, (int)blockIdx.y * LANES + in_group, {}, {}};
 #pragma unroll
-        for (int j = 0; j < N; ++j) p.k[j] = 1.f;
-        p.template walk<false>(begin, end);
+        for (int j = 0; j < N; ++j) p.k[j] = KEEPS_ALL;
+        p.template walk<false, true>(begin, end);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             maps[group][0][in_group * N + j] = p.k[j];
@@ -647,10 +674,11 @@ template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void 
         for (int g = 0; __any(g < upto); ++g)
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float bg = maps[g][1][in_group * N + j], behind = fmaf(maps[g][0][in_group * N + j], p.s[j], bg), now = g ? behind : bg;
+                const float bg = maps[g][1][in_group * N + j], behind = after<Op>(maps[g][0][in_group * N + j], p.s[j], bg);
+                const float now = g ? behind : bg;
                 p.s[j] = g < upto ? now : p.s[j];
             }
-        if (CARRY) p.template walk<true>(begin, end);
+        if (CARRY) p.template walk<true, false>(begin, end);
         else p.finish(op, r.row, group == 0);
         __syncthreads();
     }

@@ -33,15 +33,14 @@ template <int D, bool BF, bool SBF, bool STATES> struct Forward {
         r.g = *(const Words *)(item_row(F, id, no_g) + lane * 16);
     }
     __device__ __forceinline__ void load_map(Raw &r, int64_t p, int id, int lane) const { load(r, p, id, lane); }
-    __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&b)[N]) const {
+    __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&t)[N], float (&b)[N]) const {
         float x[N], g[N];
         widen<BF, N>(r.x, x);
         widen<BF, N>(r.g, g);
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            float take;
-            gate(g[c], k[c], take);
-            b[c] = take * x[c];
+            gate(g[c], k[c], t[c]);
+            b[c] = t[c] * x[c];
         }
     }
     __device__ __forceinline__ void begin(int64_t row, int lane, float (&s)[N]) const {
@@ -79,14 +78,13 @@ template <int D, bool BF, bool SBF> struct Backward {
         r.x = *(const Part<BF> *)(item_row(V, id, no_x) + lane * sizeof(Part<BF>));
         r.h = *(const Part<SBF> *)(states.p + max(p - 1, (int64_t)0) * states.ld + lane * sizeof(Part<SBF>));
     }
-    __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&b)[N]) const {
+    __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&t)[N], float (&b)[N]) const {
         float g[N], d[N];
         widen<BF, N>(r.g, g);
         widen<SBF, N>(r.d, d);
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            float take;
-            gate(g[c], k[c], take);
+            gate(g[c], k[c], t[c]);
             b[c] = k[c] * d[c];
         }
     }
@@ -145,7 +143,7 @@ __global__ __launch_bounds__(RECUR_THREADS) void recur_step_kernel(int64_t rows,
             for (int c = 0; c < N; ++c) {
                 float keep, take;
                 gate(g[c], keep, take);
-                h[c] = fmaf(keep, h[c], take * x[c]);
+                h[c] = after_map(share_of(keep, take), h[c], take * x[c]);
             }
         }
         store_piece(X, u, lane, h);

@@ -21,11 +21,12 @@ template <int D, bool BF> struct SumRows {
         r.w = id < 0 || !values ? 1.f : values[p];
     }
     __device__ __forceinline__ void load_map(Raw &r, int64_t p, int id, int lane) const { load(r, p, id, lane); }
-    __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&b)[N]) const {
+    __device__ __forceinline__ void map(const Raw &r, float (&k)[N], float (&t)[N], float (&b)[N]) const {
         widen<BF, N>(r.x, b);
 #pragma unroll
         for (int c = 0; c < N; ++c) {
             k[c] = 1.f;
+            t[c] = 0.f;
             b[c] *= r.w;
         }
     }
