@@ -89,8 +89,11 @@ constexpr float KEEPS_ALL = -0.f;
 __device__ __forceinline__ float share_of(float keep, float take) { return take < 0.125f ? -take : keep; }
 // `s` where the sign of `q` is set, 0 elsewhere
 __device__ __forceinline__ float where_negative(float q, float s) { return __int_as_float(__float_as_int(s) & __float_as_int(q) >> 31); }
-// the state s after a map with share q and what it adds
-__device__ __forceinline__ float after_map(float q, float s, float b) { return fmaf(q, s, b) + where_negative(q, s); }
+// the state s after a map with share q and what it adds; what an infinite state gives away is a number, so that it stays
+__device__ __forceinline__ float after_map(float q, float s, float b) {
+    const float number = __builtin_amdgcn_fmed3f(s, -__FLT_MAX__, __FLT_MAX__);
+    return fmaf(q, __float_as_int(q) < 0 ? number : s, b) + where_negative(q, s);
+}
 // The share of two maps after each other: p q of kept ones; -(t + v - t v) of t and v given away, q (1 - t) of one of each.  What is
 // given away stays below 1/2, else 1 + k, which is exact, is what is kept.
 __device__ __forceinline__ float share_of_both(float p, float q) {
