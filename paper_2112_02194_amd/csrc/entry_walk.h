@@ -20,7 +20,9 @@
 //                           the card holds of the entries at a time (128 MB of registers) is a tenth of a large call's.
 // Memory bounds all of it for large calls (figures at the operators).  A wavefront is its own workgroup: nothing waits for others.
 // Chunks: 512, 494, 490, 521 us with 8192, 16384, 32768, 65536 of them for the last states of 300000 rows (d = 128, bf16); rows of up to
-// 1, 2, 4, 8 chunks uncut 494, 514, 592, 701: a long row at the end keeps one wavefront busy and the others wait.
+// 1, 2, 4, 8 chunks uncut 494, 514, 592, 701: a long row at the end keeps one wavefront busy and the others wait.  Where all states are
+// wanted, and entries of cut rows are read twice, it is the same: their states 1364 and 1380 us with 1 and 2 chunks uncut, gradients of a
+// page of 2000 rows of 20 (d = 64) 42.6 and 50.
 //
 // Both walks, along a row and from its end, are this one: index i counts in the direction of the walk.  Branches and loops around values
 // are the wavefront's, never some lanes' (those have stores alone), and no vector register is spilled: the compiler was seen to place a
@@ -38,7 +40,10 @@ namespace als {
 constexpr int WALK_STAGE = 128;         // entries whose ids and marks are in LDS at a time
 constexpr int LAST_STAGE = 512;         // the same where only last states are wanted: the groups' maps are joined once a stage
 constexpr int WALK_MAX_CHUNKS = 32768;  // 2 KB of workspace each
-constexpr int FEW_CHUNKS = 48;          // a row's pieces among so few are composed by every wavefront that needs them
+// A row's pieces among so few chunks are composed by every wavefront that needs them, without a launch of their own: the states of a row of
+// 300 entries 16.5 us instead of 20.3 (d = 64), of 1000 17.8 and 21.0; from 2000 on, beyond it, the same.  With 192 instead of 48, 21 us for
+// 2000 entries and 38 for 6000: a wavefront composes a hundred pieces.
+constexpr int FEW_CHUNKS = 48;
 
 // Chunks, and what is kept of each for rows that cross its border: maps (k, b) of `d` columns.
 //   across  of the part of a long row up to the border that the walk leaves the chunk by
@@ -629,6 +634,8 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kern
 // A workgroup looks at 64 chunks (16 rows of 1024 pieces of d = 128: 16 us; one workgroup a row without a second dimension 37).  Rows of
 // a few pieces: a group of lanes each.  Others: their pieces are dealt out in stretches to all groups, whose maps are joined through
 // LDS; the columns are dealt out to the workgroups of a second dimension.
+// JOIN_FEW: 8, 24, 72 are within a percent of each other where rows are of all lengths (gradients of 100000 rows 570, 569, 576 us) or
+// all long; rows of 3000 entries 487, 486, 475.
 constexpr int JOIN_THREADS = 512, JOIN_CHUNKS = 64, JOIN_FEW = 24;
 template <class Op> constexpr int join_lanes() { return Op::L < 8 ? Op::L : 8; }
 template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(Op op, Chunks c) {
@@ -684,16 +691,16 @@ template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void 
     }
 }
 
-// Chunks of the call's entries, and the longest rows that are not cut, in chunks (4 tiles at least).  For small calls as many as the
+// Chunks of the call's entries, and the longest rows that are not cut: a chunk, 4 tiles at least.  For small calls as many as the
 // card holds wavefronts, of a tile at least; then of 64 entries, so that a chunk's search for its rows does not weigh; then as many as
 // there is room for.
-inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile, int longest) {
+inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile) {
     Chunks c{};
     const int64_t resident = (int64_t)ctx->num_cu * 12;
     const int64_t wanted = std::max((nnz + WALK_MAX_CHUNKS - 1) / WALK_MAX_CHUNKS, std::min<int64_t>(64, (nnz + resident - 1) / resident));
     c.size = std::max<int64_t>(1, (wanted + tile - 1) / tile) * tile;
     c.count = (nnz + c.size - 1) / c.size;
-    c.longest = longest * std::max<int64_t>(c.size, 4 * tile);
+    c.longest = std::max<int64_t>(c.size, 4 * tile);
     c.across = (float *)ctx->walk_maps.p;
     c.close = c.across + (int64_t)WALK_MAX_CHUNKS * 2 * 128;
     c.rows = (JoinedRow *)(c.close + (int64_t)WALK_MAX_CHUNKS * 2 * 128);
@@ -702,12 +709,12 @@ inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile, int longest) 
 // behind the chunks': rows for entries without an item, 512 bytes each: zeros, gates in fp32, gates in bf16
 constexpr size_t WALK_NONE = (size_t)WALK_MAX_CHUNKS * (4 * 128 * sizeof(float) + sizeof(JoinedRow)), WALK_BYTES = WALK_NONE + 3 * 512;
 inline const char *none_row(const als_ctx *ctx, bool gates, bool bf16) { return (const char *)ctx->walk_maps.p + WALK_NONE + (!gates ? 0 : bf16 ? 1024 : 512); }
-constexpr int EMPTY_GROUPS = 4096;  // workgroups that look for empty rows, at most
+constexpr int EMPTY_GROUPS = 4096;  // workgroups that look for empty rows, at most (1M empty rows 52, 48, 45 us with 1024, 4096, 16384; 30M 1437, 1507, 1514)
 template <class Op> dim3 join_grid(const Chunks &c) { return dim3((unsigned)((c.count + JOIN_CHUNKS - 1) / JOIN_CHUNKS), Op::L / join_lanes<Op>()); }
 inline unsigned walk_grid(const Chunks &c, int64_t rows) { return (unsigned)(c.count + std::min<int64_t>((rows + 63) / 64, EMPTY_GROUPS)); }
 
 template <class Op> void launch_last(const als_ctx *ctx, const Op &op, const als_csr *Y, hipStream_t s) {
-    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::LAST_TILE, 1);
+    const Chunks c = chunks_of(ctx, Y->nnz, Walk<Op>::LAST_TILE);
     const Lists y = lists_of(Y);
     hipLaunchKernelGGL((walk_last_kernel<Op>), dim3(walk_grid(c, Y->rows)), dim3(64), 0, s, op, y, c);
     if (Y->nnz > c.longest) hipLaunchKernelGGL((join_kernel<Op, false>), join_grid<Op>(c), dim3(JOIN_THREADS), 0, s, op, c);
