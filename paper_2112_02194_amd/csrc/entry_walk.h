@@ -19,10 +19,10 @@
 //                           The tables are read twice for entries of long rows; a row's maps cannot wait for the rows before, and what
 //                           the card holds of the entries at a time (128 MB of registers) is a tenth of a large call's.
 // Memory bounds all of it for large calls (figures at the operators).  A wavefront is its own workgroup: nothing waits for others.
-// Chunks: 512, 494, 490, 521 us with 8192, 16384, 32768, 65536 of them for the last states of 300000 rows (d = 128, bf16); rows of up to
-// 1, 2, 4, 8 chunks uncut 494, 514, 592, 701: a long row at the end keeps one wavefront busy and the others wait.  Where all states are
-// wanted, and entries of cut rows are read twice, it is the same: their states 1364 and 1380 us with 1 and 2 chunks uncut, gradients of a
-// page of 2000 rows of 20 (d = 64) 42.6 and 50.
+// Chunks: 495, 482, 489, 562 us with 8192, 16384, 32768, 65536 of them for the last states of 300000 rows (d = 128, bf16), 1435, 1363, 1365,
+// 1442 for all states.  Rows of up to 1, 2, 4, 8 chunks uncut 489, 497, 524, 575: a long row at the end keeps one wavefront busy and the
+// others wait.  Where all states are wanted, and entries of cut rows are read twice, it is the same: 1365, 1380, 1416, 1483, and gradients
+// of a page of 2000 rows of 20 (d = 64) 42.6 and 50 with 1 and 2.
 //
 // Both walks, along a row and from its end, are this one: index i counts in the direction of the walk.  Branches and loops around values
 // are the wavefront's, never some lanes' (those have stores alone), and no vector register is spilled: the compiler was seen to place a
@@ -631,10 +631,9 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kern
     Walk<Op>(op, f).piece(Op::BACK ? high : low, high - low, r.through() ? -1 : row.u, c.across + chunk * 2 * D);
 }
 
-// A workgroup looks at 64 chunks (16 rows of 1024 pieces of d = 128: 16 us; one workgroup a row without a second dimension 37).  Rows of
-// a few pieces: a group of lanes each.  Others: their pieces are dealt out in stretches to all groups, whose maps are joined through
-// LDS; the columns are dealt out to the workgroups of a second dimension.
-// JOIN_FEW: 8, 24, 72 are within a percent of each other where rows are of all lengths (gradients of 100000 rows 570, 569, 576 us) or
+// A workgroup looks at 64 chunks (16 rows of 1024 pieces of d = 128: 21 us).  Rows of a few pieces: a group of lanes each.  Others: their
+// pieces are dealt out in stretches to all groups, whose maps are joined through LDS; the columns are dealt out to the workgroups of a
+// second dimension.  JOIN_FEW: 8, 24, 72 are within a percent of each other where rows are of all lengths (gradients of 100000 rows 570, 569, 576 us) or
 // all long; rows of 3000 entries 487, 486, 475.
 constexpr int JOIN_THREADS = 512, JOIN_CHUNKS = 64, JOIN_FEW = 24;
 template <class Op> constexpr int join_lanes() { return Op::L < 8 ? Op::L : 8; }

@@ -2,12 +2,12 @@
 // dealt out stands in entry_walk.h; here are an entry's maps and outputs.
 //
 // Bytes that have to be moved, at the rates of a large copy (4.7 to 4.9 TB/s read and written), and what was measured:
-//   last states  300000 rows, 6.0M entries, d = 128, tables of 1M rows in bf16 (popular items often)  457 us.  3.1 GB gathered; 29 % from the
-//                L2, 2.8 GB from behind it at 6 TB/s, more than a copy's rate: the last-level cache has popular rows.  Vector units next:
-//                13 instruction slots an entry and column (exponential and reciprocal are 8 of them), 0.26 ms of the time
-//   all states   16 rows of 65537 entries, d = 128, fp32  518 us: pieces 220 (1.07 GB), their states 16, the walk 283 (1.61 GB)
-//   gradients    100000 rows, 2.0M entries, d = 64, fp32  565 us: 0.25 GB in pieces 70, the walk 490 (2.2 GB and what the cache misses of the
-//                gathers); 16 x 65537 in bf16 with fp32 states  702 us: 190 (0.8 GB), 24, 490 (2.7 GB)
+//   last states  300000 rows, 6.0M entries, d = 128, tables of 1M rows in bf16 (popular items often)  484 us.  3.1 GB gathered, 2.8 of them
+//                from behind the L2: 5.9 TB/s, about what reading alone reaches.  The vector units are at work for 84 % of the time (18
+//                instructions an entry and column, of which the exponential and the reciprocal take four slots each)
+//   all states   16 rows of 65537 entries, d = 128, fp32  527 us: pieces 217 (1.07 GB), their states 21, the walk 280 (1.61 GB)
+//   gradients    100000 rows, 2.0M entries, d = 64, fp32  568 us: 0.27 GB in pieces 75, joined 14, the walk 471 (2.2 GB and what the cache
+//                misses of the gathers); 16 x 65537 in bf16 with fp32 states  700 us: 175 (0.8 GB), 21, 490 (2.7 GB)
 #include <algorithm>
 #include <type_traits>
 

@@ -1,7 +1,9 @@
-// Sums of a table's rows over the rows of a CSR matrix (als_sum_rows): the walk of entry_walk.h with maps s -> s + y x.  A sum is fp32
-// over stretches of a chunk's entries, then over the stretches and chunks of a long row: its error does not grow with the row's length
-// alone.  Memory bound: the gradient of 1M items from 6.0M entries, d = 64, fp32  400 us for 1.82 GB, 4.5 TB/s in rows of 256 bytes
-// anywhere; items with one entry and with 60000 are the same work.
+// Sums of a table's rows over the rows of a CSR matrix (als_sum_rows): the walk of entry_walk.h with maps s -> s + y x.  A sum is fp32: a
+// running one of up to 256 entries in a lane's stretch (32, and sums of these, where a row is cut), then of the lane groups, of a lane's
+// up to 512 pieces and of 64 to 256 lanes.  So an entry is rounded some hundred times on its way into the sum of a long row, below 2000
+// of 2^31 entries, where one running sum would round it once for every entry behind it.  Memory bound: the gradient of 1M items
+// from 6.0M entries, d = 64, fp32  398 us for 1.82 GB, 4.6 TB/s in rows of 256 bytes anywhere; items with one entry and with 60000 are
+// the same work.
 #include "entry_walk.h"
 
 namespace als {
