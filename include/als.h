@@ -270,6 +270,7 @@ als_status als_select(als_ctx *ctx, const als_matrix *X, const als_rules *rules,
  *   states  NULL, or the state after each entry: Y->nnz rows in Y's order
  *   last    NULL, or the state after the last entry: Y->rows rows, a row's h_0 where it has no entry
  * H0, states and last are in fp32 or bf16 each; states are fp32 within the call and are rounded where they are written.
+ * states and last overlap neither each other nor what is read, H0 among it (als_recur_step may write where it reads).
  * exp(-F) is that of F = -87.34 for lower F.  What is infinite or NaN stays in its row and column; an infinite state may become NaN.
  * Rows of states that belong to no row of Y (before indptr[0], behind indptr[rows]) are left as they are. */
 als_status als_recur(als_ctx *ctx, const als_csr *Y, const als_table *V, const als_table *F, const als_table *H0,
