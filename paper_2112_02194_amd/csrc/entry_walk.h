@@ -633,8 +633,8 @@ template <class Op> __global__ __launch_bounds__(64, Op::WAVES) void pieces_kern
 
 // A workgroup looks at 64 chunks (16 rows of 1024 pieces of d = 128: 21 us).  Rows of a few pieces: a group of lanes each.  Others: their
 // pieces are dealt out in stretches to all groups, whose maps are joined through LDS; the columns are dealt out to the workgroups of a
-// second dimension.  JOIN_FEW: 8, 24, 72 are within a percent of each other where rows are of all lengths (gradients of 100000 rows 570, 569, 576 us) or
-// all long; rows of 3000 entries 487, 486, 475.
+// second dimension.  JOIN_FEW: 8, 24, 72 are within a percent of each other where rows are of all lengths (gradients of 100000 rows 570,
+// 569, 576 us) or all long; rows of 3000 entries 487, 486, 475.
 constexpr int JOIN_THREADS = 512, JOIN_CHUNKS = 64, JOIN_FEW = 24;
 template <class Op> constexpr int join_lanes() { return Op::L < 8 ? Op::L : 8; }
 template <class Op, bool CARRY> __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(Op op, Chunks c) {
@@ -708,7 +708,8 @@ inline Chunks chunks_of(const als_ctx *ctx, int64_t nnz, int tile) {
 // behind the chunks': rows for entries without an item, 512 bytes each: zeros, gates in fp32, gates in bf16
 constexpr size_t WALK_NONE = (size_t)WALK_MAX_CHUNKS * (4 * 128 * sizeof(float) + sizeof(JoinedRow)), WALK_BYTES = WALK_NONE + 3 * 512;
 inline const char *none_row(const als_ctx *ctx, bool gates, bool bf16) { return (const char *)ctx->walk_maps.p + WALK_NONE + (!gates ? 0 : bf16 ? 1024 : 512); }
-constexpr int EMPTY_GROUPS = 4096;  // workgroups that look for empty rows, at most (1M empty rows 52, 48, 45 us with 1024, 4096, 16384; 30M 1437, 1507, 1514)
+// Workgroups that look for empty rows, at most: 1M empty rows take 52, 48, 45 us with 1024, 4096, 16384 of them, 30M 1437, 1507, 1514.
+constexpr int EMPTY_GROUPS = 4096;
 template <class Op> dim3 join_grid(const Chunks &c) { return dim3((unsigned)((c.count + JOIN_CHUNKS - 1) / JOIN_CHUNKS), Op::L / join_lanes<Op>()); }
 inline unsigned walk_grid(const Chunks &c, int64_t rows) { return (unsigned)(c.count + std::min<int64_t>((rows + 63) / 64, EMPTY_GROUPS)); }
 
